@@ -436,6 +436,182 @@ int brisk_accept_profile(const int32_t* accept_len, int32_t n_blocks, int32_t M,
                          double* a, double* w_raw, double* w, double* tpf_fpt,
                          void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Operators around the step: the attention that makes a block's hidden states
+ * from a shared prefix and a paged cache, the weights and the eviction that
+ * keep that cache short, and verification from given probabilities (Section
+ * 2.1 strided decoding, Section 3.3 verification, Algorithm 1(b)).
+ * ---------------------------------------------------------------------------
+ */
+typedef enum { BRISK_BF16 = 0, BRISK_F16 = 1 } brisk_dtype;
+
+/*
+ * A paged key/value cache (host struct of device pointers and sizes).  Slot j
+ * of sequence b lies in page block_table[b, j / page_size] at place
+ * j % page_size; its key for key/value head h starts at element
+ *   page * page_stride + place * slot_stride + h * head_stride
+ * of k_pages, its value at the same element of v_pages, and the d_head
+ * elements of both are contiguous.  Offsets are computed in 64 bits.  Page
+ * ids are clamped into [0, n_pages), lengths into what the table addresses.
+ *
+ * Limits: 1 <= n_kv_heads <= 1024; d_head a multiple of 8 in [8, 128];
+ * page_size a power of two in [1, 65536]; n_pages, max_pages >= 1; max_pages *
+ * page_size <= 2^30; strides non-negative multiples of 8; k_pages and v_pages
+ * 16-byte aligned.
+ */
+typedef struct brisk_kv_cache {
+  int32_t dtype;             /* brisk_dtype of keys, values, queries, outputs */
+  int32_t n_kv_heads, d_head, page_size, n_pages, max_pages;
+  int64_t page_stride, slot_stride, head_stride;   /* in elements             */
+  uint16_t* k_pages;
+  uint16_t* v_pages;
+  const int32_t* block_table;  /* [B, max_pages]                              */
+  const int32_t* seq_len;      /* [B] slots held, the block's own included    */
+} brisk_kv_cache;
+
+/* Keys and values that every sequence of a batch shares, held once: key j of
+ * head h starts at element j * slot_stride + h * head_stride of k, its value
+ * at the same element of v.  Type, heads and d_head are the cache's; strides
+ * and alignment as there; 0 <= len <= 2^30. */
+typedef struct brisk_kv_prefix {
+  int32_t len;
+  int64_t slot_stride, head_stride;
+  const uint16_t* k;
+  const uint16_t* v;
+} brisk_kv_prefix;
+
+/* Workspace bytes brisk_block_attention needs (written to *bytes). */
+int brisk_block_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads,
+                                         int32_t d_head, int32_t prefix_len, int32_t max_seq_len,
+                                         size_t* bytes);
+
+/*
+ * Attention of every sequence's block over the shared prefix and its own
+ * cache.  The rows are the L positions of each block (L = 1: single-token
+ * decoding) times n_heads query heads; query head h reads key/value head
+ * h / (n_heads / n_kv_heads).  The block's own keys are the last L slots of
+ * its sequence (already written to the cache): with n = seq_len[b], position
+ * i sees every prefix key, every slot below n - L, and slot n - L + t when
+ * bit t of block_mask[b, i] is set (all of them when block_mask is NULL).
+ *   out = sum_j softmax_j(scale * <q, k_j>) v_j,   lse = log sum_j exp(scale * <q, k_j>)
+ * over the visible keys.  A row that sees no key gets out = 0, lse = -inf.
+ * What lies in slots that a row does not see has no effect on it, infinities
+ * and NaN included.  The prefix is read once for all sequences.
+ *
+ *   q           element (b * L + i) * q_row_stride + h * q_head_stride starts
+ *               the d_head contiguous elements of a row; strides multiples of 8
+ *   block_mask  [B, L] uint64, nullable
+ *   max_seq_len host bound of the lengths (longer ones are cut to it); 0 when
+ *               no sequence holds a key
+ *   out         [B*L, n_heads, d_head], the cache's type
+ *   lse         [B*L, n_heads] fp32, nullable
+ *   ws          device scratch of brisk_block_attention_workspace_size bytes
+ *
+ * Limits: 1 <= L <= 64, B >= 1, n_heads a multiple of n_kv_heads with
+ * B * L * n_heads <= 2^24, 0 <= max_seq_len <= max_pages * page_size,
+ * scale > 0 and finite.  Sums, maxima and partial outputs are held in fp32;
+ * probabilities are rounded to the cache's type where they meet the values.
+ * Deterministic.
+ */
+int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* prefix, const uint16_t* q,
+                          int64_t q_row_stride, int64_t q_head_stride, const uint64_t* block_mask,
+                          int32_t B, int32_t L, int32_t n_heads, int32_t max_seq_len, float scale,
+                          uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention weight received by every cached key (the measure by which
+ * brisk_cache_evict chooses).  For n = seq_len[b] and slots j < n:
+ *   score_out[b, h, j] = decay * score_in[b, h, j] + sum over the rows (i, query heads of group h)
+ *                        that see j of exp(scale * <q, k_j> - lse)
+ * and 0 for n <= j < cap.  q, block_mask, lse and L as given to and left by
+ * brisk_block_attention (so the weights are those over prefix and cache
+ * together); a row with lse = -inf adds nothing.
+ *
+ *   lse         [B*L, n_heads] fp32
+ *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array
+ *
+ * Limits as brisk_block_attention; 1 <= cap <= 2^30; lengths are cut to cap.
+ * Deterministic (fixed-order sums, no atomics).
+ */
+int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_row_stride,
+                      int64_t q_head_stride, const uint64_t* block_mask, const float* lse, int32_t B,
+                      int32_t L, int32_t n_heads, float scale, float decay, const float* score_in,
+                      float* score_out, int32_t cap, void* stream);
+
+/* Workspace bytes brisk_cache_evict needs (written to *bytes). */
+int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget,
+                                     size_t* bytes);
+
+/*
+ * Eviction to at most `budget` slots a sequence, each key/value head keeping
+ * its own keys.  For a sequence of n > budget slots, head h keeps first the
+ * slots with pos >= next_pos[b] - recent (the latest tokens), then those of
+ * the largest score; equal ones go to the lower slot, and a NaN score counts
+ * as the smallest.  Of the kept slots, those below budget stay where they
+ * are; the i-th kept slot at or above budget (ascending) moves, with its key,
+ * value, score and position, into the i-th evicted slot below budget
+ * (ascending).  A sequence of n <= budget slots keeps all.
+ *   new_len[b] = min(n, budget);
+ *   score_out, pos_out [b, h, j] = those of the slot now at j, for j < new_len; 0 and -1 beyond
+ * The slots' order carries no meaning for brisk_block_attention (keys hold
+ * their positions), so only moved slots are copied; the sources are left
+ * unchanged.  seq_len is not updated: the caller takes new_len, and releases
+ * the pages past it.
+ *
+ *   score_in, score_out  [B, n_kv_heads, cap] fp32;  pos_in, pos_out the same
+ *               in int32; outputs must not overlap the inputs
+ *   next_pos    [B] int32  position of the next token (tokens seen so far)
+ *   new_len     [B] int32 out
+ *   ws          device scratch of brisk_cache_evict_workspace_size bytes
+ *
+ * Limits: the cache's; B >= 1, B * n_kv_heads <= 2^20, 1 <= cap <= 2^24,
+ * budget >= 1, 0 <= recent <= budget; lengths are cut to cap.  Two sequences
+ * must not share a page that holds slots below budget of either.
+ */
+int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score_in,
+                      const int32_t* pos_in, int32_t cap, const int32_t* next_pos, int32_t budget,
+                      int32_t recent, float* score_out, int32_t* pos_out, int32_t* new_len, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* Workspace bytes brisk_draft_verify needs (written to *bytes). */
+int brisk_draft_verify_workspace_size(int32_t B, int32_t V, size_t* bytes);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, with the
+ * random numbers given (Section 3.3, speculative acceptance; Algorithm 1(b)
+ * verify and commit).  brisk_spec_verify is the form for a verifier's hidden
+ * states and a law over K candidates; this one takes laws over the whole
+ * vocabulary, as sampled or filtered by the caller.
+ *   position i of block b accepts x = draft_tok[b, i] when
+ *     u_accept[b, i] * draft_prob[b, i, x] < target_prob[b, i, x]   (fp32 product);
+ *   a = accept_len[b] = the positions before the first one that does not, at
+ *       most n = draft_len[b] (L when draft_len is NULL);
+ *   w = [target_prob[b, a] - draft_prob[b, a]]_+ when a < n, or
+ *       target_prob[b, a] when a = n or when that difference is positive nowhere;
+ *   token[b] = argmax_v w_v / noise[b, v] over the v with w_v > 0, the lower
+ *       id on ties; -1 when there is none.
+ * With noise drawn from Exp(1), token follows the law w / sum w, so committed
+ * tokens keep the target's law.
+ *
+ *   target_prob [B, L + 1, V] fp32, rows target_stride elements apart
+ *   draft_prob  [B, L, V]     fp32, rows draft_stride elements apart
+ *   draft_tok   [B, L] int32;  draft_len [B] int32, nullable (values are
+ *               clamped into [0, L]);  u_accept [B, L] fp32
+ *   noise       [B, V] fp32, rows noise_stride elements apart
+ *   accept_len, token  [B] int32 out
+ *   ws          device scratch of brisk_draft_verify_workspace_size bytes
+ *
+ * With L = 0 the draft's arrays may be NULL (a plain draw from the target).
+ * Limits: B >= 1, 0 <= L <= 1024, B * (L + 1) <= 2^20, 1 <= V <= 2^24, row
+ * strides >= V; 4-byte aligned pointers.
+ */
+int brisk_draft_verify(const float* target_prob, int64_t target_stride, const float* draft_prob,
+                       int64_t draft_stride, const int32_t* draft_tok, const int32_t* draft_len,
+                       const float* u_accept, const float* noise, int64_t noise_stride, int32_t B,
+                       int32_t L, int32_t V, int32_t* accept_len, int32_t* token, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,15 @@ Entry points (same names as the C ABI):
 * :func:`spec_verify` - stochastic speculative verification with residual draws;
 * :func:`accept_profile` - acceptance profile, tokens per forward and the
   risk-reward position weights from many blocks' accept lengths.
+
+Around the step, on a :class:`KVCache` of paged keys and values:
+
+* :func:`block_attention` - attention of every block (or single token) over a
+  prefix shared by the batch and its own cache;
+* :func:`cache_score` - the attention weight that every cached key received;
+* :func:`cache_evict` - eviction by that weight, in place;
+* :func:`draft_verify` - verification of drafted tokens against given
+  probabilities, with the random numbers given.
 """
 from __future__ import annotations
 
@@ -31,6 +40,7 @@ import torch
 
 __all__ = ["BriskError", "Corrector", "propose_block", "propose_block_noalloc", "propose_lmhead", "propose_merge", "rerank", "rerank_verify", "rerank_hoist", "rerank_finish", "verify_accept", "accept_profile",
            "propose_verify", "verify_commit", "corrector_loss", "spec_verify",
+           "KVCache", "block_attention", "cache_score", "cache_evict", "draft_verify",
            "lib", "LIB_PATH", "ABI_SYMBOLS", "propose_workspace_size", "rerank_workspace_size"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbrisk.so")
@@ -42,7 +52,10 @@ ABI_SYMBOLS = ("brisk_status_str", "brisk_abi_version", "brisk_propose_workspace
                "brisk_verify_accept", "brisk_propose_verify_workspace_size", "brisk_propose_verify",
                "brisk_verify_commit", "brisk_spec_verify_workspace_size", "brisk_spec_verify",
                "brisk_corrector_loss", "brisk_accept_profile_workspace_size",
-               "brisk_accept_profile", "brisk_corrector_tables_size", "brisk_corrector_prepare")
+               "brisk_accept_profile", "brisk_corrector_tables_size", "brisk_corrector_prepare",
+               "brisk_block_attention_workspace_size", "brisk_block_attention", "brisk_cache_score",
+               "brisk_cache_evict_workspace_size", "brisk_cache_evict",
+               "brisk_draft_verify_workspace_size", "brisk_draft_verify")
 PSI_FIELDS = ("A_h", "A_e", "P_h", "P_e", "pos_emb", "P_phi", "W_z", "W_h", "W_s", "W_c", "w_g")
 
 _p = ctypes.c_void_p
@@ -62,6 +75,16 @@ class _CorrectorC(ctypes.Structure):
     _fields_ = ([(n, _i32) for n in ("d_state", "d_hproj", "d_tproj", "d_pos", "d_feat", "rank", "max_L")]
                 + [(n, _p) for n in PSI_FIELDS]
                 + [("alpha", ctypes.c_float), ("b_g", ctypes.c_float), ("tables", _p), ("tables_V", _i32)])
+
+
+class _KVCacheC(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("dtype", "n_kv_heads", "d_head", "page_size", "n_pages", "max_pages")]
+                + [(n, ctypes.c_int64) for n in ("page_stride", "slot_stride", "head_stride")]
+                + [(n, _p) for n in ("k_pages", "v_pages", "block_table", "seq_len")])
+
+
+class _KVPrefixC(ctypes.Structure):
+    _fields_ = [("len", _i32), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("k", _p), ("v", _p)]
 
 
 _lib = None
@@ -135,6 +158,25 @@ def lib() -> ctypes.CDLL:
             L.brisk_corrector_prepare.restype = ctypes.c_int
             L.brisk_corrector_prepare.argtypes = [ctypes.POINTER(_CorrectorC), _p, _p, _i32, _i32, _p, _sz, _p,
                                                   _sz, _p]
+            _i64, _f32, _szp = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(_sz)
+            _cache = ctypes.POINTER(_KVCacheC)
+            L.brisk_block_attention_workspace_size.restype = ctypes.c_int
+            L.brisk_block_attention_workspace_size.argtypes = [_i32] * 7 + [_szp]
+            L.brisk_block_attention.restype = ctypes.c_int
+            L.brisk_block_attention.argtypes = [_cache, ctypes.POINTER(_KVPrefixC), _p, _i64, _i64, _p, _i32, _i32,
+                                                _i32, _i32, _f32, _p, _p, _p, _sz, _p]
+            L.brisk_cache_score.restype = ctypes.c_int
+            L.brisk_cache_score.argtypes = [_cache, _p, _i64, _i64, _p, _p, _i32, _i32, _i32, _f32, _f32, _p, _p,
+                                            _i32, _p]
+            L.brisk_cache_evict_workspace_size.restype = ctypes.c_int
+            L.brisk_cache_evict_workspace_size.argtypes = [_i32] * 4 + [_szp]
+            L.brisk_cache_evict.restype = ctypes.c_int
+            L.brisk_cache_evict.argtypes = [_cache, _i32, _p, _p, _i32, _p, _i32, _i32, _p, _p, _p, _p, _sz, _p]
+            L.brisk_draft_verify_workspace_size.restype = ctypes.c_int
+            L.brisk_draft_verify_workspace_size.argtypes = [_i32, _i32, _szp]
+            L.brisk_draft_verify.restype = ctypes.c_int
+            L.brisk_draft_verify.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p,
+                                             _sz, _p]
             _lib = L
         return _lib
 
@@ -679,3 +721,258 @@ def spec_verify(ver_hidden: torch.Tensor, lm_head: torch.Tensor, proposal: torch
                                  _ptr(out["row_resample"]), _ptr(ws), ws_n, _stream_ptr(dev, stream))
     _check(st, "brisk_spec_verify")
     return out
+
+
+# ------------------------------------------------- attention, cache and drafts
+_HALF = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class KVCache:
+    """Paged keys and values of a batch of sequences.
+
+    ``k_pages`` and ``v_pages`` are [n_pages, page_size, n_kv_heads, d_head] in
+    bfloat16 or float16 with the same strides; any strides with contiguous
+    heads will do, so head-major pages are passed as a transposed view.
+    ``block_table`` [B, max_pages] int32 lists each sequence's pages and
+    ``seq_len`` [B] int32 the slots it holds, the block in flight included.
+    The tensors stay the caller's: lengths and pages may be written between
+    calls."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor):
+        for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            _half_tensor(t, n, 4)
+        if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype:
+            raise ValueError("k_pages and v_pages must agree in shape, strides and dtype")
+        dev = k_pages.device
+        if v_pages.device != dev:
+            raise ValueError(f"v_pages is on {v_pages.device}, k_pages on {dev}")
+        _dev_tensor(block_table, "block_table", torch.int32, 2, device=dev)
+        _dev_tensor(seq_len, "seq_len", torch.int32, shape=(block_table.shape[0],), device=dev)
+        self.k_pages, self.v_pages, self.block_table, self.seq_len = k_pages, v_pages, block_table, seq_len
+        self.device, self.dtype = dev, k_pages.dtype
+        n_pages, self.page_size, self.n_kv_heads, self.d_head = k_pages.shape
+        self.B, max_pages = block_table.shape
+        self.max_seq_len = max_pages * self.page_size
+        page, slot, head, _ = k_pages.stride()
+        self._c = _KVCacheC(_HALF[self.dtype], self.n_kv_heads, self.d_head, self.page_size, n_pages, max_pages, page,
+                            slot, head, _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(seq_len))
+
+    @property
+    def c_struct(self) -> _KVCacheC:
+        return self._c
+
+
+def _half_tensor(t: torch.Tensor, name: str, ndim: int, like: Optional[KVCache] = None) -> None:
+    """A 2-byte tensor on a HIP device whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _HALF if like is None else t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {'bfloat16 or float16' if like is None else like.dtype}, got {t.dtype}")
+    if t.dim() != ndim:
+        raise ValueError(f"{name} must have {ndim} dims, got shape {tuple(t.shape)}")
+    if t.numel() and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on a HIP device, got {t.device}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {like.device}")
+
+
+def _block_queries(q: torch.Tensor, cache: KVCache, block_mask: Optional[torch.Tensor]):
+    """(B, L, H, row stride, head stride) of a block's queries, checked against the cache."""
+    _half_tensor(q, "q", 4, cache)
+    B, L, H, D = q.shape
+    if B != cache.B or D != cache.d_head:
+        raise ValueError(f"q is {tuple(q.shape)}, the cache holds {cache.B} sequences of {cache.d_head}-wide heads")
+    sb, sl, sh, _ = q.stride()
+    if B > 1 and L > 1 and sb != L * sl:
+        raise ValueError("the rows of q must be evenly spaced: stride(0) == L * stride(1)")
+    if block_mask is not None:
+        _dev_tensor(block_mask, "block_mask", torch.int64, shape=(B, L), device=cache.device)
+    return B, L, H, (sl if L > 1 else sb if B > 1 else H * sh), (sh if H > 1 else D)
+
+
+def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                    block_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                    max_seq_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of every sequence's block over the shared prefix and its own cache.
+
+    ``q`` [B, L, H, D] (L = 1: single tokens; rows and heads may be strided, as
+    in a fused projection's output), ``prefix`` = (k, v) [P, n_kv_heads, D]
+    held once for the whole batch, ``block_mask`` [B, L] int64 whose bit t lets
+    position i see the block's position t, ``scale`` 1/sqrt(D) by default,
+    ``max_seq_len`` a host bound of the lengths.  Returns (out [B, L, H, D],
+    lse [B, L, H] fp32); a row that sees no key gets zeros and -inf."""
+    B, L, H, row, head = _block_queries(q, cache, block_mask)
+    dev, D = cache.device, cache.d_head
+    pre, P = None, 0
+    if prefix is not None:
+        k, v = prefix
+        for t, n in ((k, "prefix keys"), (v, "prefix values")):
+            _half_tensor(t, n, 3, cache)
+        P = k.shape[0]
+        if k.shape[1:] != (cache.n_kv_heads, D) or v.shape != k.shape or (P and v.stride() != k.stride()):
+            raise ValueError(f"prefix must be two tensors [P, {cache.n_kv_heads}, {D}] of the same strides")
+        if P:
+            pre = _KVPrefixC(P, k.stride(0), k.stride(1), _ptr(k), _ptr(v))
+    if out is None:
+        out = torch.empty(B, L, H, D, dtype=cache.dtype, device=dev)
+    else:
+        _dev_tensor(out, "out", cache.dtype, shape=(B, L, H, D), device=dev)
+    if lse is None:
+        lse = torch.empty(B, L, H, dtype=torch.float32, device=dev)
+    else:
+        _dev_tensor(lse, "lse", torch.float32, shape=(B, L, H), device=dev)
+    most = cache.max_seq_len if max_seq_len is None else max_seq_len
+    need = block_attention_workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
+    if workspace is None:
+        workspace = _workspace(dev, need, "attention")
+    st = lib().brisk_block_attention(ctypes.byref(cache.c_struct), None if pre is None else ctypes.byref(pre), _ptr(q),
+                                     row, head, _ptr(block_mask), B, L, H, most, D ** -0.5 if scale is None else scale,
+                                     _ptr(out), _ptr(lse), _ptr(workspace), _ws_bytes(workspace, dev, need),
+                                     _stream_ptr(dev, stream))
+    _check(st, "brisk_block_attention")
+    return out, lse
+
+
+def block_attention_workspace_size(B: int, L: int, n_heads: int, n_kv_heads: int, d_head: int, prefix_len: int,
+                                   max_seq_len: int) -> int:
+    out = _sz()
+    _check(lib().brisk_block_attention_workspace_size(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len,
+                                                      ctypes.byref(out)), "brisk_block_attention_workspace_size")
+    return out.value
+
+
+def cache_score(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, score: torch.Tensor, *,
+                block_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None, decay: float = 1.0,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``decay * score`` plus the attention weight every cached key received from
+    the block's rows: [B, n_kv_heads, cap] fp32, zero past a sequence's length.
+    ``q``, ``block_mask`` and ``scale`` as in :func:`block_attention`, ``lse``
+    as it returned it.  ``out`` may be ``score`` itself."""
+    B, L, H, row, head = _block_queries(q, cache, block_mask)
+    dev = cache.device
+    _dev_tensor(lse, "lse", torch.float32, shape=(B, L, H), device=dev)
+    _dev_tensor(score, "score", torch.float32, 3, device=dev)
+    cap = score.shape[2]
+    shape = (B, cache.n_kv_heads, cap)
+    _dev_tensor(score, "score", torch.float32, shape=shape, device=dev)
+    if out is None:
+        out = torch.empty_like(score)
+    else:
+        _dev_tensor(out, "out", torch.float32, shape=shape, device=dev)
+    st = lib().brisk_cache_score(ctypes.byref(cache.c_struct), _ptr(q), row, head, _ptr(block_mask), _ptr(lse), B, L, H,
+                                 cache.d_head ** -0.5 if scale is None else scale, decay, _ptr(score), _ptr(out), cap,
+                                 _stream_ptr(dev, stream))
+    _check(st, "brisk_cache_score")
+    return out
+
+
+def cache_evict(cache: KVCache, score: torch.Tensor, pos: torch.Tensor, next_pos: torch.Tensor, budget: int,
+                recent: int, *, score_out: Optional[torch.Tensor] = None, pos_out: Optional[torch.Tensor] = None,
+                new_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Cuts every sequence's cache to ``budget`` slots, in place: each head keeps
+    the slots whose ``pos`` is among the ``recent`` latest before ``next_pos``
+    [B], then those of the largest ``score``.  ``score`` fp32 and ``pos`` int32
+    are [B, n_kv_heads, cap]; returns (score, pos, new_len [B]) of the slots as
+    they lie afterwards.  The cache's ``seq_len`` is left to the caller."""
+    dev = cache.device
+    _dev_tensor(score, "score", torch.float32, 3, device=dev)
+    cap = score.shape[2]
+    shape = (cache.B, cache.n_kv_heads, cap)
+    _dev_tensor(score, "score", torch.float32, shape=shape, device=dev)
+    _dev_tensor(pos, "pos", torch.int32, shape=shape, device=dev)
+    _dev_tensor(next_pos, "next_pos", torch.int32, shape=(cache.B,), device=dev)
+    if score_out is None:
+        score_out = torch.empty_like(score)
+    if pos_out is None:
+        pos_out = torch.empty_like(pos)
+    if new_len is None:
+        new_len = torch.empty(cache.B, dtype=torch.int32, device=dev)
+    _dev_tensor(score_out, "score_out", torch.float32, shape=shape, device=dev)
+    _dev_tensor(pos_out, "pos_out", torch.int32, shape=shape, device=dev)
+    _dev_tensor(new_len, "new_len", torch.int32, shape=(cache.B,), device=dev)
+    if _overlap(score, score_out) or _overlap(pos, pos_out):
+        raise ValueError("score_out and pos_out must not overlap score and pos")
+    nbytes = _sz()
+    _check(lib().brisk_cache_evict_workspace_size(cache.B, cache.n_kv_heads, cap, budget, ctypes.byref(nbytes)),
+           "brisk_cache_evict_workspace_size")
+    if workspace is None:
+        workspace = _workspace(dev, nbytes.value, "evict")
+    st = lib().brisk_cache_evict(ctypes.byref(cache.c_struct), cache.B, _ptr(score), _ptr(pos), cap, _ptr(next_pos),
+                                 budget, recent, _ptr(score_out), _ptr(pos_out), _ptr(new_len), _ptr(workspace),
+                                 _ws_bytes(workspace, dev, nbytes.value), _stream_ptr(dev, stream))
+    _check(st, "brisk_cache_evict")
+    return score_out, pos_out, new_len
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two contiguous tensors share memory."""
+    pa, pb = a.data_ptr(), b.data_ptr()
+    return pa < pb + b.numel() * b.element_size() and pb < pa + a.numel() * a.element_size()
+
+
+def _prob_rows(t: torch.Tensor, name: str, shape: Tuple[int, ...], device: torch.device) -> int:
+    """Row stride of fp32 rows [..., V] that may be spaced wider than V."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    if len(shape) == 2:
+        return t.stride(0) if shape[0] > 1 else shape[1]
+    if shape[0] > 1 and shape[1] > 1 and t.stride(0) != shape[1] * t.stride(1):
+        raise ValueError(f"the rows of {name} must be evenly spaced: stride(0) == {shape[1]} * stride(1)")
+    return t.stride(1) if shape[1] > 1 else t.stride(0) if shape[0] > 1 else shape[2]
+
+
+def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok: torch.Tensor, u_accept: torch.Tensor,
+                 noise: torch.Tensor, *, draft_len: Optional[torch.Tensor] = None,
+                 accept_len: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Verifies drafted tokens against given probabilities with given random numbers.
+
+    ``target_prob`` [B, L + 1, V] and ``draft_prob`` [B, L, V] fp32 (rows may be
+    padded), ``draft_tok`` [B, L] int32, ``u_accept`` [B, L] uniforms, ``noise``
+    [B, V] Exp(1) variates, ``draft_len`` [B] for drafts of different lengths.
+    Returns (accept_len [B], token [B]) int32: the accepted prefix of each draft
+    and the token after it, drawn from [p - q]_+ after a rejection and from the
+    target's next row after a full acceptance (-1 if no weight is positive)."""
+    _dev_tensor(draft_tok, "draft_tok", torch.int32, 2)
+    B, L = draft_tok.shape
+    dev = draft_tok.device
+    if not isinstance(target_prob, torch.Tensor) or target_prob.dim() != 3:
+        raise ValueError("target_prob must be a [B, L + 1, V] tensor")
+    V = target_prob.shape[2]
+    t_stride = _prob_rows(target_prob, "target_prob", (B, L + 1, V), dev)
+    d_stride = _prob_rows(draft_prob, "draft_prob", (B, L, V), dev) if L else V
+    n_stride = _prob_rows(noise, "noise", (B, V), dev)
+    _dev_tensor(u_accept, "u_accept", torch.float32, shape=(B, L), device=dev)
+    if draft_len is not None:
+        _dev_tensor(draft_len, "draft_len", torch.int32, shape=(B,), device=dev)
+    if accept_len is None:
+        accept_len = torch.empty(B, dtype=torch.int32, device=dev)
+    else:
+        _dev_tensor(accept_len, "accept_len", torch.int32, shape=(B,), device=dev)
+    if token is None:
+        token = torch.empty(B, dtype=torch.int32, device=dev)
+    else:
+        _dev_tensor(token, "token", torch.int32, shape=(B,), device=dev)
+    nbytes = _sz()
+    _check(lib().brisk_draft_verify_workspace_size(B, V, ctypes.byref(nbytes)), "brisk_draft_verify_workspace_size")
+    if workspace is None:
+        workspace = _workspace(dev, nbytes.value, "draft")
+    st = lib().brisk_draft_verify(_ptr(target_prob), t_stride, _ptr(draft_prob) if L else None, d_stride,
+                                  _ptr(draft_tok) if L else None, _ptr(draft_len), _ptr(u_accept) if L else None,
+                                  _ptr(noise), n_stride, B, L, V, _ptr(accept_len), _ptr(token), _ptr(workspace),
+                                  _ws_bytes(workspace, dev, nbytes.value), _stream_ptr(dev, stream))
+    _check(st, "brisk_draft_verify")
+    return accept_len, token

@@ -23,6 +23,53 @@ bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0
 constexpr int32_t kMaxProfileM = 1024;
 constexpr int32_t kMaxProfileBlocks = 1 << 30;
 
+constexpr int32_t kMaxAttnRows = 1 << 24;
+constexpr int32_t kMaxSlots = 1 << 30;
+constexpr int32_t kMaxEvictCap = 1 << 24;
+// The paged cache: sizes, strides and alignment.  `view` is filled on success.
+int cache_check(const brisk_kv_cache* c, brisk::KvView* view) {
+  if (!c || !c->k_pages || !c->v_pages || !c->block_table || !c->seq_len) return BRISK_ERR_NULL;
+  if ((c->dtype != BRISK_BF16 && c->dtype != BRISK_F16) || c->n_kv_heads < 1 || c->n_kv_heads > 1024 ||
+      c->d_head < 8 || c->d_head > 128 || c->page_size < 1 || c->page_size > 65536 || c->n_pages < 1 ||
+      c->max_pages < 1 || static_cast<int64_t>(c->max_pages) * c->page_size > (int64_t{1} << 30) ||
+      c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0)
+    return BRISK_ERR_SHAPE;
+  if (c->d_head % 8 != 0 || (c->page_size & (c->page_size - 1)) != 0 || c->page_stride % 8 != 0 ||
+      c->slot_stride % 8 != 0 || c->head_stride % 8 != 0 || !aligned16(c->k_pages) ||
+      !aligned16(c->v_pages) || !aligned4(c->block_table) || !aligned4(c->seq_len))
+    return BRISK_ERR_UNSUPPORTED;
+  int shift = 0;
+  while ((1 << shift) < c->page_size) ++shift;
+  *view = {c->k_pages, c->v_pages, c->block_table, c->seq_len, c->page_stride, c->slot_stride,
+           c->head_stride, shift, c->n_pages, c->max_pages};
+  return BRISK_OK;
+}
+
+// Rows of a block's queries: [B * L, n_heads] with head groups of the cache.
+int block_rows_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads) {
+  if (B < 1 || L < 1 || L > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 ||
+      B > kMaxAttnRows / L || static_cast<int64_t>(B) * L * n_heads > kMaxAttnRows)
+    return BRISK_ERR_SHAPE;
+  return BRISK_OK;
+}
+
+int attention_shape_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                          int32_t prefix_len, int32_t max_seq_len) {
+  if (n_kv_heads > 1024 || d_head < 8 || d_head > 128 || prefix_len < 0 || prefix_len > kMaxSlots ||
+      max_seq_len < 0 || max_seq_len > kMaxSlots)
+    return BRISK_ERR_SHAPE;
+  const int st = block_rows_check(B, L, n_heads, n_kv_heads);
+  if (st != BRISK_OK) return st;
+  return d_head % 8 != 0 ? BRISK_ERR_UNSUPPORTED : BRISK_OK;
+}
+
+int evict_shape_check(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget) {
+  if (B < 1 || n_kv_heads < 1 || n_kv_heads > 1024 || static_cast<int64_t>(B) * n_kv_heads > kMaxRows ||
+      cap < 1 || cap > kMaxEvictCap || budget < 1)
+    return BRISK_ERR_SHAPE;
+  return BRISK_OK;
+}
+
 // hidden [rows, d] x lm_head [V, d]: shapes, alignment and the 32-bit byte
 // offsets the LM-head kernel addresses both matrices with
 int lmhead_check(const uint16_t* hidden, const uint16_t* lm_head, int32_t rows, int32_t d, int32_t V,
@@ -394,6 +441,174 @@ int brisk_accept_profile(const int32_t* accept_len, int32_t n_blocks, int32_t M,
   if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
   brisk::launch_accept_profile(accept_len, n_blocks, M, eps, a, w_raw, w, tpf_fpt, ws,
                                static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_block_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads,
+                                         int32_t d_head, int32_t prefix_len, int32_t max_seq_len,
+                                         size_t* bytes) {
+  if (!bytes) return BRISK_ERR_NULL;
+  const int st = attention_shape_check(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len);
+  if (st != BRISK_OK) return st;
+  *bytes = brisk::attention_workspace_bytes(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len);
+  return BRISK_OK;
+}
+
+int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* prefix, const uint16_t* q,
+                          int64_t q_row_stride, int64_t q_head_stride, const uint64_t* block_mask,
+                          int32_t B, int32_t L, int32_t n_heads, int32_t max_seq_len, float scale,
+                          uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  brisk::AttentionArgs a{};
+  int st = cache_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  const int32_t prefix_len = prefix ? prefix->len : 0;
+  if (!q || !out || (prefix_len > 0 && (!prefix->k || !prefix->v))) return BRISK_ERR_NULL;
+  st = attention_shape_check(B, L, n_heads, cache->n_kv_heads, cache->d_head, prefix_len, max_seq_len);
+  if (st != BRISK_OK) return st;
+  if (max_seq_len > static_cast<int64_t>(cache->max_pages) * cache->page_size || q_row_stride < 0 ||
+      q_head_stride < 0 || !(scale > 0.f) || scale > 3.0e38f ||
+      (prefix && (prefix->slot_stride < 0 || prefix->head_stride < 0)))
+    return BRISK_ERR_SHAPE;
+  if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned16(out) ||
+      !aligned4(lse) || !aligned8(block_mask))
+    return BRISK_ERR_UNSUPPORTED;
+  if (prefix_len > 0) {
+    if (!aligned16(prefix->k) || !aligned16(prefix->v) || prefix->slot_stride % 8 != 0 ||
+        prefix->head_stride % 8 != 0)
+      return BRISK_ERR_UNSUPPORTED;
+    a.pre_k = prefix->k;
+    a.pre_v = prefix->v;
+    a.pre_slot_stride = prefix->slot_stride;
+    a.pre_head_stride = prefix->head_stride;
+  }
+  const size_t need = brisk::attention_workspace_bytes(B, L, n_heads, cache->n_kv_heads, cache->d_head,
+                                                       prefix_len, max_seq_len);
+  if (ws_bytes < need || (need > 0 && !ws)) return BRISK_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
+  a.q = q;
+  a.q_row_stride = q_row_stride;
+  a.q_head_stride = q_head_stride;
+  a.mask = block_mask;
+  a.out = out;
+  a.lse = lse;
+  a.B = B;
+  a.L = L;
+  a.H = n_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->d_head;
+  a.prefix_len = prefix_len;
+  a.max_seq_len = max_seq_len;
+  a.scale = scale;
+  brisk::launch_attention(a, cache->dtype == BRISK_F16, ws, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_row_stride,
+                      int64_t q_head_stride, const uint64_t* block_mask, const float* lse, int32_t B,
+                      int32_t L, int32_t n_heads, float scale, float decay, const float* score_in,
+                      float* score_out, int32_t cap, void* stream) {
+  brisk::ScoreArgs a{};
+  int st = cache_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  if (!q || !lse || !score_in || !score_out) return BRISK_ERR_NULL;
+  st = block_rows_check(B, L, n_heads, cache->n_kv_heads);
+  if (st != BRISK_OK) return st;
+  if (cap < 1 || cap > kMaxSlots || q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) ||
+      scale > 3.0e38f)
+    return BRISK_ERR_SHAPE;
+  if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned8(block_mask) ||
+      !aligned4(lse) || !aligned4(score_in) || !aligned4(score_out))
+    return BRISK_ERR_UNSUPPORTED;
+  a.q = q;
+  a.q_row_stride = q_row_stride;
+  a.q_head_stride = q_head_stride;
+  a.mask = block_mask;
+  a.lse = lse;
+  a.score_in = score_in;
+  a.score_out = score_out;
+  a.B = B;
+  a.L = L;
+  a.H = n_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->d_head;
+  a.cap = cap;
+  a.scale = scale;
+  a.decay = decay;
+  brisk::launch_cache_score(a, cache->dtype == BRISK_F16, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget,
+                                     size_t* bytes) {
+  if (!bytes) return BRISK_ERR_NULL;
+  const int st = evict_shape_check(B, n_kv_heads, cap, budget);
+  if (st != BRISK_OK) return st;
+  *bytes = brisk::evict_workspace_bytes(B, n_kv_heads, cap, budget);
+  return BRISK_OK;
+}
+
+int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score_in,
+                      const int32_t* pos_in, int32_t cap, const int32_t* next_pos, int32_t budget,
+                      int32_t recent, float* score_out, int32_t* pos_out, int32_t* new_len, void* ws,
+                      size_t ws_bytes, void* stream) {
+  brisk::EvictArgs a{};
+  int st = cache_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  if (!score_in || !pos_in || !next_pos || !score_out || !pos_out || !new_len) return BRISK_ERR_NULL;
+  st = evict_shape_check(B, cache->n_kv_heads, cap, budget);
+  if (st != BRISK_OK) return st;
+  if (recent < 0 || recent > budget) return BRISK_ERR_SHAPE;
+  if (!aligned4(score_in) || !aligned4(pos_in) || !aligned4(next_pos) || !aligned4(score_out) ||
+      !aligned4(pos_out) || !aligned4(new_len))
+    return BRISK_ERR_UNSUPPORTED;
+  const size_t need = brisk::evict_workspace_bytes(B, cache->n_kv_heads, cap, budget);
+  if (ws_bytes < need || !ws) return BRISK_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
+  a.k = cache->k_pages;
+  a.v = cache->v_pages;
+  a.score_in = score_in;
+  a.pos_in = pos_in;
+  a.next_pos = next_pos;
+  a.score_out = score_out;
+  a.pos_out = pos_out;
+  a.new_len = new_len;
+  a.B = B;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->d_head;
+  a.cap = cap;
+  a.budget = budget;
+  a.recent = recent;
+  brisk::launch_cache_evict(a, ws, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_draft_verify_workspace_size(int32_t B, int32_t V, size_t* bytes) {
+  if (!bytes) return BRISK_ERR_NULL;
+  if (B < 1 || B > kMaxRows || V < 1 || V > kMaxTableV) return BRISK_ERR_SHAPE;
+  *bytes = brisk::draft_verify_workspace_bytes(B, V);
+  return BRISK_OK;
+}
+
+int brisk_draft_verify(const float* target_prob, int64_t target_stride, const float* draft_prob,
+                       int64_t draft_stride, const int32_t* draft_tok, const int32_t* draft_len,
+                       const float* u_accept, const float* noise, int64_t noise_stride, int32_t B,
+                       int32_t L, int32_t V, int32_t* accept_len, int32_t* token, void* ws,
+                       size_t ws_bytes, void* stream) {
+  if (!target_prob || !noise || !accept_len || !token ||
+      (L > 0 && (!draft_prob || !draft_tok || !u_accept)))
+    return BRISK_ERR_NULL;
+  if (B < 1 || L < 0 || L > 1024 || static_cast<int64_t>(B) * (L + 1) > kMaxRows || V < 1 ||
+      V > kMaxTableV || target_stride < V || noise_stride < V || (L > 0 && draft_stride < V))
+    return BRISK_ERR_SHAPE;
+  if (!aligned4(target_prob) || !aligned4(draft_prob) || !aligned4(draft_tok) || !aligned4(draft_len) ||
+      !aligned4(u_accept) || !aligned4(noise) || !aligned4(accept_len) || !aligned4(token))
+    return BRISK_ERR_UNSUPPORTED;
+  const size_t need = brisk::draft_verify_workspace_bytes(B, V);
+  if (ws_bytes < need || (need > 0 && !ws)) return BRISK_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
+  const brisk::DraftArgs a{target_prob, draft_prob, target_stride, draft_stride, draft_tok, draft_len,
+                           u_accept, noise, noise_stride, B, L, V, accept_len, token};
+  brisk::launch_draft_verify(a, ws, static_cast<hipStream_t>(stream));
   return launch_status();
 }
 

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "brisk.h"
+#include "kv_view.h"
 
 namespace brisk {
 
@@ -83,5 +84,64 @@ void launch_corrector_loss(const uint16_t* ver_hidden, const uint16_t* lm_head, 
 size_t accept_profile_workspace_bytes(int n_blocks, int M);
 void launch_accept_profile(const int32_t* accept_len, int n_blocks, int M, double eps, double* a,
                            double* w_raw, double* w, double* tpf_fpt, void* ws, hipStream_t s);
+
+// ---- block attention over a shared prefix and a paged cache -------------------
+struct AttentionArgs {
+  KvView kv;
+  const uint16_t *pre_k, *pre_v;                   // may be null when prefix_len == 0
+  int64_t pre_slot_stride, pre_head_stride;        // elements
+  const uint16_t* q;
+  int64_t q_row_stride, q_head_stride;             // elements
+  const uint64_t* mask;                            // [B, L], nullable
+  uint16_t* out;
+  float* lse;                                      // nullable
+  int B, L, H, Hkv, D, prefix_len, max_seq_len;
+  float scale;
+};
+size_t attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len);
+void launch_attention(const AttentionArgs& a, bool f16, void* ws, hipStream_t s);
+
+// ---- received attention weight, eviction ---------------------------------------
+struct ScoreArgs {
+  KvView kv;
+  const uint16_t* q;
+  int64_t q_row_stride, q_head_stride;
+  const uint64_t* mask;
+  const float* lse;
+  const float* score_in;
+  float* score_out;
+  int B, L, H, Hkv, D, cap;
+  float scale, decay;
+};
+void launch_cache_score(const ScoreArgs& a, bool f16, hipStream_t s);
+
+struct EvictArgs {
+  KvView kv;
+  uint16_t *k, *v;                                 // kv's pages, to be written
+  const float* score_in;
+  const int32_t* pos_in;
+  const int32_t* next_pos;
+  float* score_out;
+  int32_t* pos_out;
+  int32_t* new_len;
+  int32_t *count, *src, *dst;                      // in the workspace, set by the launcher
+  int B, Hkv, D, cap, budget, recent, list_len;
+};
+int evict_list_len(int cap, int budget);
+size_t evict_workspace_bytes(int B, int Hkv, int cap, int budget);
+void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s);
+
+// ---- verification of drafts from given probabilities ---------------------------
+struct DraftArgs {
+  const float *target, *draft;
+  int64_t target_stride, draft_stride;
+  const int32_t *tok, *draft_len;                  // draft_len nullable
+  const float *u, *noise;
+  int64_t noise_stride;
+  int B, L, V;
+  int32_t *accept_len, *token;
+};
+size_t draft_verify_workspace_bytes(int B, int V);
+void launch_draft_verify(const DraftArgs& a, void* ws, hipStream_t s);
 
 }  // namespace brisk
