@@ -3,6 +3,19 @@
 //
 //   s_j = scale <q, k_j>,  m = max_j s_j,  l = sum_j exp(s_j - m)
 //   out = sum_j exp(s_j - m) v_j / l,  lse = m + log l
+//
+// All rows that read the same keys share one pass over them: the prefix is
+// read by tiles of rows of the whole batch (rows of every sequence and of
+// every query head of a group), a sequence's own cache by the rows of its
+// block.  A workgroup takes a tile of rows and a run of keys; runs of the same
+// rows are joined afterwards from their normalised sums and log-sum-exps:
+//   out = sum_r exp(lse_r - lse) out_r,  lse = log sum_r exp(lse_r)
+//
+// Inside a wavefront the logits are computed transposed, S^T = K Q^T, so that
+// a lane holds one row's logits: the softmax statistics need one exchange
+// between the wavefront's halves, and the probabilities are already the
+// operand of out^T = V^T P^T, with the keys in an order that the transposed
+// LDS reads of V follow.
 #include "kernels.h"
 #include "kv_common.h"
 
@@ -10,77 +23,558 @@ namespace brisk {
 
 namespace {
 
-// One workgroup a row: each wavefront takes every fourth key, a lane two
-// elements of it, and the four running maxima and sums are joined at the end.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
+
+constexpr int kCUs = 256;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+
+// Source of LDS rows and chunks that hold nothing.
+__device__ const uint4 g_zeros[1] = {};
+
+// What one launch works on: prefix items, then own items.
+struct AttnPlan {
+  float* part;           // [rows][splits][D] normalised sums, null when every row has one run
+  float* part_lse;       // [rows][splits]
+  int pre_groups, pre_tiles, pre_splits, pre_run;  // (head, split) pairs, row tiles, runs of pre_run keys
+  int own_groups, own_tiles, own_splits, own_run;  // (sequence, head, split) triples, ...
+  int splits;            // pre_splits + own_splits of all launches of the call
+  int own_first;         // index of the first own split
+};
+
 template <bool F16>
-__global__ __launch_bounds__(256) void attention_kernel(AttentionArgs a) {
-  __shared__ float s_m[4], s_l[4], s_o[4][128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = blockIdx.x;
-  const int h = static_cast<int>(row % a.H), bi = static_cast<int>(row / a.H), b = bi / a.L;
-  const int hk = h / (a.H / a.Hkv), n = kv_len(a.kv, b, a.max_seq_len), base = n - a.L;
-  const uint64_t mask = a.mask ? a.mask[bi] : ~0ull;
-  const uint16_t* q = a.q + bi * a.q_row_stride + h * a.q_head_stride;
-  const int e0 = lane * 2;
-  const bool on = e0 < a.D;
-  const float q0 = on ? half_to_f32<F16>(q[e0]) : 0.f, q1 = on ? half_to_f32<F16>(q[e0 + 1]) : 0.f;
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int64_t j = wave; j < static_cast<int64_t>(a.prefix_len) + n; j += 4) {
-    const uint16_t *k, *v;
-    if (j < a.prefix_len) {
-      const int64_t at = j * a.pre_slot_stride + hk * a.pre_head_stride;
-      k = a.pre_k + at;
-      v = a.pre_v + at;
-    } else {
-      const int s = static_cast<int>(j - a.prefix_len);
-      if (s >= base && !block_sees(mask, s - base)) continue;
-      const int64_t at = kv_slot(a.kv, b, s) + hk * a.kv.head_stride;
-      k = a.kv.k + at;
-      v = a.kv.v + at;
+__device__ __forceinline__ floatx16 mfma32(uint4 a, uint4 b, floatx16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (F16) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, h2{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, b2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
+  }
+}
+
+// Which of 32 keys a row sees: bit x is set when x < left and the key's place
+// in the block, at + x, is negative (before the block) or set in `word`.
+__device__ __forceinline__ uint32_t seen32(uint64_t word, int at, int left) {
+  uint64_t bits = at >= 64 ? 0 : at >= 0 ? word >> at : at > -32 ? (word << -at) | ((1ull << -at) - 1) : ~0ull;
+  bits = left >= 32 ? bits : left <= 0 ? 0 : bits & ((1ull << left) - 1);
+  return static_cast<uint32_t>(bits);
+}
+
+__device__ __forceinline__ float swap32_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Rows of keys in LDS: RB bytes each, their 16-byte chunks permuted by the
+// key so that neither the b128 reads of K (one chunk of 16 keys) nor the
+// transposed b64 reads of V (four chunks of 4 keys) meet in a bank.
+template <int RB>
+__device__ __forceinline__ int k_swizzle(int key) { return RB == 256 ? key & 15 : (key >> 1) & 7; }
+template <int RB>
+__device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; }
+
+// ND: 32-wide slices of the head; QT: 32-row tiles a wavefront; RW wavefronts
+// of different rows share each tile of 32 * NT keys, KW groups of them take
+// alternate tiles.
+template <bool F16, int ND, int QT, int RW, int KW, int NT>
+__global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, AttnPlan p) {
+  constexpr int RB = ND > 2 ? 256 : 128, T = 32 * NT, NC = 2 * ND;
+  constexpr int RPI = 1024 / RB;                 // rows of a wavefront's copy
+  constexpr int NI = T / RPI / RW;               // copies of K (and of V) a wavefront
+  constexpr int kTile = T * RB;                  // bytes of K (or V) of a tile
+  constexpr int kStage = 2 * kTile, kStages = 2;
+  constexpr int kRows = RW * QT * 32;
+  constexpr int kOutRow = ND * 32 + 4;           // floats of a row of the join
+  constexpr int kJoin = KW > 1 ? KW * kRows * (kOutRow + 2) * 4 : 0;
+  constexpr int kLds = kStages * kStage * KW > kJoin ? kStages * kStage * KW : kJoin;
+  static_assert(T % (RPI * RW) == 0 && kLds <= 163840);
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
+  const int half = lane >> 5, col = lane & 31;
+  const int G = a.H / a.Hkv;
+
+  // ---- which rows and keys: the row tiles of a group follow each other on one XCD
+  int bid = blockIdx.x;
+  const int pre_grid = (p.pre_groups + 7) / 8 * 8 * p.pre_tiles;
+  const bool own = bid >= pre_grid;
+  if (own) bid -= pre_grid;
+  const int tiles = own ? p.own_tiles : p.pre_tiles;
+  const int group = bid / 8 / tiles * 8 + bid % 8, tile = bid / 8 % tiles;
+  if (group >= (own ? p.own_groups : p.pre_groups)) return;
+  int b = 0, hk, split, key0, key1, row0, rows;
+  if (own) {
+    split = group % p.own_splits;
+    hk = group / p.own_splits % a.Hkv;
+    b = group / p.own_splits / a.Hkv;
+    const int n = kv_len(a.kv, b, a.max_seq_len);
+    key0 = split * p.own_run;
+    key1 = min(n, key0 + p.own_run);
+    if (key0 >= n && split > 0) return;          // nobody reads this run
+    row0 = b * a.L * G;
+    rows = a.L * G;
+    split += p.own_first;
+  } else {
+    split = group % p.pre_splits;
+    hk = group / p.pre_splits;
+    key0 = split * p.pre_run;
+    key1 = min(a.prefix_len, key0 + p.pre_run);
+    row0 = 0;
+    rows = a.B * a.L * G;
+  }
+  row0 += tile * kRows;
+  rows = min(kRows, rows - tile * kRows);
+  const int base = own ? kv_len(a.kv, b, a.max_seq_len) - a.L : 0;  // first slot of the block itself
+  const bool masked = own && a.mask;
+  const float c = a.scale * kLog2e;
+
+  // ---- this wavefront's queries, as the second operand of K Q^T
+  uint4 q[QT][NC];
+  uint64_t words[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = (rw * QT + t) * 32 + col;
+    const int row = row0 + min(r, rows - 1), bi = row / G;
+    const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
+    words[t] = masked ? a.mask[bi] : ~0ull;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int e = 16 * i + 8 * half;
+      q[t][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
     }
-    const float s = a.scale * wave_sum(on ? q0 * half_to_f32<F16>(k[e0]) + q1 * half_to_f32<F16>(k[e0 + 1]) : 0.f);
-    const float M = fmaxf(m, s);
-    if (M == -INFINITY) continue;
-    const float keep = __expf(m - M), p = __expf(s - M);
-    l = l * keep + p;
-    o0 = o0 * keep + (on ? p * half_to_f32<F16>(v[e0]) : 0.f);
-    o1 = o1 * keep + (on ? p * half_to_f32<F16>(v[e0 + 1]) : 0.f);
-    m = M;
   }
-  if (lane == 0) {
-    s_m[wave] = m;
-    s_l[wave] = l;
+
+  const uint16_t* const k_src = (own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
+  const uint16_t* const v_src = (own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
+  uint8_t* const lds = smem + kw * (kStages * kStage);
+
+  // Page ids of the rows this lane copies of the tile at j0.
+  int page[NI];
+  auto look_up = [&](int j0) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int j = min(j0 + (rw * NI + i) * RPI + lane / (RB / 16), key1 - 1);
+      page[i] = own ? a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (max(j, 0) >> a.kv.page_shift)] : 0;
+    }
+  };
+  // Copies the tile at j0; slots from v_end on get no value (key1, or where the block begins).
+  auto stage = [&](int j0, int buf, int v_end) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int copy = rw * NI + i, key = copy * RPI + lane / (RB / 16), pc = lane % (RB / 16), j = j0 + key;
+      const int64_t at = own ? clamp_id(page[i], a.kv.n_pages) * a.kv.page_stride +
+                                   (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride
+                             : j * a.pre_slot_stride;
+      const int ek = (pc ^ k_swizzle<RB>(key)) * 8, ev = (pc ^ v_swizzle<RB>(key)) * 8;
+      const void* zeros = g_zeros;
+      const void* sk = j < key1 && ek < a.D ? k_src + at + ek : zeros;
+      const void* sv = j < v_end && ev < a.D ? v_src + at + ev : zeros;
+      uint8_t* dst = lds + buf * kStage + copy * 1024;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sk,
+                                       (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sv,
+                                       (__attribute__((address_space(3))) void*)(dst + kTile), 16, 0, 0);
+    }
+  };
+
+  floatx16 o[QT][ND];
+  float m[QT], mc[QT], l[QT];  // m: subtracted logit (unscaled), mc = c * m; l: this lane's part of the sum
+  const int steps = (key1 - key0 + T * KW - 1) / (T * KW);
+
+  // The second time round only where values that some rows must not see are
+  // not finite: the block's own values then join by vector arithmetic, row by row.
+  for (int careful = 0;; ++careful) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      m[t] = -INFINITY;
+      mc[t] = l[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[t][d] = floatx16{};
+    }
+    const int v_end = careful ? min(key1, max(base, 0)) : key1;
+    int j0 = key0 + kw * T;
+    if (steps > 0) {
+      look_up(j0);
+      stage(j0, 0, v_end);
+      look_up(j0 + T * KW);
+    }
+    for (int step = 0; step < steps; ++step, j0 += T * KW) {
+      const int buf = step & 1;
+      __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // vmcnt(0): this wavefront's copies have landed
+      __syncthreads();
+      if (step + 1 < steps) {
+        stage(j0 + T * KW, buf ^ 1, v_end);
+        look_up(j0 + 2 * T * KW);
+      }
+      if (j0 >= key1) continue;  // uniform in the wavefront; its tile is past the run
+      const uint8_t* kt = lds + buf * kStage;
+      const uint8_t* vt = kt + kTile;
+
+      // ---- S^T = K Q^T: register r of a lane is key 8 (r / 4) + 4 half + r % 4 of each 32
+      floatx16 s[QT][NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) s[t][n] = floatx16{};
+        const int key = n * 32 + col;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ k_swizzle<RB>(key)) << 4));
+#pragma unroll
+          for (int t = 0; t < QT; ++t) s[t][n] = mfma32<F16>(kf, q[t][i], s[t][n]);
+        }
+      }
+      if (j0 + T > key1 || (masked && j0 + T > base)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int first = j0 + n * 32 + 4 * half;  // the key of this lane's first register
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const uint32_t seen = seen32(masked ? words[t] : ~0ull, masked ? first - base : 0, key1 - first);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][n][r] = (seen >> (8 * (r / 4) + r % 4)) & 1 ? s[t][n][r] : -INFINITY;
+          }
+        }
+      }
+      // ---- softmax statistics and P^T
+      uint4 pf[QT][2 * NT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float top = s[t][0][0];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][n][r]);
+        top = swap32_max(top);
+        // The subtracted logit follows the maximum only once that is 2^8 times ahead.
+        if (__any(top * c > mc[t] + 8.f || (m[t] == -INFINITY && top > -INFINITY))) {
+          const float up = fmaxf(m[t], top);
+          const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[t] - up) * c);
+          l[t] *= f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[t][d] *= f;
+          m[t] = up;
+          mc[t] = up == -INFINITY ? 0.f : up * c;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          uint32_t w[8];
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][n][r], c, -mc[t]));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][n][r + 1], c, -mc[t]));
+            l[t] += p0 + p1;
+            w[r / 2] = pack2<F16>(p0, p1);
+          }
+          pf[t][2 * n] = make_uint4(w[0], w[1], w[2], w[3]);
+          pf[t][2 * n + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      }
+      // ---- out^T += V^T P^T, 16 keys at a time
+#pragma unroll
+      for (int g = 0; g < 2 * NT; ++g) {
+        const int key = g * 16 + 4 * half + (lane & 15) / 4;  // and 8 further
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, in = (lane & 1) * 8;
+          const uint8_t* v0 = vt + key * RB + ((chunk ^ v_swizzle<RB>(key)) << 4) + in;
+          const uint8_t* v1 = vt + (key + 8) * RB + ((chunk ^ v_swizzle<RB>(key + 8)) << 4) + in;
+          const shortx4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v0));
+          const shortx4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v1));
+          const uint2 y0 = __builtin_bit_cast(uint2, x0), y1 = __builtin_bit_cast(uint2, x1);
+          const uint4 vf = make_uint4(y0.x, y0.y, y1.x, y1.y);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][d] = mfma32<F16>(vf, pf[t][g], o[t][d]);
+        }
+      }
+      if (careful && j0 + T > base) {
+        for (int j = max(j0, base); j < min(j0 + T, key1); ++j) {
+          const int key = j - j0;
+          const uint16_t* v = v_src + kv_slot(a.kv, b, j);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ k_swizzle<RB>(key)) << 4));
+              const uint32_t kw4[4] = {kf.x, kf.y, kf.z, kf.w};
+              uint32_t qw4[4] = {q[t][i].x, q[t][i].y, q[t][i].z, q[t][i].w};
+              // converted here, not ahead of the loop: this path is rare and the registers are not
+              asm volatile("" : "+v"(qw4[0]), "+v"(qw4[1]), "+v"(qw4[2]), "+v"(qw4[3]));
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                dot += half_to_f32<F16>(kw4[w] & 0xFFFF) * half_to_f32<F16>(qw4[w] & 0xFFFF) +
+                       half_to_f32<F16>(kw4[w] >> 16) * half_to_f32<F16>(qw4[w] >> 16);
+            }
+            dot = swap32_sum(dot);
+            if (!block_sees(words[t], j - base)) continue;
+            const float w = __builtin_amdgcn_exp2f(fmaf(dot, c, -mc[t]));
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+#pragma unroll
+              for (int r = 0; r < 16; r += 4) {
+                const int e = 32 * d + 8 * (r / 4) + 4 * half;
+                if (e >= a.D) continue;
+                const uint2 x = *reinterpret_cast<const uint2*>(v + e);
+                o[t][d][r] = fmaf(w, half_to_f32<F16>(x.x & 0xFFFF), o[t][d][r]);
+                o[t][d][r + 1] = fmaf(w, half_to_f32<F16>(x.x >> 16), o[t][d][r + 1]);
+                o[t][d][r + 2] = fmaf(w, half_to_f32<F16>(x.y & 0xFFFF), o[t][d][r + 2]);
+                o[t][d][r + 3] = fmaf(w, half_to_f32<F16>(x.y >> 16), o[t][d][r + 3]);
+              }
+              asm volatile("" ::: "memory");  // a few loads in flight
+            }
+          }
+        }
+      }
+    }
+    if (!masked || careful) break;
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd |= !(fabsf(o[t][d][r]) < INFINITY);
+    if (!__syncthreads_or(odd)) break;
   }
-  s_o[wave][e0] = o0;
-  s_o[wave][e0 + 1] = o1;
-  __syncthreads();
-  if (wave != 0) return;
-  const float M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float L = 0.f, a0 = 0.f, a1 = 0.f;
-  for (int w = 0; w < 4 && M > -INFINITY; ++w) {
-    const float f = __expf(s_m[w] - M);
-    L += f * s_l[w];
-    a0 += f * s_o[w][e0];
-    a1 += f * s_o[w][e0 + 1];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) l[t] = swap32_sum(l[t]);
+
+  // ---- join the key groups and write
+  auto put = [&](int row, int e, float4 x) {  // elements e..e+3 of a row's normalised sum
+    const int64_t out = (static_cast<int64_t>(row / G) * a.H + hk * G + row % G);
+    if (p.part) {
+      *reinterpret_cast<float4*>(p.part + (out * p.splits + split) * a.D + e) = x;
+    } else {
+      *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(x.x, x.y), pack2<F16>(x.z, x.w));
+    }
+  };
+  auto put_lse = [&](int row, float x) {
+    const int64_t out = (static_cast<int64_t>(row / G) * a.H + hk * G + row % G);
+    if (p.part)
+      p.part_lse[out * p.splits + split] = x;
+    else if (a.lse)
+      a.lse[out] = x;
+  };
+  if constexpr (KW == 1) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int r0 = (rw * QT + t) * 32 + col;
+      if (r0 >= rows) continue;
+      const float inv = m[t] == -INFINITY ? 0.f : 1.f / l[t];
+      if (half == 0) put_lse(row0 + r0, m[t] == -INFINITY ? -INFINITY : (mc[t] + __builtin_amdgcn_logf(l[t])) * kLn2);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int e = 32 * d + 8 * (r / 4) + 4 * half;
+          if (e < a.D)
+            put(row0 + r0, e, make_float4(o[t][d][r] * inv, o[t][d][r + 1] * inv, o[t][d][r + 2] * inv, o[t][d][r + 3] * inv));
+        }
+    }
+  } else {
+    float* const acc = reinterpret_cast<float*>(smem);                   // [KW][kRows][kOutRow]
+    float* const stat = acc + KW * kRows * kOutRow;                      // [KW][kRows][2]
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int r0 = kw * kRows + (rw * QT + t) * 32 + col;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4*>(acc + r0 * kOutRow + 32 * d + 8 * (r / 4) + 4 * half) =
+              make_float4(o[t][d][r], o[t][d][r + 1], o[t][d][r + 2], o[t][d][r + 3]);
+      if (half == 0) {
+        stat[r0 * 2] = m[t] == -INFINITY ? -INFINITY : mc[t];
+        stat[r0 * 2 + 1] = l[t];
+      }
+    }
+    __syncthreads();
+    for (int x = tid; x < rows * (ND * 8); x += 64 * RW * KW) {
+      const int r = x / (ND * 8), e = x % (ND * 8) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) M = fmaxf(M, stat[(w * kRows + r) * 2]);
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      // a NaN statistic (NaN logits) keeps M from seeing it, but not L
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float mw = stat[(w * kRows + r) * 2];
+        if (mw == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(mw - M);
+        L += f * stat[(w * kRows + r) * 2 + 1];
+        const float4 y = *reinterpret_cast<const float4*>(acc + (w * kRows + r) * kOutRow + e);
+        sum.x += f * y.x;
+        sum.y += f * y.y;
+        sum.z += f * y.z;
+        sum.w += f * y.w;
+      }
+      const float inv = M == -INFINITY ? 0.f : 1.f / L;
+      if (e < a.D) put(row0 + r, e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+      if (e == 0) put_lse(row0 + r, M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2);
+    }
   }
-  if (on) {
-    uint16_t* out = a.out + row * a.D;
-    out[e0] = f32_to_half<F16>(M > -INFINITY ? a0 / L : 0.f);
-    out[e0 + 1] = f32_to_half<F16>(M > -INFINITY ? a1 / L : 0.f);
+}
+
+// Joins the runs of a row, one wavefront a row: prefix runs, then the own runs
+// that hold keys (the first one always).
+template <bool F16>
+__global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, AttnPlan p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= static_cast<int64_t>(a.B) * a.L * a.H) return;
+  const int b = static_cast<int>(row / a.H / a.L);
+  int runs = p.own_first;
+  if (p.own_splits > 0)
+    runs += max(1, (kv_len(a.kv, b, a.max_seq_len) + p.own_run - 1) / p.own_run);
+  const float* lse = p.part_lse + row * p.splits;
+  const float* part = p.part + row * p.splits * a.D;
+  float M = -INFINITY;
+  for (int s = lane; s < runs; s += 64) M = fmaxf(M, lse[s]);
+  M = wave_allmax(M);
+  float L = 0.f, o0 = 0.f, o1 = 0.f;
+  const int e = lane * 2;
+  if (M > -INFINITY) {
+    for (int s = 0; s < runs; ++s) {
+      const float f = __expf(lse[s] - M);
+      if (lse[s] == -INFINITY) continue;
+      L += f;
+      if (e < a.D) {
+        const float2 x = *reinterpret_cast<const float2*>(part + static_cast<int64_t>(s) * a.D + e);
+        o0 += f * x.x;
+        o1 += f * x.y;
+      }
+    }
   }
+  const float inv = M > -INFINITY ? 1.f / L : 0.f;
+  if (e < a.D) *reinterpret_cast<uint32_t*>(a.out + row * a.D + e) = pack2<F16>(o0 * inv, o1 * inv);
   if (lane == 0 && a.lse) a.lse[row] = M > -INFINITY ? M + __logf(L) : -INFINITY;
+}
+
+int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
+
+// The tile of a launch: rows, and keys of a step of the whole workgroup.
+struct TileShape { int rows, keys; };
+constexpr TileShape kShapes[] = {{32, 128}, {64, 128}, {128, 64}, {256, 64}};
+int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
+
+struct CallPlan {
+  AttnPlan p;
+  int pre_shape, own_shape;  // -1: nothing to do
+};
+
+CallPlan make_plan(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len) {
+  CallPlan c{};
+  const int G = H / Hkv;
+  c.pre_shape = c.own_shape = -1;
+  if (prefix_len > 0) {
+    const int64_t rows = static_cast<int64_t>(B) * L * G;
+    c.pre_shape = shape_for(rows);
+    const TileShape t = kShapes[c.pre_shape];
+    c.p.pre_tiles = ceil_div(rows, t.rows);
+    // runs: the fewest rounds of workgroups, each paying its start and its join
+    int best = 1;
+    double cost = 1e300;
+    for (int s = 1; s <= 64; ++s) {
+      const int run = ceil_div(ceil_div(prefix_len, s), t.keys) * t.keys;
+      const int used = ceil_div(prefix_len, run);
+      if (used != s) continue;
+      const double x = ceil_div(static_cast<int64_t>(c.p.pre_tiles) * Hkv * s, kCUs) * (run + 512.0);
+      if (x < cost) {
+        cost = x;
+        best = s;
+      }
+    }
+    c.p.pre_run = ceil_div(ceil_div(prefix_len, best), t.keys) * t.keys;
+    c.p.pre_splits = best;
+    c.p.pre_groups = Hkv * best;
+  }
+  if (max_seq_len > 0 || prefix_len == 0) {
+    const int rows = L * G;
+    c.own_shape = shape_for(rows);
+    const TileShape t = kShapes[c.own_shape];
+    c.p.own_tiles = ceil_div(rows, t.rows);
+    const int64_t whole = static_cast<int64_t>(B) * Hkv * c.p.own_tiles;
+    const int most = max_seq_len > 0 ? max_seq_len : 1;
+    const int want = static_cast<int>(whole >= 2 * kCUs ? 1 : ceil_div(2 * kCUs, whole));
+    c.p.own_run = ceil_div(ceil_div(most, want < 64 ? want : 64), t.keys) * t.keys;
+    c.p.own_splits = ceil_div(most, c.p.own_run);
+    c.p.own_groups = B * Hkv * c.p.own_splits;
+  }
+  c.p.own_first = c.p.pre_splits;
+  c.p.splits = c.p.pre_splits + c.p.own_splits;
+  return c;
+}
+
+template <bool F16, int ND>
+void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
+  const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
+  switch (shape) {
+    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 4, 1>), grid, dim3(256), 0, s, a, p); break;
+    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 4, 1>), grid, dim3(256), 0, s, a, p); break;
+    case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
+    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
+  }
+}
+
+template <bool F16>
+void launch_all(const AttentionArgs& a, const CallPlan& c, hipStream_t s) {
+  auto go = [&](int shape, const AttnPlan& p) {
+    if (a.D <= 64)
+      launch_shape<F16, 2>(shape, a, p, s);
+    else if (a.D <= 96)
+      launch_shape<F16, 3>(shape, a, p, s);
+    else
+      launch_shape<F16, 4>(shape, a, p, s);
+  };
+  if (c.pre_shape == c.own_shape) {
+    go(c.pre_shape, c.p);
+  } else {
+    AttnPlan pre = c.p, own = c.p;
+    pre.own_groups = own.pre_groups = 0;
+    if (c.pre_shape >= 0) go(c.pre_shape, pre);
+    if (c.own_shape >= 0) go(c.own_shape, own);
+  }
+  if (c.p.part) {
+    const int64_t rows = static_cast<int64_t>(a.B) * a.L * a.H;
+    hipLaunchKernelGGL(join_kernel<F16>, dim3(ceil_div(rows, 4)), dim3(256), 0, s, a, c.p);
+  }
 }
 
 }  // namespace
 
-size_t attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len) { return 0; }
+// Workspace: where rows have several runs, a log-sum-exp and D sums of each.
+size_t attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len) {
+  const CallPlan c = make_plan(B, L, H, Hkv, D, prefix_len, max_seq_len);
+  if (c.p.splits <= 1) return 0;
+  const size_t runs = static_cast<size_t>(B) * L * H * c.p.splits;
+  return (runs + 3) / 4 * 16 + runs * D * sizeof(float);
+}
 
 void launch_attention(const AttentionArgs& a, bool f16, void* ws, hipStream_t s) {
-  const dim3 grid(a.B * a.L * a.H);
+  CallPlan c = make_plan(a.B, a.L, a.H, a.Hkv, a.D, a.prefix_len, a.max_seq_len);
+  if (c.p.splits > 1) {
+    const size_t runs = static_cast<size_t>(a.B) * a.L * a.H * c.p.splits;
+    c.p.part_lse = static_cast<float*>(ws);
+    c.p.part = c.p.part_lse + (runs + 3) / 4 * 4;
+  }
   if (f16)
-    hipLaunchKernelGGL(attention_kernel<true>, grid, dim3(256), 0, s, a);
+    launch_all<true>(a, c, s);
   else
-    hipLaunchKernelGGL(attention_kernel<false>, grid, dim3(256), 0, s, a);
+    launch_all<false>(a, c, s);
 }
 
 }  // namespace brisk
