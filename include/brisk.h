@@ -531,7 +531,8 @@ int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* pr
  *   lse         [B*L, n_heads] fp32
  *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array
  *
- * Limits as brisk_block_attention; 1 <= cap <= 2^30; lengths are cut to cap.
+ * Limits as brisk_block_attention; 1 <= cap <= 2^30, B * n_kv_heads * cap <=
+ * 2^36; lengths are cut to cap.
  * Deterministic (fixed-order sums, no atomics).
  */
 int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_row_stride,
@@ -566,7 +567,8 @@ int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap,
  *   ws          device scratch of brisk_cache_evict_workspace_size bytes
  *
  * Limits: the cache's; B >= 1, B * n_kv_heads <= 2^20, 1 <= cap <= 2^24,
- * budget >= 1, 0 <= recent <= budget; lengths are cut to cap.  Two sequences
+ * B * n_kv_heads * cap <= 2^36, budget >= 1, 0 <= recent <= budget; lengths
+ * are cut to cap.  Two sequences
  * must not share a page that holds slots below budget of either.
  */
 int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score_in,

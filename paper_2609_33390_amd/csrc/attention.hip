@@ -16,20 +16,16 @@
 // between the wavefront's halves, and the probabilities are already the
 // operand of out^T = V^T P^T, with the keys in an order that the transposed
 // LDS reads of V follow.
+#include "half_mfma.h"
 #include "kernels.h"
-#include "kv_common.h"
 
 namespace brisk {
 
 namespace {
 
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 
 constexpr int kCUs = 256;
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
 // Source of LDS rows and chunks that hold nothing.
 __device__ const uint4 g_zeros[1] = {};
@@ -43,14 +39,6 @@ struct AttnPlan {
   int splits;            // pre_splits + own_splits of all launches of the call
   int own_first;         // index of the first own split
 };
-
-template <bool F16>
-__device__ __forceinline__ floatx16 mfma32(uint4 a, uint4 b, floatx16 c) {
-  if constexpr (F16)
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
 
 template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -76,11 +64,8 @@ __device__ __forceinline__ float swap32_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Rows of keys in LDS: RB bytes each, their 16-byte chunks permuted by the
-// key so that neither the b128 reads of K (one chunk of 16 keys) nor the
-// transposed b64 reads of V (four chunks of 4 keys) meet in a bank.
-template <int RB>
-__device__ __forceinline__ int k_swizzle(int key) { return RB == 256 ? key & 15 : (key >> 1) & 7; }
+// Values take another permutation than keys, for the transposed b64 reads of
+// four chunks of 4 keys.
 template <int RB>
 __device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; }
 
@@ -177,7 +162,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
       const int64_t at = own ? clamp_id(page[i], a.kv.n_pages) * a.kv.page_stride +
                                    (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride
                              : j * a.pre_slot_stride;
-      const int ek = (pc ^ k_swizzle<RB>(key)) * 8, ev = (pc ^ v_swizzle<RB>(key)) * 8;
+      const int ek = (pc ^ row_swizzle<RB>(key)) * 8, ev = (pc ^ v_swizzle<RB>(key)) * 8;
       const void* zeros = g_zeros;
       const void* sk = j < key1 && ek < a.D ? k_src + at + ek : zeros;
       const void* sv = j < v_end && ev < a.D ? v_src + at + ev : zeros;
@@ -231,7 +216,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
         const int key = n * 32 + col;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ k_swizzle<RB>(key)) << 4));
+          const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
 #pragma unroll
           for (int t = 0; t < QT; ++t) s[t][n] = mfma32<F16>(kf, q[t][i], s[t][n]);
         }
@@ -308,7 +293,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
             float dot = 0.f;
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-              const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ k_swizzle<RB>(key)) << 4));
+              const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
               const uint32_t kw4[4] = {kf.x, kf.y, kf.z, kf.w};
               uint32_t qw4[4] = {q[t][i].x, q[t][i].y, q[t][i].z, q[t][i].w};
               // converted here, not ahead of the loop: this path is rare and the registers are not

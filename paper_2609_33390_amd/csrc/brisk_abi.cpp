@@ -26,6 +26,7 @@ constexpr int32_t kMaxProfileBlocks = 1 << 30;
 constexpr int32_t kMaxAttnRows = 1 << 24;
 constexpr int32_t kMaxSlots = 1 << 30;
 constexpr int32_t kMaxEvictCap = 1 << 24;
+constexpr int64_t kMaxScores = int64_t{1} << 36;  // slots of all sequences and heads
 // The paged cache: sizes, strides and alignment.  `view` is filled on success.
 int cache_check(const brisk_kv_cache* c, brisk::KvView* view) {
   if (!c || !c->k_pages || !c->v_pages || !c->block_table || !c->seq_len) return BRISK_ERR_NULL;
@@ -65,7 +66,8 @@ int attention_shape_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_he
 
 int evict_shape_check(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget) {
   if (B < 1 || n_kv_heads < 1 || n_kv_heads > 1024 || static_cast<int64_t>(B) * n_kv_heads > kMaxRows ||
-      cap < 1 || cap > kMaxEvictCap || budget < 1)
+      cap < 1 || cap > kMaxEvictCap || budget < 1 ||
+      static_cast<int64_t>(B) * n_kv_heads * cap > kMaxScores)
     return BRISK_ERR_SHAPE;
   return BRISK_OK;
 }
@@ -513,8 +515,8 @@ int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_
   if (!q || !lse || !score_in || !score_out) return BRISK_ERR_NULL;
   st = block_rows_check(B, L, n_heads, cache->n_kv_heads);
   if (st != BRISK_OK) return st;
-  if (cap < 1 || cap > kMaxSlots || q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) ||
-      scale > 3.0e38f)
+  if (cap < 1 || cap > kMaxSlots || static_cast<int64_t>(B) * cache->n_kv_heads * cap > kMaxScores ||
+      q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) || scale > 3.0e38f)
     return BRISK_ERR_SHAPE;
   if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned8(block_mask) ||
       !aligned4(lse) || !aligned4(score_in) || !aligned4(score_out))
