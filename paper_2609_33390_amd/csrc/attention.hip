@@ -16,6 +16,8 @@
 // between the wavefront's halves, and the probabilities are already the
 // operand of out^T = V^T P^T, with the keys in an order that the transposed
 // LDS reads of V follow.
+#include <utility>
+
 #include "half_mfma.h"
 #include "kernels.h"
 
@@ -141,41 +143,65 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
     }
   }
 
-  const uint16_t* const k_src = (own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
-  const uint16_t* const v_src = (own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
+  // ---- copies of keys and values to LDS
+  // A copy is 1 KiB: RPI keys, RB / 16 lanes a key.  The place of a key in
+  // memory is worked out once, by the lane that holds it for this wavefront's
+  // copies, and handed to the key's lanes by broadcasts inside 16-lane rows.
+  const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
+  const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
   uint8_t* const lds = smem + kw * (kStages * kStage);
-
-  // Page ids of the rows this lane copies of the tile at j0.
-  int page[NI];
+  constexpr int kPerRow = 256 / RB;              // keys of a copy in 16 lanes
+  const int held = (rw * NI + lane % 16 / kPerRow) * RPI + lane / 16 * kPerRow + lane % kPerRow;
+  const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
+  const bool whole = a.D == 32 * ND;
+  int page = 0;                                  // page id of the held key, a tile ahead
   auto look_up = [&](int j0) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int j = min(j0 + (rw * NI + i) * RPI + lane / (RB / 16), key1 - 1);
-      page[i] = own ? a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (max(j, 0) >> a.kv.page_shift)] : 0;
-    }
+    const int j = max(min(j0 + held, key1 - 1), 0);
+    if (own) page = a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (j >> a.kv.page_shift)];
   };
   // Copies the tile at j0; slots from v_end on get no value (key1, or where the block begins).
   auto stage = [&](int j0, int buf, int v_end) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int copy = rw * NI + i, key = copy * RPI + lane / (RB / 16), pc = lane % (RB / 16), j = j0 + key;
-      const int64_t at = own ? clamp_id(page[i], a.kv.n_pages) * a.kv.page_stride +
-                                   (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride
-                             : j * a.pre_slot_stride;
-      const int ek = (pc ^ row_swizzle<RB>(key)) * 8, ev = (pc ^ v_swizzle<RB>(key)) * 8;
-      const void* zeros = g_zeros;
-      const void* sk = j < key1 && ek < a.D ? k_src + at + ek : zeros;
-      const void* sv = j < v_end && ev < a.D ? v_src + at + ev : zeros;
-      uint8_t* dst = lds + buf * kStage + copy * 1024;
+    const int j = max(min(j0 + held, key1 - 1), 0);
+    const int64_t at = 2 * (own ? clamp_id(page, a.kv.n_pages) * a.kv.page_stride +
+                                      (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride
+                                : j * a.pre_slot_stride);
+    const int lo = static_cast<int>(at), hi = static_cast<int>(at >> 32);
+    const bool plain = whole && j0 + T <= v_end;
+    uint8_t* dst = lds + buf * kStage + rw * NI * 1024;
+    auto copy = [&](auto index) {
+      constexpr int i = index;
+      int l, h;
+      if constexpr (kPerRow == 1) {
+        l = __builtin_amdgcn_update_dpp(0, lo, 0x150 + i, 0xF, 0xF, false);
+        h = __builtin_amdgcn_update_dpp(0, hi, 0x150 + i, 0xF, 0xF, false);
+      } else {
+        l = __builtin_amdgcn_update_dpp(0, lo, 0x150 + 2 * i, 0xF, 0x3, false);
+        h = __builtin_amdgcn_update_dpp(0, hi, 0x150 + 2 * i, 0xF, 0x3, false);
+        l = __builtin_amdgcn_update_dpp(l, lo, 0x150 + 2 * i + 1, 0xF, 0xC, false);
+        h = __builtin_amdgcn_update_dpp(h, hi, 0x150 + 2 * i + 1, 0xF, 0xC, false);
+      }
+      const int64_t off = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(h)) << 32 | static_cast<uint32_t>(l));
+      const int key = (rw * NI + i) * RPI + key_in;
+      const int ck = pc ^ row_swizzle<RB>(key), cv = pc ^ v_swizzle<RB>(key);
+      const void *sk = k_src + off + ck * 16, *sv = v_src + off + cv * 16;
+      if (!plain) {
+        const void* zeros = g_zeros;
+        sk = j0 + key < key1 && ck * 8 < a.D ? sk : zeros;
+        sv = j0 + key < v_end && cv * 8 < a.D ? sv : zeros;
+      }
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sk,
-                                       (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+                                       (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sv,
-                                       (__attribute__((address_space(3))) void*)(dst + kTile), 16, 0, 0);
-    }
+                                       (__attribute__((address_space(3))) void*)(dst + i * 1024 + kTile), 16, 0, 0);
+    };
+    [&]<int... I>(std::integer_sequence<int, I...>) { (copy(std::integral_constant<int, I>{}), ...); }(
+        std::make_integer_sequence<int, NI>{});
   };
 
   floatx16 o[QT][ND];
-  float m[QT], mc[QT], l[QT];  // m: subtracted logit (unscaled), mc = c * m; l: this lane's part of the sum
+  // m: the subtracted logit (unscaled); mc = c * m; l: this lane's part of the sum, zero while
+  // the row has seen no key (NaN logits pass the maximum by, but not the sum)
+  float m[QT], mc[QT], l[QT];
   const int steps = (key1 - key0 + T * KW - 1) / (T * KW);
 
   // The second time round only where values that some rows must not see are
@@ -198,7 +224,10 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
     for (int step = 0; step < steps; ++step, j0 += T * KW) {
       const int buf = step & 1;
       __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // vmcnt(0): this wavefront's copies have landed
-      __syncthreads();
+      if constexpr (RW > 1)
+        __syncthreads();
+      else
+        __builtin_amdgcn_wave_barrier();         // no other wavefront writes or reads this one's tiles
       if (step + 1 < steps) {
         stage(j0 + T * KW, buf ^ 1, v_end);
         look_up(j0 + 2 * T * KW);
@@ -287,7 +316,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
       if (careful && j0 + T > base) {
         for (int j = max(j0, base); j < min(j0 + T, key1); ++j) {
           const int key = j - j0;
-          const uint16_t* v = v_src + kv_slot(a.kv, b, j);
+          const uint16_t* v = reinterpret_cast<const uint16_t*>(v_src) + kv_slot(a.kv, b, j);
 #pragma unroll
           for (int t = 0; t < QT; ++t) {
             float dot = 0.f;
@@ -358,8 +387,8 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
     for (int t = 0; t < QT; ++t) {
       const int r0 = (rw * QT + t) * 32 + col;
       if (r0 >= rows) continue;
-      const float inv = m[t] == -INFINITY ? 0.f : 1.f / l[t];
-      if (half == 0) put_lse(row0 + r0, m[t] == -INFINITY ? -INFINITY : (mc[t] + __builtin_amdgcn_logf(l[t])) * kLn2);
+      const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
+      if (half == 0) put_lse(row0 + r0, l[t] == 0.f ? -INFINITY : (mc[t] + __builtin_amdgcn_logf(l[t])) * kLn2);
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -383,7 +412,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
           *reinterpret_cast<float4*>(acc + r0 * kOutRow + 32 * d + 8 * (r / 4) + 4 * half) =
               make_float4(o[t][d][r], o[t][d][r + 1], o[t][d][r + 2], o[t][d][r + 3]);
       if (half == 0) {
-        stat[r0 * 2] = m[t] == -INFINITY ? -INFINITY : mc[t];
+        stat[r0 * 2] = l[t] == 0.f ? -INFINITY : mc[t];
         stat[r0 * 2 + 1] = l[t];
       }
     }
@@ -394,11 +423,10 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
 #pragma unroll
       for (int w = 0; w < KW; ++w) M = fmaxf(M, stat[(w * kRows + r) * 2]);
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      // a NaN statistic (NaN logits) keeps M from seeing it, but not L
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const float mw = stat[(w * kRows + r) * 2];
-        if (mw == -INFINITY) continue;
+        if (mw == -INFINITY) continue;             // no key seen
         const float f = __builtin_amdgcn_exp2f(mw - M);
         L += f * stat[(w * kRows + r) * 2 + 1];
         const float4 y = *reinterpret_cast<const float4*>(acc + (w * kRows + r) * kOutRow + e);
@@ -407,46 +435,56 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
         sum.z += f * y.z;
         sum.w += f * y.w;
       }
-      const float inv = M == -INFINITY ? 0.f : 1.f / L;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
       if (e < a.D) put(row0 + r, e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
-      if (e == 0) put_lse(row0 + r, M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2);
+      if (e == 0) put_lse(row0 + r, L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2);
     }
   }
 }
 
-// Joins the runs of a row, one wavefront a row: prefix runs, then the own runs
-// that hold keys (the first one always).
+// Joins the runs of a row: prefix runs, then the own runs that hold keys (the
+// first one always).  One wavefront a row; a half takes every second run with
+// four elements a lane, and four runs of a half are in flight.
 template <bool F16>
 __global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, AttnPlan p) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (row >= static_cast<int64_t>(a.B) * a.L * a.H) return;
   const int b = static_cast<int>(row / a.H / a.L);
-  int runs = p.own_first;
-  if (p.own_splits > 0)
-    runs += max(1, (kv_len(a.kv, b, a.max_seq_len) + p.own_run - 1) / p.own_run);
-  const float* lse = p.part_lse + row * p.splits;
   const float* part = p.part + row * p.splits * a.D;
-  float M = -INFINITY;
-  for (int s = lane; s < runs; s += 64) M = fmaxf(M, lse[s]);
-  M = wave_allmax(M);
-  float L = 0.f, o0 = 0.f, o1 = 0.f;
-  const int e = lane * 2;
-  if (M > -INFINITY) {
-    for (int s = 0; s < runs; ++s) {
-      const float f = __expf(lse[s] - M);
-      if (lse[s] == -INFINITY) continue;
-      L += f;
-      if (e < a.D) {
-        const float2 x = *reinterpret_cast<const float2*>(part + static_cast<int64_t>(s) * a.D + e);
-        o0 += f * x.x;
-        o1 += f * x.y;
-      }
+  const float* lse = p.part_lse + row * p.splits;
+  const int n = p.own_splits > 0 ? kv_len(a.kv, b, a.max_seq_len) : 0;
+  const int runs = p.own_first + (p.own_splits > 0 ? max(1, (n + p.own_run - 1) / p.own_run) : 0);  // at most 128
+  const float z0 = lane < runs ? lse[lane] : -INFINITY, z1 = lane + 64 < runs ? lse[lane + 64] : -INFINITY;
+  const float M = wave_allmax(fmaxf(z0, z1)), sub = M == -INFINITY ? 0.f : M;
+  // fmaxf passes over a NaN, the exponentials and their sum do not
+  const float f0 = __builtin_amdgcn_exp2f((z0 - sub) * kLog2e), f1 = __builtin_amdgcn_exp2f((z1 - sub) * kLog2e);
+  const float L = wave_allsum(f0 + f1);
+  const int e = (lane & 31) * 4, at = min(e, a.D - 4);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < runs; s += 8) {
+    float4 x[4];
+    float f[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = s + 2 * u + half;
+      x[u] = *reinterpret_cast<const float4*>(part + static_cast<int64_t>(min(r, runs - 1)) * a.D + at);
+      f[u] = __shfl(s < 64 ? f0 : f1, r & 63, kWave);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (f[u] == 0.f || s + 2 * u + half >= runs) continue;  // an empty run adds nothing
+      o.x += f[u] * x[u].x;
+      o.y += f[u] * x[u].y;
+      o.z += f[u] * x[u].z;
+      o.w += f[u] * x[u].w;
     }
   }
-  const float inv = M > -INFINITY ? 1.f / L : 0.f;
-  if (e < a.D) *reinterpret_cast<uint32_t*>(a.out + row * a.D + e) = pack2<F16>(o0 * inv, o1 * inv);
-  if (lane == 0 && a.lse) a.lse[row] = M > -INFINITY ? M + __logf(L) : -INFINITY;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  o = make_float4(swap32_sum(o.x) * inv, swap32_sum(o.y) * inv, swap32_sum(o.z) * inv, swap32_sum(o.w) * inv);
+  if (half == 0 && e < a.D)
+    *reinterpret_cast<uint2*>(a.out + row * a.D + e) = make_uint2(pack2<F16>(o.x, o.y), pack2<F16>(o.z, o.w));
+  if (lane == 0 && a.lse) a.lse[row] = L == 0.f ? -INFINITY : sub + __builtin_amdgcn_logf(L) * kLn2;
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }

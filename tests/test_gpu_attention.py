@@ -122,6 +122,18 @@ def test_hidden_slots_have_no_effect(bad, what, shape):
         assert not torch.isfinite(out[:, t:]).any()
 
 
+@pytest.mark.parametrize("H", [4, 40])
+def test_nan_queries_stay_in_their_rows(H):
+    """A row of NaN queries is NaN, not empty; the others do not notice."""
+    c = Case(2, 4, H, 2, 128, 100, [300, 40], mask="causal", seed=16)
+    ref = c.attention()
+    c.q[1, 2, 1, 5] = float("nan")
+    out, lse = _run(c)
+    assert torch.isnan(out[1, 2, 1]).all() and torch.isnan(lse[1, 2, 1])
+    out[1, 2, 1], lse[1, 2, 1] = torch.from_numpy(ref[0][1, 2, 1]).to(out), float(ref[1][1, 2, 1])
+    _check(c, out, lse, ref)
+
+
 def test_strided_queries_and_given_buffers():
     """Queries inside a fused projection, one position of a longer block, and the caller's own buffers."""
     c = Case(3, 6, 8, 2, 128, 40, [50, 6, 33], mask="causal", seed=9)
