@@ -103,16 +103,23 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
   if (group >= (own ? p.own_groups : p.pre_groups)) return;
   int b = 0, hk, split, key0, key1, row0, rows;
   if (own) {
-    split = group % p.own_splits;
-    hk = group / p.own_splits % a.Hkv;
-    b = group / p.own_splits / a.Hkv;
+    // first runs of all sequences, then second ones, ...: later runs are fewer where lengths differ
+    hk = group % a.Hkv;
+    b = group / a.Hkv % a.B;
+    split = group / a.Hkv / a.B;
     const int n = kv_len(a.kv, b, a.max_seq_len);
     key0 = split * p.own_run;
     key1 = min(n, key0 + p.own_run);
-    if (key0 >= n && split > 0) return;          // nobody reads this run
     row0 = b * a.L * G;
     rows = a.L * G;
     split += p.own_first;
+    if (key0 >= n && p.part) {                   // a run past the sequence: the join reads that it is empty
+      for (int r = tile * kRows + tid; r < min(rows, (tile + 1) * kRows); r += 64 * RW * KW) {
+        const int row = row0 + r;
+        p.part_lse[(static_cast<int64_t>(row / G) * a.H + hk * G + row % G) * p.splits + split] = -INFINITY;
+      }
+      return;
+    }
   } else {
     split = group % p.pre_splits;
     hk = group / p.pre_splits;
@@ -442,19 +449,17 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
   }
 }
 
-// Joins the runs of a row: prefix runs, then the own runs that hold keys (the
-// first one always).  One wavefront a row; a half takes every second run with
-// four elements a lane, and four runs of a half are in flight.
+// Joins the runs of a row, prefix and own.  One wavefront a row; a half takes
+// every second run with four elements a lane, and four runs of a half are in
+// flight.  What an empty run (log-sum-exp -inf) left in its sums is not used.
 template <bool F16>
 __global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, AttnPlan p) {
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (row >= static_cast<int64_t>(a.B) * a.L * a.H) return;
-  const int b = static_cast<int>(row / a.H / a.L);
   const float* part = p.part + row * p.splits * a.D;
   const float* lse = p.part_lse + row * p.splits;
-  const int n = p.own_splits > 0 ? kv_len(a.kv, b, a.max_seq_len) : 0;
-  const int runs = p.own_first + (p.own_splits > 0 ? max(1, (n + p.own_run - 1) / p.own_run) : 0);  // at most 128
+  const int runs = p.splits;  // at most 128
   const float z0 = lane < runs ? lse[lane] : -INFINITY, z1 = lane + 64 < runs ? lse[lane + 64] : -INFINITY;
   const float M = wave_allmax(fmaxf(z0, z1)), sub = M == -INFINITY ? 0.f : M;
   // fmaxf passes over a NaN, the exponentials and their sum do not
@@ -491,7 +496,7 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 // The tile of a launch: rows, and keys of a step of the whole workgroup.
 struct TileShape { int rows, keys; };
-constexpr TileShape kShapes[] = {{32, 128}, {64, 128}, {128, 64}, {256, 64}};
+constexpr TileShape kShapes[] = {{32, 64}, {64, 64}, {128, 64}, {256, 64}};
 int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
 
 struct CallPlan {
@@ -546,8 +551,8 @@ template <bool F16, int ND>
 void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
   const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
   switch (shape) {
-    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 4, 1>), grid, dim3(256), 0, s, a, p); break;
-    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 4, 1>), grid, dim3(256), 0, s, a, p); break;
+    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
+    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
     case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
     default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
   }
