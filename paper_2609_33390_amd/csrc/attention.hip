@@ -16,8 +16,6 @@
 // between the wavefront's halves, and the probabilities are already the
 // operand of out^T = V^T P^T, with the keys in an order that the transposed
 // LDS reads of V follow.
-#include <utility>
-
 #include "half_mfma.h"
 #include "kernels.h"
 
@@ -28,9 +26,6 @@ namespace {
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCUs = 256;
-
-// Source of LDS rows and chunks that hold nothing.
-__device__ const uint4 g_zeros[1] = {};
 
 // What one launch works on: prefix items, then own items.
 struct AttnPlan {
@@ -157,8 +152,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
   const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
   const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
   uint8_t* const lds = smem + kw * (kStages * kStage);
-  constexpr int kPerRow = 256 / RB;              // keys of a copy in 16 lanes
-  const int held = (rw * NI + lane % 16 / kPerRow) * RPI + lane / 16 * kPerRow + lane % kPerRow;
+  const int held = rw * NI * RPI + held_key<RB>(lane);
   const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
   const bool whole = a.D == 32 * ND;
   int page = 0;                                  // page id of the held key, a tile ahead
@@ -172,22 +166,11 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
     const int64_t at = 2 * (own ? clamp_id(page, a.kv.n_pages) * a.kv.page_stride +
                                       (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride
                                 : j * a.pre_slot_stride);
-    const int lo = static_cast<int>(at), hi = static_cast<int>(at >> 32);
     const bool plain = whole && j0 + T <= v_end;
     uint8_t* dst = lds + buf * kStage + rw * NI * 1024;
-    auto copy = [&](auto index) {
+    each_index<NI>([&](auto index) {
       constexpr int i = index;
-      int l, h;
-      if constexpr (kPerRow == 1) {
-        l = __builtin_amdgcn_update_dpp(0, lo, 0x150 + i, 0xF, 0xF, false);
-        h = __builtin_amdgcn_update_dpp(0, hi, 0x150 + i, 0xF, 0xF, false);
-      } else {
-        l = __builtin_amdgcn_update_dpp(0, lo, 0x150 + 2 * i, 0xF, 0x3, false);
-        h = __builtin_amdgcn_update_dpp(0, hi, 0x150 + 2 * i, 0xF, 0x3, false);
-        l = __builtin_amdgcn_update_dpp(l, lo, 0x150 + 2 * i + 1, 0xF, 0xC, false);
-        h = __builtin_amdgcn_update_dpp(h, hi, 0x150 + 2 * i + 1, 0xF, 0xC, false);
-      }
-      const int64_t off = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(h)) << 32 | static_cast<uint32_t>(l));
+      const int64_t off = held_offset<RB, i>(at);
       const int key = (rw * NI + i) * RPI + key_in;
       const int ck = pc ^ row_swizzle<RB>(key), cv = pc ^ v_swizzle<RB>(key);
       const void *sk = k_src + off + ck * 16, *sv = v_src + off + cv * 16;
@@ -196,13 +179,9 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
         sk = j0 + key < key1 && ck * 8 < a.D ? sk : zeros;
         sv = j0 + key < v_end && cv * 8 < a.D ? sv : zeros;
       }
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sk,
-                                       (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)sv,
-                                       (__attribute__((address_space(3))) void*)(dst + i * 1024 + kTile), 16, 0, 0);
-    };
-    [&]<int... I>(std::integer_sequence<int, I...>) { (copy(std::integral_constant<int, I>{}), ...); }(
-        std::make_integer_sequence<int, NI>{});
+      copy_to_lds(sk, dst + i * 1024);
+      copy_to_lds(sv, dst + i * 1024 + kTile);
+    });
   };
 
   floatx16 o[QT][ND];
@@ -230,7 +209,7 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
     }
     for (int step = 0; step < steps; ++step, j0 += T * KW) {
       const int buf = step & 1;
-      __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // vmcnt(0): this wavefront's copies have landed
+      copies_landed();
       if constexpr (RW > 1)
         __syncthreads();
       else

@@ -12,103 +12,154 @@ namespace {
 //
 // S = Q K^T with a key a lane: the sum over rows is a sum over a lane's
 // registers and its partner in the other half, in a fixed order.  A wavefront
-// keeps KT tiles of 32 keys in registers and passes over the rows of the
-// sequence's group (L x heads of the group), which the workgroup stages 64 at
-// a time in LDS, so each key is read from memory once.
+// holds 64 rows of the sequence's group (L x heads of the group) in registers
+// and passes over its run of 32-key tiles, copied to LDS one tile ahead; groups
+// of more than 64 rows pass over the run again, whose keys then come from the
+// L2, and add to what the passes before left.  No wavefront waits for another.
 // ---------------------------------------------------------------------------
-constexpr int kScoreWaves = 4, kScoreRows = 64, kKeyTiles = 2;
-constexpr int kScoreKeys = kScoreWaves * kKeyTiles * 32;  // of a workgroup
+constexpr int kScoreWaves = 4, kMaxTiles = 8;
 
-template <bool F16, int ND>
-__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs a, int runs) {
-  constexpr int RB = ND > 2 ? 256 : 128, NC = 2 * ND, CH = RB / 16;
-  __shared__ __attribute__((aligned(16))) uint8_t s_q[kScoreRows * RB];
-  __shared__ __attribute__((aligned(16))) float s_lse[kScoreRows];  // times log2 e; +inf: the row adds nothing
-  __shared__ uint64_t s_word[kScoreRows];
+// QT: 32-row tiles of queries in registers.
+template <bool F16, int ND, int QT>
+__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs a, int tiles) {
+  constexpr int RB = ND > 2 ? 256 : 128, NC = 2 * ND, kTile = 32 * RB, NI = kTile / 1024, RPI = 1024 / RB;
+  constexpr int kScoreRows = 32 * QT;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_keys[kScoreWaves][2][kTile];
+  __shared__ __attribute__((aligned(16))) float s_lse[kScoreWaves][kScoreRows];  // times log2 e; +inf: adds nothing
+  __shared__ uint64_t s_word[kScoreWaves][kScoreRows];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = blockIdx.x / runs, b = bh / a.Hkv, hk = bh % a.Hkv, G = a.H / a.Hkv;
-  const int first = blockIdx.x % runs * kScoreKeys + wave * (kKeyTiles * 32);
-  const int n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift));
+  // first runs of all sequences, then second ones, ...: the runs past the shorter
+  // sequences then spread over the XCDs
+  const int heads = a.B * a.Hkv, bh = blockIdx.x % heads, b = bh / a.Hkv, hk = bh % a.Hkv, G = a.H / a.Hkv;
+  const int first = (blockIdx.x / heads * kScoreWaves + wave) * tiles * 32;
+  if (first >= a.cap) return;
+  const int n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift)), base = n - a.L;
   const int64_t at = static_cast<int64_t>(bh) * a.cap;
-  if (blockIdx.x % runs * kScoreKeys >= n) {  // the whole workgroup is past the sequence
-    for (int j = first + lane; j < min(a.cap, first + kKeyTiles * 32); j += 64) a.score_out[at + j] = 0.f;
-    return;
-  }
-  const int base = n - a.L;
+  const int held_tiles = min(tiles, (n - first + 31) / 32);  // tiles that hold keys
   const float c = a.scale * kLog2e;
-
-  uint4 k[kKeyTiles][NC];
-#pragma unroll
-  for (int t = 0; t < kKeyTiles; ++t) {
-    const int j = first + t * 32 + col;
-    const uint16_t* src = a.kv.k + kv_slot(a.kv, b, min(j, n - 1)) + hk * a.kv.head_stride;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int e = 16 * i + 8 * half;
-      k[t][i] = j < n && e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
-    }
-  }
-  float sum[kKeyTiles] = {};
   const int rows = a.L * G;
-  for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
-    __syncthreads();
-    for (int x = tid; x < kScoreRows * CH; x += 64 * kScoreWaves) {
-      const int r = x / CH, e = x % CH * 8, row = r0 + r;
-      const int64_t bi = static_cast<int64_t>(b) * a.L + row / G;
-      const bool on = row < rows && e < a.D;
-      *reinterpret_cast<uint4*>(s_q + r * RB + (((e / 8) ^ row_swizzle<RB>(r)) << 4)) =
-          on ? *reinterpret_cast<const uint4*>(a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride + e)
-             : make_uint4(0, 0, 0, 0);
-    }
-    if (tid < kScoreRows) {
-      const int row = r0 + tid;
-      const int64_t bi = static_cast<int64_t>(b) * a.L + row / G;
-      const float z = row < rows ? a.lse[bi * a.H + hk * G + row % G] : -INFINITY;
-      s_lse[tid] = z == -INFINITY ? INFINITY : z * kLog2e;
-      s_word[tid] = row < rows && a.mask ? a.mask[bi] : ~0ull;
-    }
-    __syncthreads();
+  const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(a.kv.k + hk * a.kv.head_stride);
+
+  // the slot this lane holds the place of; slots past the sequence repeat its last key
+  int page = 0;
+  auto held_slot = [&](int t) { return max(min(first + t * 32 + held_key<RB>(lane) % 32, n - 1), 0); };
+  auto look_up = [&](int t) {
+    page = a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (held_slot(t) >> a.kv.page_shift)];
+  };
+  auto stage = [&](int t, int buf) {
+    const int j = held_slot(t);
+    const int64_t at_held = 2 * (clamp_id(page, a.kv.n_pages) * a.kv.page_stride +
+                                 (j & ((1 << a.kv.page_shift) - 1)) * a.kv.slot_stride);
+    each_index<NI>([&](auto index) {
+      constexpr int i = index;
+      const int key = i * RPI + lane / (RB / 16), chunk = lane % (RB / 16) ^ row_swizzle<RB>(key);
+      const void* src = k_src + held_offset<RB, i>(at_held) + chunk * 16;
+      const void* zeros = g_zeros;
+      copy_to_lds(chunk * 8 < a.D ? src : zeros, s_keys[wave][buf] + i * 1024);
+    });
+  };
+
+  int buf = 0;
+  if (held_tiles > 0) {
+    look_up(0);
+    stage(0, 0);
+    look_up(held_tiles > 1 ? 1 : 0);
+  }
+  // What a tile's scores start from is loaded, and its result stored, a tile
+  // away from its products: loads and stores count with the copies, so a wait
+  // for either here would be a wait for the next tile's keys.
+  auto start_of = [&](int t, int r0) {
+    const int j = min(first + t * 32 + col, n - 1);
+    return (r0 == 0 ? a.score_in : a.score_out)[at + j];
+  };
+  float old = held_tiles > 0 ? start_of(0, 0) : 0.f, done = 0.f;
+  int done_tile = -1;
+  auto flush = [&] {
+    const int j = first + done_tile * 32 + col;
+    if (done_tile >= 0 && half == 0 && j < n) a.score_out[at + j] = done;
+    done_tile = -1;
+  };
+  for (int r0 = 0; r0 < rows && held_tiles > 0; r0 += kScoreRows) {
+    // ---- a tile of queries, their log-sum-exps and mask words; the rows past the last
+    // repeat it and add nothing
+    uint4 q[QT][NC];
 #pragma unroll
-    for (int q0 = 0; q0 < kScoreRows; q0 += 32) {
-      if (r0 + q0 >= rows) break;
-      floatx16 s[kKeyTiles];
-#pragma unroll
-      for (int t = 0; t < kKeyTiles; ++t) s[t] = floatx16{};
+    for (int t = 0; t < QT; ++t) {
+      const int row = min(r0 + t * 32 + col, rows - 1);
+      const int64_t bi = static_cast<int64_t>(b) * a.L + row / G;
+      const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        const int r = q0 + col;
-        const uint4 q = *reinterpret_cast<const uint4*>(s_q + r * RB + (((2 * i + half) ^ row_swizzle<RB>(r)) << 4));
-#pragma unroll
-        for (int t = 0; t < kKeyTiles; ++t) s[t] = mfma32<F16>(q, k[t][i], s[t]);
-      }
-      const bool block = a.mask && first + kKeyTiles * 32 > base;
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int row = q0 + 8 * (r / 4) + 4 * half;
-        const float4 z4 = *reinterpret_cast<const float4*>(s_lse + row);
-        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int t = 0; t < kKeyTiles; ++t) {
-            float p = __builtin_amdgcn_exp2f(fmaf(s[t][r + x], c, -z[x]));
-            bool off = z[x] == INFINITY;
-            if (block) {
-              const int place = first + t * 32 + col - base;
-              off |= place >= 0 && !block_sees(s_word[row + x], place);
-            }
-            sum[t] += off ? 0.f : p;
-          }
+        const int e = 16 * i + 8 * half;
+        q[t][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
       }
     }
-  }
+    const int row_in = r0 + lane % kScoreRows;
+    const int64_t bi_in = static_cast<int64_t>(b) * a.L + min(row_in, rows - 1) / G;
+    const float z_in = row_in < rows ? a.lse[bi_in * a.H + hk * G + row_in % G] : -INFINITY;
+    s_lse[wave][lane % kScoreRows] = z_in == -INFINITY ? INFINITY : z_in * kLog2e;
+    s_word[wave][lane % kScoreRows] = a.mask ? a.mask[bi_in] : ~0ull;
+    const bool holes = __any(z_in == -INFINITY);   // rows that add nothing
+    __builtin_amdgcn_wave_barrier();
+    for (int t = 0; t < held_tiles; ++t) {
+      copies_landed();
+      __builtin_amdgcn_wave_barrier();
+      const uint8_t* kt = s_keys[wave][buf];
+      buf ^= 1;
+      const int next = t + 1 < held_tiles ? t + 1 : 0;  // and round again for the next rows
+      const float begin = r0 == 0 ? a.decay * old : old;
+      flush();
+      if (next > 0 || r0 + kScoreRows < rows) {
+        stage(next, buf);
+        look_up(next + 1 < held_tiles ? next + 1 : 0);
+        // the next rows' start at a run of one tile is this tile's own result
+        if (held_tiles > 1) old = start_of(next, next > 0 ? r0 : r0 + kScoreRows);
+      }
+      floatx16 s[QT];
 #pragma unroll
-  for (int t = 0; t < kKeyTiles; ++t) {
-    const float x = swap32_sum(sum[t]);
-    const int j = first + t * 32 + col;
-    if (half == 0 && j < a.cap) a.score_out[at + j] = j < n ? a.decay * a.score_in[at + j] + x : 0.f;
+      for (int u = 0; u < QT; ++u) s[u] = floatx16{};
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const uint4 k = *reinterpret_cast<const uint4*>(kt + col * RB + (((2 * i + half) ^ row_swizzle<RB>(col)) << 4));
+#pragma unroll
+        for (int u = 0; u < QT; ++u) s[u] = mfma32<F16>(q[u][i], k, s[u]);
+      }
+      const int j = first + t * 32 + col, place = j - base;
+      float sum = 0.f;
+      // What a lane adds; `plain`: every row adds its weight, whichever the key
+      auto add_up = [&](auto plain) {
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const int row = u * 32 + 8 * (r / 4) + 4 * half;
+            const float4 z4 = *reinterpret_cast<const float4*>(s_lse[wave] + row);
+            const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r + x], c, -z[x]));
+              if constexpr (decltype(plain)::value) {
+                sum += p;
+              } else {
+                const bool off = (z[x] == INFINITY) | (place >= 0 && !block_sees(s_word[wave][row + x], place));
+                sum += off ? 0.f : p;
+              }
+            }
+          }
+      };
+      if (holes || (a.mask && first + t * 32 + 32 > base))
+        add_up(std::false_type{});
+      else
+        add_up(std::true_type{});
+      done = begin + swap32_sum(sum);
+      done_tile = t;
+      if (held_tiles == 1) old = done;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
+  flush();
+  for (int j = max(first, n) + lane; j < min(a.cap, first + tiles * 32); j += kWave) a.score_out[at + j] = 0.f;
 }
 
 // ---------------------------------------------------------------------------
@@ -278,8 +329,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 
 // Moves listed rows, 16 lanes a row and kRowsInFlight rows at once.
 constexpr int kRowsInFlight = 4, kMoveRows = 16 * kRowsInFlight;
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int runs) {
-  const int bh = blockIdx.x / runs, r0 = blockIdx.x % runs * kMoveRows;
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
+  const int heads = a.B * a.Hkv, bh = blockIdx.x % heads, r0 = blockIdx.x / heads * kMoveRows;
   const int count = a.count[bh];
   if (r0 >= count) return;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -313,16 +364,24 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int runs) 
   }
 }
 
+// Tiles of a wavefront: eight, so that its start and its queries are paid once
+// for 256 keys, unless that leaves CUs without a workgroup.
 template <bool F16>
 void launch_score(const ScoreArgs& a, hipStream_t s) {
-  const int runs = (a.cap + kScoreKeys - 1) / kScoreKeys;
-  const dim3 grid(static_cast<uint32_t>(a.B) * a.Hkv * runs), threads(64 * kScoreWaves);
+  const int64_t whole = static_cast<int64_t>(a.B) * a.Hkv;
+  int tiles = kMaxTiles;
+  auto runs_of = [&](int t) { return (a.cap + kScoreWaves * t * 32 - 1) / (kScoreWaves * t * 32); };
+  while (tiles > 1 && whole * runs_of(tiles) < 512) tiles /= 2;
+  const int runs = runs_of(tiles);
+  const dim3 grid(static_cast<uint32_t>(whole * runs)), threads(64 * kScoreWaves);
+  const bool two = a.L * (a.H / a.Hkv) > 32;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, s, a, tiles); };
   if (a.D <= 64)
-    hipLaunchKernelGGL((score_kernel<F16, 2>), grid, threads, 0, s, a, runs);
+    two ? go(score_kernel<F16, 2, 2>) : go(score_kernel<F16, 2, 1>);
   else if (a.D <= 96)
-    hipLaunchKernelGGL((score_kernel<F16, 3>), grid, threads, 0, s, a, runs);
+    two ? go(score_kernel<F16, 3, 2>) : go(score_kernel<F16, 3, 1>);
   else
-    hipLaunchKernelGGL((score_kernel<F16, 4>), grid, threads, 0, s, a, runs);
+    two ? go(score_kernel<F16, 4, 2>) : go(score_kernel<F16, 4, 1>);
 }
 
 }  // namespace
@@ -355,7 +414,7 @@ void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s) {
     hipLaunchKernelGGL(evict_select_kernel<false>, dim3(heads), dim3(kSelectThreads), 0, s, a);
   if (a.list_len > 0) {
     const int runs = (a.list_len + kMoveRows - 1) / kMoveRows;
-    hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(256), 0, s, a, runs);
+    hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(256), 0, s, a);
   }
 }
 

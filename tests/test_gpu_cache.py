@@ -26,6 +26,8 @@ SCORE_CASES = [
     dict(B=2, L=5, H=15, Hkv=5, D=104, lens=[129, 31], mask="causal", page=8),
     dict(B=1, L=2, H=14, Hkv=2, D=128, lens=[5000], mask="causal", page=128),
     dict(B=2, L=40, H=7, Hkv=1, D=96, lens=[400, 41], mask="mixed", dtype="f16"),
+    # enough heads for long runs of tiles, with more rows than a wavefront holds
+    dict(B=66, L=5, H=128, Hkv=8, D=16, lens=[3 * b for b in range(66)], mask="causal"),
 ]
 
 
