@@ -214,28 +214,57 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
         __syncthreads();
       else
         __builtin_amdgcn_wave_barrier();         // no other wavefront writes or reads this one's tiles
-      if (step + 1 < steps) {
-        stage(j0 + T * KW, buf ^ 1, v_end);
-        look_up(j0 + 2 * T * KW);
-      }
-      if (j0 >= key1) continue;  // uniform in the wavefront; its tile is past the run
+      if (j0 >= key1) continue;  // uniform in the wavefront; this tile and all later ones are past the run
       const uint8_t* kt = lds + buf * kStage;
       const uint8_t* vt = kt + kTile;
 
       // ---- S^T = K Q^T: register r of a lane is key 8 (r / 4) + 4 half + r % 4 of each 32
+      // All reads first (the fences keep the compiler from putting each one in front of
+      // the product that needs it), so that the products follow each other.
       floatx16 s[QT][NT];
+      {
+        uint4 kf[NT][NC];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int t = 0; t < QT; ++t) s[t][n] = floatx16{};
-        const int key = n * 32 + col;
+          for (int i = 0; i < NC; ++i) {
+            const int key = n * 32 + col;
+            kf[n][i] = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
+          }
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < steps) {
+          stage(j0 + T * KW, buf ^ 1, v_end);
+          look_up(j0 + 2 * T * KW);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int t = 0; t < QT; ++t) s[t][n] = mfma32<F16>(kf, q[t][i], s[t][n]);
+          for (int t = 0; t < QT; ++t) s[t][n] = floatx16{};
+#pragma unroll
+          for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) s[t][n] = mfma32<F16>(kf[n][i], q[t][i], s[t][n]);
         }
       }
+      // The values of 16 keys, as the first operand: 8 keys of a lane's column in the
+      // order in which the lane holds their probabilities.
+      auto values = [&](int g, uint4 (&vf)[ND]) {
+        const int key = g * 16 + 4 * half + (lane & 15) / 4;  // and 8 further
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, in = (lane & 1) * 8;
+          const uint8_t* v0 = vt + key * RB + ((chunk ^ v_swizzle<RB>(key)) << 4) + in;
+          const uint8_t* v1 = v0 + 8 * RB;                      // of the same permutation
+          const shortx4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v0));
+          const shortx4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v1));
+          const uint2 y0 = __builtin_bit_cast(uint2, x0), y1 = __builtin_bit_cast(uint2, x1);
+          vf[d] = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        }
+      };
+      uint4 vf[2][ND];
+      values(0, vf[0]);
+      __builtin_amdgcn_sched_barrier(0);
       if (j0 + T > key1 || (masked && j0 + T > base)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -282,22 +311,14 @@ __global__ __launch_bounds__(64 * RW * KW) void attend_kernel(AttentionArgs a, A
           pf[t][2 * n + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
       }
-      // ---- out^T += V^T P^T, 16 keys at a time
+      // ---- out^T += V^T P^T, 16 keys at a time, the next ones' values on the way
 #pragma unroll
       for (int g = 0; g < 2 * NT; ++g) {
-        const int key = g * 16 + 4 * half + (lane & 15) / 4;  // and 8 further
+        if (g + 1 < 2 * NT) values(g + 1, vf[(g + 1) & 1]);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, in = (lane & 1) * 8;
-          const uint8_t* v0 = vt + key * RB + ((chunk ^ v_swizzle<RB>(key)) << 4) + in;
-          const uint8_t* v1 = vt + (key + 8) * RB + ((chunk ^ v_swizzle<RB>(key + 8)) << 4) + in;
-          const shortx4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v0));
-          const shortx4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(v1));
-          const uint2 y0 = __builtin_bit_cast(uint2, x0), y1 = __builtin_bit_cast(uint2, x1);
-          const uint4 vf = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int t = 0; t < QT; ++t) o[t][d] = mfma32<F16>(vf, pf[t][g], o[t][d]);
-        }
+          for (int t = 0; t < QT; ++t) o[t][d] = mfma32<F16>(vf[g & 1][d], pf[t][g], o[t][d]);
       }
       if (careful && j0 + T > base) {
         for (int j = max(j0, base); j < min(j0 + T, key1); ++j) {

@@ -58,6 +58,8 @@ __device__ __forceinline__ int held_key(int lane) {
 // the same in all lanes).  Written as assembly because the compiler waits for
 // every copy it knows of before any LDS read, and so would not let the copies
 // of one tile fly while another is read; copies_landed() is the wait.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved, so naming it as clobbered is noted
 __device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
   const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)dst));
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
@@ -65,6 +67,7 @@ __device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
                : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(src)
                : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Waits for the wavefront's own copies.
 __device__ __forceinline__ void copies_landed() {
