@@ -560,7 +560,7 @@ void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStrea
     case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1, 2>), grid, dim3(128), 0, s, a, p); break;
     case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 2, 1, 2>), grid, dim3(128), 0, s, a, p); break;
     case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2, 2>), grid, dim3(256), 0, s, a, p); break;
-    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2, 4>), grid, dim3(512), 0, s, a, p); break;
+    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2, 2>), grid, dim3(512), 0, s, a, p); break;
   }
 }
 

@@ -180,8 +180,34 @@ __device__ __forceinline__ uint32_t keep_key(float score, bool late) {
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048;
 constexpr int kLdsSlots = 32768;  // keys of a workgroup that fit in LDS beside the histogram
 
-// IN_LDS: the keys of a sequence are computed once and held in LDS; longer
-// sequences compute them anew from scores and positions in each pass.
+// The keys of sequences too long for LDS, and the outputs as they are before
+// any slot moves: many workgroups, where the selection below has one a head.
+__global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a) {
+  const int heads = a.B * a.Hkv, bh = blockIdx.x % heads, b = bh / a.Hkv;
+  const int n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift)), m = min(n, a.budget);
+  const int64_t at = static_cast<int64_t>(bh) * a.cap;
+  const int from = a.next_pos[b] - a.recent;
+  const int j0 = blockIdx.x / heads * 1024 + threadIdx.x;
+  float s[4];
+  int x[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int j = min(j0 + u * 256, a.cap - 1);
+    s[u] = a.score_in[at + j];
+    x[u] = a.pos_in[at + j];
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int j = j0 + u * 256;
+    if (j >= a.cap) break;
+    a.keys[at + j] = keep_key(s[u], x[u] >= from);
+    a.score_out[at + j] = j < m ? s[u] : 0.f;
+    a.pos_out[at + j] = j < m ? x[u] : -1;
+  }
+}
+
+// IN_LDS: the keys of a sequence are computed here and held in LDS; otherwise
+// evict_keys_kernel left them in memory, and each pass keeps more of them in flight.
 template <bool IN_LDS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   extern __shared__ uint32_t s_keys[];
@@ -194,16 +220,28 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cap;
   const float* const score = a.score_in + at;
   const int32_t* const pos = a.pos_in + at;
-  const int from = a.next_pos[b] - a.recent;
+  constexpr int kFlight = IN_LDS ? 4 : 16;
   if (tid == 0 && blockIdx.x % a.Hkv == 0) a.new_len[b] = m;
-  auto compute = [&](int j) { return keep_key(score[j], pos[j] >= from); };
-  for (int j = tid; j < a.cap; j += kSelectThreads) {
-    const float s = j < n ? score[j] : 0.f;
-    const int x = j < n ? pos[j] : -1;
-    if constexpr (IN_LDS)
-      if (j < n) s_keys[j] = keep_key(s, x >= from);
-    a.score_out[at + j] = j < m ? s : 0.f;
-    a.pos_out[at + j] = j < m ? x : -1;
+  if constexpr (IN_LDS) {
+    const int from = a.next_pos[b] - a.recent;
+    for (int j0 = tid; j0 < a.cap; j0 += kSelectThreads * 4) {
+      float s[4];
+      int x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = min(j0 + u * kSelectThreads, a.cap - 1);
+        s[u] = score[j];
+        x[u] = pos[j];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = j0 + u * kSelectThreads;
+        if (j >= a.cap) break;
+        s_keys[j] = keep_key(s[u], x[u] >= from);
+        a.score_out[at + j] = j < m ? s[u] : 0.f;
+        a.pos_out[at + j] = j < m ? x[u] : -1;
+      }
+    }
   }
   if (n <= m) {
     if (tid == 0) a.count[blockIdx.x] = 0;
@@ -213,7 +251,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     if constexpr (IN_LDS)
       return s_keys[j];
     else
-      return compute(j);
+      return a.keys[at + j];
   };
   // ---- the m-th largest key: `found` holds its leading bits, `left` how many of the
   // keys that share them are still to be taken
@@ -223,15 +261,15 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
     __syncthreads();
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads * 4) {
-      uint32_t key[4];
+    for (int j0 = 0; j0 < n; j0 += kSelectThreads * kFlight) {
+      uint32_t key[kFlight];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kFlight; ++u) {
         const int j = j0 + u * kSelectThreads + tid;
         key[u] = j < n ? key_of(j) : 0;
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < kFlight; ++u) {
         const int j = j0 + u * kSelectThreads + tid;
         const bool in = j < n && (pass == 0 || (key[u] >> (shift + bits)) == found);
         const uint32_t digit = (key[u] >> shift) & ((1u << bits) - 1);
@@ -279,12 +317,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int per = (len + kHalf * kWave - 1) / (kHalf * kWave) * kWave;
   const int j0 = min(lo + w * per, lo + len), j1 = min(j0 + per, lo + len);
   uint32_t above = 0, ties = 0;
-  for (int j = j0; j < j1; j += kWave * 4) {
-    uint32_t key[4];
+  for (int j = j0; j < j1; j += kWave * kFlight) {
+    uint32_t key[kFlight];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
+    for (int u = 0; u < kFlight; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kFlight; ++u) {
       const bool in = j + u * kWave + lane < j1;
       above += __popcll(__ballot(in && key[u] > found));
       ties += __popcll(__ballot(in && key[u] == found));
@@ -308,12 +346,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   }
   int32_t* const list = (wave < kHalf ? a.dst : a.src) + static_cast<int64_t>(blockIdx.x) * a.list_len;
   const uint64_t below = (1ull << lane) - 1;
-  for (int j = j0; j < j1; j += kWave * 4) {
-    uint32_t key[4];
+  for (int j = j0; j < j1; j += kWave * kFlight) {
+    uint32_t key[kFlight];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
+    for (int u = 0; u < kFlight; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kFlight; ++u) {
       const int x = j + u * kWave + lane;
       const bool in = x < j1;
       const uint64_t same = __ballot(in && key[u] == found);
@@ -395,11 +433,12 @@ void launch_cache_score(const ScoreArgs& a, bool f16, hipStream_t s) {
 
 int evict_list_len(int cap, int budget) { return cap > budget ? (budget < cap - budget ? budget : cap - budget) : 0; }
 
-// Workspace: a count for each (sequence, head), then the lists of sources and
-// targets, at most min(budget, cap - budget) entries each.
+// Workspace: a count for each (sequence, head), the lists of sources and
+// targets, at most min(budget, cap - budget) entries each, and the keys where
+// they do not fit LDS.
 size_t evict_workspace_bytes(int B, int Hkv, int cap, int budget) {
   const size_t heads = static_cast<size_t>(B) * Hkv, len = evict_list_len(cap, budget);
-  return ((heads + 3) / 4 * 4 + 2 * heads * len) * sizeof(int32_t);
+  return ((heads + 3) / 4 * 4 + 2 * heads * len + (cap > kLdsSlots ? heads * cap : 0)) * sizeof(int32_t);
 }
 
 void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s) {
@@ -408,10 +447,13 @@ void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s) {
   a.count = static_cast<int32_t*>(ws);
   a.src = a.count + (heads + 3) / 4 * 4;
   a.dst = a.src + heads * a.list_len;
-  if (a.cap <= kLdsSlots)
+  a.keys = reinterpret_cast<uint32_t*>(a.dst + heads * a.list_len);
+  if (a.cap <= kLdsSlots) {
     hipLaunchKernelGGL(evict_select_kernel<true>, dim3(heads), dim3(kSelectThreads), a.cap * sizeof(uint32_t), s, a);
-  else
+  } else {
+    hipLaunchKernelGGL(evict_keys_kernel, dim3(heads * ((a.cap + 1023) / 1024)), dim3(256), 0, s, a);
     hipLaunchKernelGGL(evict_select_kernel<false>, dim3(heads), dim3(kSelectThreads), 0, s, a);
+  }
   if (a.list_len > 0) {
     const int runs = (a.list_len + kMoveRows - 1) / kMoveRows;
     hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(256), 0, s, a);
