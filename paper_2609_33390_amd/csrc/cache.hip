@@ -163,10 +163,19 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs a, in
 }
 
 // ---------------------------------------------------------------------------
-// Eviction.  One workgroup a (sequence, head) finds the budget-th largest key
-// by three histogram passes (11 + 11 + 10 bits), then lists the kept slots at
-// or above the budget and the evicted ones below it, both ascending; a second
-// launch moves the rows.
+// Eviction.  The budget-th largest key is found by three histogram passes (11 +
+// 11 + 10 bits); then the evicted slots below the budget and the kept ones at
+// or above it are listed, and a last launch moves the rows.  A slot's place in
+// a list follows from the number of kept slots before it: the hole at slot j is
+// number j - kept(j), and a mover at slot j has budget - kept(j) kept slots
+// from it on, itself included (the list of movers runs backwards).
+//
+// Caches of up to 32768 slots are selected by one workgroup each, with the keys
+// in LDS (one launch; 64 x 8 heads of 4100 slots: 20 us).  One workgroup is bound
+// by its own instructions beyond that (120000 slots: 130 us), so longer caches are
+// cut into chunks, each with a workgroup and a histogram of its own; every
+// workgroup adds the histograms up for itself, which also tells it how many keys
+// lie above and at the wanted one in the chunks before its own.
 // ---------------------------------------------------------------------------
 // Slots in the order of eviction's choice as unsigned integers: the latest
 // tokens first, then larger scores; NaN lowest, -0 as +0.
@@ -179,143 +188,93 @@ __device__ __forceinline__ uint32_t keep_key(float score, bool late) {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave, kBins = 2048;
 constexpr int kLdsSlots = 32768;  // keys of a workgroup that fit in LDS beside the histogram
+constexpr int kPasses = 3;
+constexpr int kShift[kPasses] = {21, 10, 0}, kBits[kPasses] = {11, 11, 10};
 
-// The keys of sequences too long for LDS, and the outputs as they are before
-// any slot moves: many workgroups, where the selection below has one a head.
-__global__ __launch_bounds__(256) void evict_keys_kernel(EvictArgs a) {
-  const int heads = a.B * a.Hkv, bh = blockIdx.x % heads, b = bh / a.Hkv;
-  const int n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift)), m = min(n, a.budget);
-  const int64_t at = static_cast<int64_t>(bh) * a.cap;
-  const int from = a.next_pos[b] - a.recent;
-  const int j0 = blockIdx.x / heads * 1024 + threadIdx.x;
-  float s[4];
-  int x[4];
+struct SelectShared {
+  uint32_t hist[kBins];
+  uint32_t wave[2][kSelectWaves];
+  uint32_t digit, left;
+};
+
+// Adds a wavefront's keys to the histogram.  The keys that share the first
+// one's digit are added at once: scores are often all alike.
+__device__ __forceinline__ void count_digit(uint32_t* hist, uint32_t digit, bool in) {
+  const uint64_t active = __ballot(in);
+  if (!active) return;
+  const int leader = __builtin_ctzll(active);
+  const uint32_t one = __builtin_amdgcn_readlane(digit, leader);
+  const uint64_t same = __ballot(in && digit == one);
+  if (static_cast<int>(threadIdx.x & 63) == leader) atomicAdd(&hist[one], static_cast<uint32_t>(__popcll(same)));
+  if (in && digit != one) atomicAdd(&hist[digit], 1u);
+}
+
+__device__ __forceinline__ bool shares_prefix(uint32_t key, int pass, uint32_t found) {
+  return pass == 0 || (key >> (kShift[pass] + kBits[pass])) == found;
+}
+__device__ __forceinline__ uint32_t digit_of(uint32_t key, int pass) {
+  return (key >> kShift[pass]) & ((1u << kBits[pass]) - 1);
+}
+
+// The bin in which the count from the top reaches `left`, and what is left to
+// be taken in it, into sh.digit and sh.left.  Thread t brings the counts of
+// bins kBins - 1 - 2 t (c0) and the one below it (c1).
+__device__ __forceinline__ void find_digit(SelectShared& sh, uint32_t c0, uint32_t c1, uint32_t left) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = kBins - 1 - 2 * tid;
+  uint32_t run = c0 + c1;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = min(j0 + u * 256, a.cap - 1);
-    s[u] = a.score_in[at + j];
-    x[u] = a.pos_in[at + j];
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(run, off, kWave);
+    if (lane >= off) run += o;
   }
+  if (lane == 63) sh.wave[0][wave] = run;
+  __syncthreads();
+  uint32_t before = run - c0 - c1;
+  for (int w = 0; w < wave; ++w) before += sh.wave[0][w];
+  if (before < left && before + c0 >= left) {
+    sh.digit = hi;
+    sh.left = left - before;
+  } else if (before + c0 < left && before + c0 + c1 >= left) {
+    sh.digit = hi - 1;
+    sh.left = left - before - c0;
+  }
+  __syncthreads();
+}
+
+// Lists the slots [j0, j1) of one wavefront, in order: `above` and `ties` are
+// the keys above and at `found` before j0, `left` the ties to be kept.
+template <int kFlight, class KeyOf>
+__device__ __forceinline__ void list_slots(const EvictArgs& a, int head, int m, int j0, int j1, uint32_t found,
+                                           uint32_t left, uint32_t above, uint32_t ties, KeyOf key_of) {
+  const int lane = threadIdx.x & 63;
+  int32_t* const src = a.src + static_cast<int64_t>(head) * a.list_len;
+  int32_t* const dst = a.dst + static_cast<int64_t>(head) * a.list_len;
+  const uint64_t below = (1ull << lane) - 1;
+  for (int j = j0; j < j1; j += kWave * kFlight) {
+    uint32_t key[kFlight];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = j0 + u * 256;
-    if (j >= a.cap) break;
-    a.keys[at + j] = keep_key(s[u], x[u] >= from);
-    a.score_out[at + j] = j < m ? s[u] : 0.f;
-    a.pos_out[at + j] = j < m ? x[u] : -1;
+    for (int u = 0; u < kFlight; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) {
+      const int x = j + u * kWave + lane;
+      const bool in = x < j1;
+      const uint64_t more = __ballot(in && key[u] > found), same = __ballot(in && key[u] == found);
+      const uint32_t tie = ties + __popcll(same & below);
+      const int kept = above + __popcll(more & below) + min(tie, left);  // slots kept before this one
+      const bool keep = key[u] > found || (key[u] == found && tie < left);
+      if (in && x < m && !keep) dst[x - kept] = x;
+      if (in && x >= m && keep) src[m - kept - 1] = x;
+      if (in && x == m) a.count[head] = m - kept;
+      above += __popcll(more);
+      ties += __popcll(same);
+    }
   }
 }
 
-// IN_LDS: the keys of a sequence are computed here and held in LDS; otherwise
-// evict_keys_kernel left them in memory, and each pass keeps more of them in flight.
-template <bool IN_LDS>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  extern __shared__ uint32_t s_keys[];
-  __shared__ uint32_t s_hist[kBins];
-  __shared__ uint32_t s_wave[2][kSelectWaves];
-  __shared__ uint32_t s_digit, s_left;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = blockIdx.x / a.Hkv, n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift));
-  const int m = min(n, a.budget);
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * a.cap;
-  const float* const score = a.score_in + at;
-  const int32_t* const pos = a.pos_in + at;
-  constexpr int kFlight = IN_LDS ? 4 : 16;
-  if (tid == 0 && blockIdx.x % a.Hkv == 0) a.new_len[b] = m;
-  if constexpr (IN_LDS) {
-    const int from = a.next_pos[b] - a.recent;
-    for (int j0 = tid; j0 < a.cap; j0 += kSelectThreads * 4) {
-      float s[4];
-      int x[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int j = min(j0 + u * kSelectThreads, a.cap - 1);
-        s[u] = score[j];
-        x[u] = pos[j];
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int j = j0 + u * kSelectThreads;
-        if (j >= a.cap) break;
-        s_keys[j] = keep_key(s[u], x[u] >= from);
-        a.score_out[at + j] = j < m ? s[u] : 0.f;
-        a.pos_out[at + j] = j < m ? x[u] : -1;
-      }
-    }
-  }
-  if (n <= m) {
-    if (tid == 0) a.count[blockIdx.x] = 0;
-    return;
-  }
-  auto key_of = [&](int j) {
-    if constexpr (IN_LDS)
-      return s_keys[j];
-    else
-      return a.keys[at + j];
-  };
-  // ---- the m-th largest key: `found` holds its leading bits, `left` how many of the
-  // keys that share them are still to be taken
-  uint32_t found = 0, left = m;
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
-    __syncthreads();
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads * kFlight) {
-      uint32_t key[kFlight];
-#pragma unroll
-      for (int u = 0; u < kFlight; ++u) {
-        const int j = j0 + u * kSelectThreads + tid;
-        key[u] = j < n ? key_of(j) : 0;
-      }
-#pragma unroll
-      for (int u = 0; u < kFlight; ++u) {
-        const int j = j0 + u * kSelectThreads + tid;
-        const bool in = j < n && (pass == 0 || (key[u] >> (shift + bits)) == found);
-        const uint32_t digit = (key[u] >> shift) & ((1u << bits) - 1);
-        // equal digits of a whole wavefront (scores that are all alike) are added at once
-        const uint64_t active = __ballot(in);
-        if (!active) continue;
-        const uint32_t one = __builtin_amdgcn_readlane(digit, __builtin_ctzll(active));
-        if (__ballot(in && digit == one) == active) {
-          if (lane == 0) atomicAdd(&s_hist[one], static_cast<uint32_t>(__popcll(active)));
-        } else if (in) {
-          atomicAdd(&s_hist[digit], 1u);
-        }
-      }
-    }
-    __syncthreads();
-    // the bin where the count from above reaches `left`: each thread sums two bins
-    // (descending), wavefronts scan, then the one bin that crosses writes
-    const int hi = kBins - 1 - 2 * tid;
-    const uint32_t c0 = s_hist[hi], c1 = s_hist[hi - 1];
-    uint32_t run = c0 + c1;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const uint32_t o = __shfl_up(run, off, kWave);
-      if (lane >= off) run += o;
-    }
-    if (lane == 63) s_wave[0][wave] = run;
-    __syncthreads();
-    uint32_t before = run - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += s_wave[0][w];
-    if (before < left && before + c0 >= left) {
-      s_digit = hi;
-      s_left = left - before;
-    } else if (before + c0 < left && before + c0 + c1 >= left) {
-      s_digit = hi - 1;
-      s_left = left - before - c0;
-    }
-    __syncthreads();
-    found = (found << bits) | s_digit;
-    left = s_left;
-    __syncthreads();
-  }
-  // ---- the first half of the wavefronts take [0, m), the others [m, n), each a run of slots
-  constexpr int kHalf = kSelectWaves / 2;
-  const int w = wave % kHalf, lo = wave < kHalf ? 0 : m, len = wave < kHalf ? m : n - m;
-  const int per = (len + kHalf * kWave - 1) / (kHalf * kWave) * kWave;
-  const int j0 = min(lo + w * per, lo + len), j1 = min(j0 + per, lo + len);
+// How many keys of [j0, j1) lie above and at `found`, for the whole wavefront.
+template <int kFlight, class KeyOf>
+__device__ __forceinline__ uint2 count_slots(int j0, int j1, uint32_t found, KeyOf key_of) {
+  const int lane = threadIdx.x & 63;
   uint32_t above = 0, ties = 0;
   for (int j = j0; j < j1; j += kWave * kFlight) {
     uint32_t key[kFlight];
@@ -328,41 +287,186 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
       ties += __popcll(__ballot(in && key[u] == found));
     }
   }
+  return make_uint2(above, ties);
+}
+
+// The outputs as they are before any slot moves, and the keys: loads of four slots
+// a thread in flight.
+template <class Store>
+__device__ __forceinline__ void start_outputs(const EvictArgs& a, int64_t at, int n, int m, int from, int j0, int end,
+                                              int stride, Store store_key) {
+  for (int j = j0; j < end; j += stride * 4) {
+    float s[4];
+    int x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = min(j + u * stride, a.cap - 1);
+      s[u] = a.score_in[at + i];
+      x[u] = a.pos_in[at + i];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = j + u * stride;
+      if (i >= end) break;
+      if (i < n) store_key(i, keep_key(s[u], x[u] >= from));
+      a.score_out[at + i] = i < m ? s[u] : 0.f;
+      a.pos_out[at + i] = i < m ? x[u] : -1;
+    }
+  }
+}
+
+// One workgroup a (sequence, head), keys in LDS.
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+  extern __shared__ uint32_t s_keys[];
+  __shared__ SelectShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.x, b = head / a.Hkv, n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift));
+  const int m = min(n, a.budget);
+  if (tid == 0 && head % a.Hkv == 0) a.new_len[b] = m;
+  start_outputs(a, static_cast<int64_t>(head) * a.cap, n, m, a.next_pos[b] - a.recent, tid, a.cap, kSelectThreads,
+                [&](int j, uint32_t key) { s_keys[j] = key; });
+  if (n <= m) {
+    if (tid == 0) a.count[head] = 0;
+    return;
+  }
+  uint32_t found = 0, left = m;
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+    for (int i = tid; i < kBins; i += kSelectThreads) sh.hist[i] = 0;
+    __syncthreads();
+    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
+      const int j = j0 + tid;
+      const uint32_t key = j < n ? s_keys[j] : 0;
+      count_digit(sh.hist, digit_of(key, pass), j < n && shares_prefix(key, pass, found));
+    }
+    __syncthreads();
+    find_digit(sh, sh.hist[kBins - 1 - 2 * tid], sh.hist[kBins - 2 - 2 * tid], left);
+    found = (found << kBits[pass]) | sh.digit;
+    left = sh.left;
+    __syncthreads();
+  }
+  // a run of slots for each wavefront
+  const int per = (n + kSelectThreads - 1) / kSelectThreads * kWave, j0 = min(wave * per, n), j1 = min(j0 + per, n);
+  auto key_of = [&](int j) { return s_keys[j]; };
+  const uint2 mine = count_slots<4>(j0, j1, found, key_of);
   if (lane == 0) {
-    s_wave[0][wave] = above;
-    s_wave[1][wave] = ties;
+    sh.wave[0][wave] = mine.x;
+    sh.wave[1][wave] = mine.y;
   }
   __syncthreads();
-  uint32_t tie = 0, rank = 0;  // ties, and listed slots of this half, in the runs before
-  for (int x = 0; x < wave; ++x) {
-    const uint32_t taken = min(s_wave[1][x], left > tie ? left - tie : 0u);
-    if (x / kHalf == wave / kHalf) {
-      const int l0 = x < kHalf ? 0 : m, ln = x < kHalf ? m : n - m;
-      const int a0 = min(l0 + x % kHalf * per, l0 + ln), a1 = min(a0 + per, l0 + ln);
-      const uint32_t kept = s_wave[0][x] + taken;
-      rank += x < kHalf ? (a1 - a0) - kept : kept;
-    }
-    tie += s_wave[1][x];
+  uint32_t above = 0, ties = 0;
+  for (int w = 0; w < wave; ++w) {
+    above += sh.wave[0][w];
+    ties += sh.wave[1][w];
   }
-  int32_t* const list = (wave < kHalf ? a.dst : a.src) + static_cast<int64_t>(blockIdx.x) * a.list_len;
-  const uint64_t below = (1ull << lane) - 1;
-  for (int j = j0; j < j1; j += kWave * kFlight) {
-    uint32_t key[kFlight];
+  list_slots<4>(a, head, m, j0, j1, found, left, above, ties, key_of);
+}
+
+// Chunks of a long cache: at most 64, so that adding up their histograms stays
+// short, and of at least 4096 slots.
+int evict_chunk(int cap) { return max(4096, ((cap + 63) / 64 + 4095) / 4096 * 4096); }
+int evict_chunks(int cap) { return (cap + evict_chunk(cap) - 1) / evict_chunk(cap); }
+
+// What the passes over a long cache know of it so far.
+struct ChunkState { uint32_t found, left, above; };  // above: keys above `found`'s digits in the chunks before
+
+// Pass 0 starts the outputs, writes the keys and counts their first digit; pass
+// 1 and 2 count the next ones; pass 3 lists.
+template <int PASS>
+__global__ __launch_bounds__(kSelectThreads) void evict_chunk_kernel(EvictArgs a, int chunk, int chunks, uint32_t* keys,
+                                                                     uint32_t* hists, ChunkState* states) {
+  __shared__ SelectShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int heads = a.B * a.Hkv, head = blockIdx.x % heads, mine = blockIdx.x / heads, b = head / a.Hkv;
+  const int n = kv_len(a.kv, b, min(a.cap, a.kv.max_pages << a.kv.page_shift)), m = min(n, a.budget);
+  const int begin = mine * chunk, end = min(begin + chunk, a.cap);
+  uint32_t* const key = keys + static_cast<int64_t>(head) * a.cap;
+  auto hist_of = [&](int pass) { return hists + (static_cast<int64_t>(pass) * heads + head) * chunks * kBins; };
+  if constexpr (PASS == 0) {
+    if (tid == 0 && mine == 0) {
+      if (head % a.Hkv == 0) a.new_len[b] = m;
+      if (n <= m) a.count[head] = 0;
+    }
+    for (int i = tid; i < kBins; i += kSelectThreads) sh.hist[i] = 0;
+    __syncthreads();
+    start_outputs(a, static_cast<int64_t>(head) * a.cap, n, m, a.next_pos[b] - a.recent, begin + tid, end, kSelectThreads,
+                  [&](int j, uint32_t k) {
+                    key[j] = k;
+                    count_digit(sh.hist, digit_of(k, 0), true);
+                  });
+    if (n <= m) return;
+  } else {
+    if (n <= m) return;
+    ChunkState st = {0, static_cast<uint32_t>(m), 0};
+    if constexpr (PASS > 1) st = states[(static_cast<int64_t>(PASS - 2) * heads + head) * chunks + mine];
+    // the histograms of the pass before, all of them and those of the chunks before this one
+    const uint2* h = reinterpret_cast<const uint2*>(hist_of(PASS - 1)) + (kBins / 2 - 1 - tid);
+    uint32_t c0 = 0, c1 = 0, p0 = 0, p1 = 0;
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c) {
+      const uint2 x = h[c * (kBins / 2)];
+      c0 += x.y;
+      c1 += x.x;
+      p0 += c < mine ? x.y : 0;
+      p1 += c < mine ? x.x : 0;
+    }
+    find_digit(sh, c0, c1, st.left);
+    const uint32_t digit = sh.digit, hi = kBins - 1 - 2 * tid;
+    st.found = (st.found << kBits[PASS - 1]) | digit;
+    st.left = sh.left;
+    uint32_t up = (hi > digit ? p0 : 0) + (hi - 1 > digit ? p1 : 0), tie = hi == digit ? p0 : hi - 1 == digit ? p1 : 0;
 #pragma unroll
-    for (int u = 0; u < kFlight; ++u) key[u] = j + u * kWave + lane < j1 ? key_of(j + u * kWave + lane) : 0;
+    for (int off = 32; off >= 1; off >>= 1) {
+      up += __shfl_xor(up, off, kWave);
+      tie += __shfl_xor(tie, off, kWave);
+    }
+    if (lane == 0) {
+      sh.wave[0][wave] = up;
+      sh.wave[1][wave] = tie;
+    }
+    if constexpr (PASS < kPasses)
+      for (int i = tid; i < kBins; i += kSelectThreads) sh.hist[i] = 0;
+    __syncthreads();
+    uint32_t ties = 0;
+    for (int w = 0; w < kSelectWaves; ++w) {
+      st.above += sh.wave[0][w];
+      ties += sh.wave[1][w];
+    }
+    const int last = min(end, n);
+    if constexpr (PASS < kPasses) {
+      if (tid == 0) states[(static_cast<int64_t>(PASS - 1) * heads + head) * chunks + mine] = st;
+      for (int j0 = begin; j0 < last; j0 += kSelectThreads * 4) {
+        uint32_t k[4];
 #pragma unroll
-    for (int u = 0; u < kFlight; ++u) {
-      const int x = j + u * kWave + lane;
-      const bool in = x < j1;
-      const uint64_t same = __ballot(in && key[u] == found);
-      const bool kept = key[u] > found || (key[u] == found && tie + __popcll(same & below) < left);
-      const uint64_t listed = __ballot(in && kept == (wave >= kHalf));
-      if (in && kept == (wave >= kHalf)) list[rank + __popcll(listed & below)] = x;
-      tie += __popcll(same);
-      rank += __popcll(listed);
+        for (int u = 0; u < 4; ++u) k[u] = key[min(j0 + u * kSelectThreads + tid, last - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          count_digit(sh.hist, digit_of(k[u], PASS),
+                      j0 + u * kSelectThreads + tid < last && shares_prefix(k[u], PASS, st.found));
+      }
+    } else {
+      const int per = (max(last - begin, 0) + kSelectThreads - 1) / kSelectThreads * kWave;
+      const int j0 = min(begin + wave * per, last), j1 = min(j0 + per, last);
+      auto key_of = [&](int j) { return key[j]; };
+      __syncthreads();
+      const uint2 c = count_slots<4>(j0, j1, st.found, key_of);
+      if (lane == 0) {
+        sh.wave[0][wave] = c.x;
+        sh.wave[1][wave] = c.y;
+      }
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) {
+        st.above += sh.wave[0][w];
+        ties += sh.wave[1][w];
+      }
+      list_slots<4>(a, head, m, j0, j1, st.found, st.left, st.above, ties, key_of);
     }
   }
-  if (wave == kSelectWaves - 1 && lane == 0) a.count[blockIdx.x] = rank;
+  if constexpr (PASS < kPasses) {
+    __syncthreads();
+    uint32_t* const out = hist_of(PASS) + static_cast<int64_t>(mine) * kBins;
+    for (int i = tid; i < kBins; i += kSelectThreads) out[i] = sh.hist[i];
+  }
 }
 
 // Moves listed rows, 16 lanes a row and kRowsInFlight rows at once.
@@ -374,11 +478,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int64_t at = static_cast<int64_t>(bh) * a.cap, list = static_cast<int64_t>(bh) * a.list_len;
   const int lane = threadIdx.x & 15, e = min(lane * 8, a.D - 8);  // narrow heads: the last lanes repeat a chunk
-  int src[kRowsInFlight], dst[kRowsInFlight];
+  int src[kRowsInFlight], dst[kRowsInFlight];  // the movers' list runs backwards
 #pragma unroll
   for (int u = 0; u < kRowsInFlight; ++u) {
     const int r = min(r0 + u * 16 + static_cast<int>(threadIdx.x >> 4), count - 1);  // past the end: the last row again
-    src[u] = a.src[list + r];
+    src[u] = a.src[list + count - 1 - r];
     dst[u] = a.dst[list + r];
   }
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -434,28 +538,51 @@ void launch_cache_score(const ScoreArgs& a, bool f16, hipStream_t s) {
 int evict_list_len(int cap, int budget) { return cap > budget ? (budget < cap - budget ? budget : cap - budget) : 0; }
 
 // Workspace: a count for each (sequence, head), the lists of sources and
-// targets, at most min(budget, cap - budget) entries each, and the keys where
-// they do not fit LDS.
+// targets, at most min(budget, cap - budget) entries each; for long caches the
+// keys, and a histogram of each pass and a state of each chunk.
+namespace {
+struct EvictSpace {
+  size_t count, lists, keys, hists, states, words;
+  EvictSpace(int B, int Hkv, int cap, int budget) {
+    const size_t heads = static_cast<size_t>(B) * Hkv, chunks = cap > kLdsSlots ? evict_chunks(cap) : 0;
+    auto even = [](size_t x) { return (x + 3) / 4 * 4; };
+    count = 0;
+    lists = even(heads);
+    keys = lists + even(2 * heads * evict_list_len(cap, budget));
+    hists = keys + (chunks ? even(heads * cap) : 0);
+    states = hists + kPasses * heads * chunks * kBins;
+    words = states + 2 * heads * chunks * (sizeof(ChunkState) / sizeof(uint32_t));
+  }
+};
+}  // namespace
+
 size_t evict_workspace_bytes(int B, int Hkv, int cap, int budget) {
-  const size_t heads = static_cast<size_t>(B) * Hkv, len = evict_list_len(cap, budget);
-  return ((heads + 3) / 4 * 4 + 2 * heads * len + (cap > kLdsSlots ? heads * cap : 0)) * sizeof(int32_t);
+  return EvictSpace(B, Hkv, cap, budget).words * sizeof(uint32_t);
 }
 
 void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s) {
-  const size_t heads = static_cast<size_t>(a.B) * a.Hkv;
+  const uint32_t heads = static_cast<uint32_t>(a.B) * a.Hkv;
+  const EvictSpace at(a.B, a.Hkv, a.cap, a.budget);
   a.list_len = evict_list_len(a.cap, a.budget);
-  a.count = static_cast<int32_t*>(ws);
-  a.src = a.count + (heads + 3) / 4 * 4;
-  a.dst = a.src + heads * a.list_len;
-  a.keys = reinterpret_cast<uint32_t*>(a.dst + heads * a.list_len);
+  a.count = static_cast<int32_t*>(ws) + at.count;
+  a.src = static_cast<int32_t*>(ws) + at.lists;
+  a.dst = a.src + static_cast<size_t>(heads) * a.list_len;
   if (a.cap <= kLdsSlots) {
-    hipLaunchKernelGGL(evict_select_kernel<true>, dim3(heads), dim3(kSelectThreads), a.cap * sizeof(uint32_t), s, a);
+    hipLaunchKernelGGL(evict_select_kernel, dim3(heads), dim3(kSelectThreads), a.cap * sizeof(uint32_t), s, a);
   } else {
-    hipLaunchKernelGGL(evict_keys_kernel, dim3(heads * ((a.cap + 1023) / 1024)), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(evict_select_kernel<false>, dim3(heads), dim3(kSelectThreads), 0, s, a);
+    uint32_t* const words = static_cast<uint32_t*>(ws);
+    const int chunks = evict_chunks(a.cap);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(heads * chunks), dim3(kSelectThreads), 0, s, a, evict_chunk(a.cap), chunks,
+                         words + at.keys, words + at.hists, reinterpret_cast<ChunkState*>(words + at.states));
+    };
+    go(evict_chunk_kernel<0>);
+    go(evict_chunk_kernel<1>);
+    go(evict_chunk_kernel<2>);
+    go(evict_chunk_kernel<3>);
   }
   if (a.list_len > 0) {
-    const int runs = (a.list_len + kMoveRows - 1) / kMoveRows;
+    const uint32_t runs = (a.list_len + kMoveRows - 1) / kMoveRows;
     hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(256), 0, s, a);
   }
 }

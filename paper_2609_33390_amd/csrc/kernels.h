@@ -125,7 +125,6 @@ struct EvictArgs {
   int32_t* pos_out;
   int32_t* new_len;
   int32_t *count, *src, *dst;                      // in the workspace, set by the launcher
-  uint32_t* keys;
   int B, Hkv, D, cap, budget, recent, list_len;
 };
 int evict_list_len(int cap, int budget);
