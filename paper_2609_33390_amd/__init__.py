@@ -32,6 +32,7 @@ Around the step, on a :class:`KVCache` of paged keys and values:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 from typing import Dict, Optional, Tuple
@@ -94,6 +95,8 @@ _lib_lock = threading.Lock()
 def lib() -> ctypes.CDLL:
     """The loaded library; raises if it has not been built."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lib_lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -199,6 +202,9 @@ def _dev_tensor(t: torch.Tensor, name: str, dtype: torch.dtype, ndim: Optional[i
     dimension count or exact shape, contiguity, a HIP device, and (when
     ``device`` is given) the same device as the call's other tensors.  A
     wrong shape would otherwise let a kernel read or write past the buffer."""
+    if (shape is not None and device is not None and type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
+            and t.device == device and device.type == "cuda" and t.is_contiguous()):
+        return                                     # nothing to object to: most calls end here
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
@@ -237,8 +243,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it, where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_ptr(device: torch.device, stream) -> Optional[int]:
     if stream is None:
+        if _raw_stream is not None and device.index is not None:
+            return _raw_stream(device.index)
         stream = torch.cuda.current_stream(device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -756,6 +768,7 @@ class KVCache:
         page, slot, head, _ = k_pages.stride()
         self._c = _KVCacheC(_HALF[self.dtype], self.n_kv_heads, self.d_head, self.page_size, n_pages, max_pages, page,
                             slot, head, _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(seq_len))
+        self._ref = ctypes.byref(self._c)
 
     @property
     def c_struct(self) -> _KVCacheC:
@@ -829,7 +842,7 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
     need = block_attention_workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
     if workspace is None:
         workspace = _workspace(dev, need, "attention")
-    st = lib().brisk_block_attention(ctypes.byref(cache.c_struct), None if pre is None else ctypes.byref(pre), _ptr(q),
+    st = lib().brisk_block_attention(cache._ref, None if pre is None else ctypes.byref(pre), _ptr(q),
                                      row, head, _ptr(block_mask), B, L, H, most, D ** -0.5 if scale is None else scale,
                                      _ptr(out), _ptr(lse), _ptr(workspace), _ws_bytes(workspace, dev, need),
                                      _stream_ptr(dev, stream))
@@ -837,6 +850,7 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
     return out, lse
 
 
+@functools.lru_cache(maxsize=1024)
 def block_attention_workspace_size(B: int, L: int, n_heads: int, n_kv_heads: int, d_head: int, prefix_len: int,
                                    max_seq_len: int) -> int:
     out = _sz()
@@ -863,7 +877,7 @@ def cache_score(q: torch.Tensor, lse: torch.Tensor, cache: KVCache, score: torch
         out = torch.empty_like(score)
     else:
         _dev_tensor(out, "out", torch.float32, shape=shape, device=dev)
-    st = lib().brisk_cache_score(ctypes.byref(cache.c_struct), _ptr(q), row, head, _ptr(block_mask), _ptr(lse), B, L, H,
+    st = lib().brisk_cache_score(cache._ref, _ptr(q), row, head, _ptr(block_mask), _ptr(lse), B, L, H,
                                  cache.d_head ** -0.5 if scale is None else scale, decay, _ptr(score), _ptr(out), cap,
                                  _stream_ptr(dev, stream))
     _check(st, "brisk_cache_score")
@@ -897,16 +911,22 @@ def cache_evict(cache: KVCache, score: torch.Tensor, pos: torch.Tensor, next_pos
     _dev_tensor(new_len, "new_len", torch.int32, shape=(cache.B,), device=dev)
     if _overlap(score, score_out) or _overlap(pos, pos_out):
         raise ValueError("score_out and pos_out must not overlap score and pos")
-    nbytes = _sz()
-    _check(lib().brisk_cache_evict_workspace_size(cache.B, cache.n_kv_heads, cap, budget, ctypes.byref(nbytes)),
-           "brisk_cache_evict_workspace_size")
+    need = _evict_workspace_size(cache.B, cache.n_kv_heads, cap, budget)
     if workspace is None:
-        workspace = _workspace(dev, nbytes.value, "evict")
-    st = lib().brisk_cache_evict(ctypes.byref(cache.c_struct), cache.B, _ptr(score), _ptr(pos), cap, _ptr(next_pos),
+        workspace = _workspace(dev, need, "evict")
+    st = lib().brisk_cache_evict(cache._ref, cache.B, _ptr(score), _ptr(pos), cap, _ptr(next_pos),
                                  budget, recent, _ptr(score_out), _ptr(pos_out), _ptr(new_len), _ptr(workspace),
-                                 _ws_bytes(workspace, dev, nbytes.value), _stream_ptr(dev, stream))
+                                 _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
     _check(st, "brisk_cache_evict")
     return score_out, pos_out, new_len
+
+
+@functools.lru_cache(maxsize=1024)
+def _evict_workspace_size(B: int, n_kv_heads: int, cap: int, budget: int) -> int:
+    out = _sz()
+    _check(lib().brisk_cache_evict_workspace_size(B, n_kv_heads, cap, budget, ctypes.byref(out)),
+           "brisk_cache_evict_workspace_size")
+    return out.value
 
 
 def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
@@ -917,6 +937,9 @@ def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
 
 def _prob_rows(t: torch.Tensor, name: str, shape: Tuple[int, ...], device: torch.device) -> int:
     """Row stride of fp32 rows [..., V] that may be spaced wider than V."""
+    if (type(t) is torch.Tensor and t.dtype is torch.float32 and t.shape == shape and t.device == device
+            and t.is_contiguous()):
+        return shape[-1]
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != torch.float32:
@@ -932,6 +955,13 @@ def _prob_rows(t: torch.Tensor, name: str, shape: Tuple[int, ...], device: torch
     if shape[0] > 1 and shape[1] > 1 and t.stride(0) != shape[1] * t.stride(1):
         raise ValueError(f"the rows of {name} must be evenly spaced: stride(0) == {shape[1]} * stride(1)")
     return t.stride(1) if shape[1] > 1 else t.stride(0) if shape[0] > 1 else shape[2]
+
+
+@functools.lru_cache(maxsize=1024)
+def _draft_workspace_size(B: int, V: int) -> int:
+    out = _sz()
+    _check(lib().brisk_draft_verify_workspace_size(B, V, ctypes.byref(out)), "brisk_draft_verify_workspace_size")
+    return out.value
 
 
 def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok: torch.Tensor, u_accept: torch.Tensor,
@@ -966,13 +996,12 @@ def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok:
         token = torch.empty(B, dtype=torch.int32, device=dev)
     else:
         _dev_tensor(token, "token", torch.int32, shape=(B,), device=dev)
-    nbytes = _sz()
-    _check(lib().brisk_draft_verify_workspace_size(B, V, ctypes.byref(nbytes)), "brisk_draft_verify_workspace_size")
+    need = _draft_workspace_size(B, V)
     if workspace is None:
-        workspace = _workspace(dev, nbytes.value, "draft")
+        workspace = _workspace(dev, need, "draft")
     st = lib().brisk_draft_verify(_ptr(target_prob), t_stride, _ptr(draft_prob) if L else None, d_stride,
                                   _ptr(draft_tok) if L else None, _ptr(draft_len), _ptr(u_accept) if L else None,
                                   _ptr(noise), n_stride, B, L, V, _ptr(accept_len), _ptr(token), _ptr(workspace),
-                                  _ws_bytes(workspace, dev, nbytes.value), _stream_ptr(dev, stream))
+                                  _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
     _check(st, "brisk_draft_verify")
     return accept_len, token
