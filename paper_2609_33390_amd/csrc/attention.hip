@@ -16,7 +16,6 @@
 // between the wavefront's halves, and the probabilities are already the
 // operand of out^T = V^T P^T, with the keys in an order that the transposed
 // LDS reads of V follow.
-#include <cstdlib>
 #include "half_mfma.h"
 #include "kernels.h"
 
@@ -503,7 +502,7 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 // The tile of a launch: rows, and keys of a step of the whole workgroup.
 struct TileShape { int rows, keys, slots; };  // slots: workgroups the GPU holds at once
 constexpr TileShape kShapes[] = {{32, 64, 2 * kCUs}, {64, 64, 2 * kCUs}, {128, 64, 2 * kCUs}, {256, 64, kCUs}};
-int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 || getenv("MM") ? 2 : 3; }
+int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
 
 struct CallPlan {
   AttnPlan p;
