@@ -68,8 +68,8 @@ __device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3)
 
 // ND: 32-wide slices of the head; QT: 32-row tiles a wavefront; RW wavefronts
 // of different rows share each tile of 32 * NT keys, KW groups of them take
-// alternate tiles; ST: tiles of a group in LDS, all but one of them under way.
-template <bool F16, int ND, int QT, int RW, int KW, int NT, int ST>
+// alternate tiles, one in LDS and the next one on its way.
+template <bool F16, int ND, int QT, int RW, int KW, int NT>
 __global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(AttentionArgs a, AttnPlan p) {
   constexpr int RB = ND > 2 ? 256 : 128, T = 32 * NT, NC = 2 * ND;
   constexpr int RPI = 1024 / RB;                 // rows of a wavefront's copy
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(A
   constexpr int kRows = RW * QT * 32;
   constexpr int kOutRow = ND * 32 + 4;           // floats of a row of the join
   constexpr int kJoin = KW > 1 ? KW * kRows * (kOutRow + 2) * 4 : 0;
-  constexpr int kLds = ST * kStage * KW > kJoin ? ST * kStage * KW : kJoin;
+  constexpr int kLds = 2 * kStage * KW > kJoin ? 2 * kStage * KW : kJoin;
   static_assert(T % (RPI * RW) == 0 && kLds <= 163840);
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds];
 
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(A
   // copies, and handed to the key's lanes by broadcasts inside 16-lane rows.
   const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
   const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
-  uint8_t* const lds = smem + kw * (ST * kStage);
+  uint8_t* const lds = smem + kw * (2 * kStage);
   const int held = rw * NI * RPI + held_key<RB>(lane);
   const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
   const bool whole = a.D == 32 * ND;
@@ -202,19 +202,14 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(A
     }
     const int v_end = careful ? min(key1, max(base, 0)) : key1;
     int j0 = key0 + kw * T;
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s)
-      if (s < steps) {
-        look_up(j0 + s * T * KW);
-        stage(j0 + s * T * KW, s, v_end);
-      }
-    look_up(j0 + (ST - 1) * T * KW);
-    int buf = 0;
-    for (int step = 0; step < steps; ++step, j0 += T * KW, buf = buf + 1 < ST ? buf + 1 : 0) {
-      if (step + ST - 1 <= steps)
-        copies_landed<(ST - 2) * 2 * NI>();      // this tile's; the later ones may still be under way
-      else
-        copies_landed();
+    if (steps > 0) {
+      look_up(j0);
+      stage(j0, 0, v_end);
+      look_up(j0 + T * KW);
+    }
+    for (int step = 0; step < steps; ++step, j0 += T * KW) {
+      const int buf = step & 1;
+      copies_landed();
       if constexpr (RW > 1)
         __syncthreads();
       else
@@ -237,9 +232,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(A
             kf[n][i] = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
           }
         __builtin_amdgcn_sched_barrier(0);
-        if (step + ST - 1 < steps) {
-          stage(j0 + (ST - 1) * T * KW, buf > 0 ? buf - 1 : ST - 1, v_end);
-          look_up(j0 + ST * T * KW);
+        if (step + 1 < steps) {
+          stage(j0 + T * KW, buf ^ 1, v_end);
+          look_up(j0 + 2 * T * KW);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -556,10 +551,10 @@ template <bool F16, int ND>
 void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
   const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
   switch (shape) {
-    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1, 2>), grid, dim3(128), 0, s, a, p); break;
-    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 2, 1, 2>), grid, dim3(128), 0, s, a, p); break;
-    case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2, 2>), grid, dim3(256), 0, s, a, p); break;
-    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2, 2>), grid, dim3(512), 0, s, a, p); break;
+    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
+    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
+    case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
+    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
   }
 }
 

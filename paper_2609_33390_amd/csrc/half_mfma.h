@@ -69,11 +69,9 @@ __device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
 }
 #pragma clang diagnostic pop
 
-// Waits for the wavefront's own copies, all but the N last issued.
-template <int N = 0>
+// Waits for the wavefront's own copies.
 __device__ __forceinline__ void copies_landed() {
-  static_assert(N >= 0 && N <= 63);
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | (7 << 4) | (15 << 8));  // vmcnt(N)
+  __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // vmcnt(0)
   asm volatile("" ::: "memory");
 }
 
