@@ -255,3 +255,33 @@ def test_writes_stay_inside_the_buffers(kw):
                           workspace=ws.t)
     assert out.intact() and lse.intact() and ws.intact()
     _check(c, out.t, lse.t)
+
+
+def test_binding_refuses_what_does_not_fit():
+    """Wrong types, shapes, strides and devices never reach the library."""
+    c = Case(2, 3, 4, 2, 64, 8, [10, 20], seed=17)
+    cache, q, pre = c.cache(brisk), c.q.cuda(), c.gpu_prefix()
+    call = brisk.block_attention
+    for bad, kw in ((q.cpu(), {}), (q[:1], {}), (q[..., :32], {}), (q[:, :, :, ::2], {}),
+                    (q.transpose(0, 1).contiguous().transpose(0, 1), {}), (q, dict(prefix=(pre[0], pre[1][:, :1]))),
+                    (q, dict(prefix=(pre[0], pre[1].transpose(0, 1).contiguous().transpose(0, 1)))),
+                    (q, dict(block_mask=torch.zeros(2, 4, dtype=torch.int64, device="cuda"))),
+                    (q, dict(out=torch.empty(2, 3, 4, 32, dtype=q.dtype, device="cuda"))),
+                    (q, dict(prefix=pre, workspace=torch.empty(1, dtype=torch.uint8, device="cuda")))):
+        with pytest.raises(ValueError):
+            call(bad, cache, **kw)
+    for bad, kw in ((q.half(), {}), (q, dict(prefix=(pre[0].half(), pre[1].half()))),
+                    (q, dict(block_mask=torch.zeros(2, 3, dtype=torch.int32, device="cuda"))),
+                    (q, dict(lse=torch.empty(2, 3, 4, dtype=torch.bfloat16, device="cuda")))):
+        with pytest.raises(TypeError):
+            call(bad, cache, **kw)
+    with pytest.raises(brisk.BriskError) as e:
+        call(q, cache, scale=-1.0)
+    assert e.value.status == -2
+    with pytest.raises(brisk.BriskError):
+        call(q, cache, max_seq_len=cache.max_seq_len + 1)
+    k = cache.k_pages
+    with pytest.raises(ValueError):
+        brisk.KVCache(k, k[:, :8], cache.block_table, cache.seq_len)
+    with pytest.raises(ValueError):
+        brisk.KVCache(k, k, cache.block_table, cache.seq_len[:1])

@@ -253,3 +253,25 @@ def test_attention_over_an_evicted_cache():
             want = p @ own_v[b][keep, h] / p.sum()
             tol = 2.0 ** -8 * (np.abs(want) + p @ np.abs(own_v[b][keep, h]) / p.sum()) + 1e-3
             assert (np.abs(out[b, 0, h].double().cpu().numpy() - want) <= tol).all()
+
+
+def test_binding_refuses_overlap_and_misfits():
+    e = EvictCase([40, 30], 10, 2, seed=23)
+    cache = e.c.cache(brisk)
+    s, p, n = (torch.from_numpy(x).cuda() for x in (e.score, e.pos, e.next_pos))
+    for kw in (dict(score_out=s), dict(pos_out=p), dict(score_out=s[:, :, :-1]), dict(new_len=n[:1]),
+               dict(workspace=torch.empty(4, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ValueError):
+            brisk.cache_evict(cache, s, p, n, 10, 2, **kw)
+    with pytest.raises(TypeError):
+        brisk.cache_evict(cache, s, p.long(), n, 10, 2)
+    for budget, recent in ((0, 0), (10, 11), (10, -1)):
+        with pytest.raises(brisk.BriskError):
+            brisk.cache_evict(cache, s, p, n, budget, recent)
+    q, lse = e.c.q.cuda(), torch.zeros(2, 1, 2, device="cuda")
+    with pytest.raises(ValueError):
+        brisk.cache_score(q, lse[:1], cache, s)
+    with pytest.raises(ValueError):
+        brisk.cache_score(q, lse, cache, s[:1])
+    with pytest.raises(TypeError):
+        brisk.cache_score(q, lse, cache, s.double())

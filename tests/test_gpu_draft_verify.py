@@ -158,3 +158,18 @@ def test_graph_and_guard_bands():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(acc.t, ref[0]) and torch.equal(tok.t, ref[1])
+
+
+def test_binding_refuses_what_does_not_fit():
+    rng = np.random.default_rng(6)
+    t, d, x, u, e = (torch.from_numpy(v).cuda() for v in _laws(3, 4, 50, rng))
+    call = brisk.draft_verify
+    for args in ((t[:, :4], d, x, u, e), (t, d[:, :3], x, u, e), (t, d, x, u[:2], e), (t, d, x, u, e[:, :49]),
+                 (t[..., ::2], d, x, u, e), (t.cpu(), d, x, u, e), (t[0], d, x, u, e)):
+        with pytest.raises(ValueError):
+            call(*args)
+    for args in ((t.double(), d, x, u, e), (t, d.half(), x, u, e), (t, d, x.long(), u, e)):
+        with pytest.raises(TypeError):
+            call(*args)
+    with pytest.raises(ValueError):
+        call(t, d, x, u, e, draft_len=torch.zeros(2, dtype=torch.int32, device="cuda"))
