@@ -503,14 +503,15 @@ int brisk_block_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, 
  *               the d_head contiguous elements of a row; strides multiples of 8
  *   block_mask  [B, L] uint64, nullable
  *   max_seq_len host bound of the lengths (longer ones are cut to it); 0 when
- *               no sequence holds a key
+ *               no sequence holds a key.  The split of long caches over the
+ *               GPU follows from it, so a bound near the real lengths is faster
  *   out         [B*L, n_heads, d_head], the cache's type
  *   lse         [B*L, n_heads] fp32, nullable
  *   ws          device scratch of brisk_block_attention_workspace_size bytes
  *
  * Limits: 1 <= L <= 64, B >= 1, n_heads a multiple of n_kv_heads with
  * B * L * n_heads <= 2^24, 0 <= max_seq_len <= max_pages * page_size,
- * scale > 0 and finite.  Sums, maxima and partial outputs are held in fp32;
+ * 0 < scale <= 1e30.  Sums, maxima and partial outputs are held in fp32;
  * probabilities are rounded to the cache's type where they meet the values.
  * Deterministic.
  */

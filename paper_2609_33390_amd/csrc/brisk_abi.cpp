@@ -25,6 +25,7 @@ constexpr int32_t kMaxProfileBlocks = 1 << 30;
 
 constexpr int32_t kMaxAttnRows = 1 << 24;
 constexpr int32_t kMaxSlots = 1 << 30;
+constexpr float kMaxScale = 1.0e30f;  // stays finite in base 2
 constexpr int32_t kMaxEvictCap = 1 << 24;
 constexpr int64_t kMaxScores = int64_t{1} << 36;  // slots of all sequences and heads
 // The paged cache: sizes, strides and alignment.  `view` is filled on success.
@@ -468,7 +469,7 @@ int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* pr
   st = attention_shape_check(B, L, n_heads, cache->n_kv_heads, cache->d_head, prefix_len, max_seq_len);
   if (st != BRISK_OK) return st;
   if (max_seq_len > static_cast<int64_t>(cache->max_pages) * cache->page_size || q_row_stride < 0 ||
-      q_head_stride < 0 || !(scale > 0.f) || scale > 3.0e38f ||
+      q_head_stride < 0 || !(scale > 0.f) || scale > kMaxScale ||
       (prefix && (prefix->slot_stride < 0 || prefix->head_stride < 0)))
     return BRISK_ERR_SHAPE;
   if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned16(out) ||
@@ -516,7 +517,7 @@ int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_
   st = block_rows_check(B, L, n_heads, cache->n_kv_heads);
   if (st != BRISK_OK) return st;
   if (cap < 1 || cap > kMaxSlots || static_cast<int64_t>(B) * cache->n_kv_heads * cap > kMaxScores ||
-      q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) || scale > 3.0e38f)
+      q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) || scale > kMaxScale)
     return BRISK_ERR_SHAPE;
   if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned8(block_mask) ||
       !aligned4(lse) || !aligned4(score_in) || !aligned4(score_out))

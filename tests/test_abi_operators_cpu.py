@@ -57,7 +57,8 @@ def test_cache_is_checked_by_every_call(kw, want):
     (dict(q=None), ENULL), (dict(out=None), ENULL), (dict(B=0), ESHAPE), (dict(L=0), ESHAPE), (dict(L=65), ESHAPE),
     (dict(H=0), ESHAPE), (dict(H=30), ESHAPE), (dict(B=1 << 24), ESHAPE), (dict(B=(1 << 15) + 1), ESHAPE), (dict(most=-1), ESHAPE),
     (dict(most=2049), ESHAPE), (dict(scale=0.0), ESHAPE), (dict(scale=-1.0), ESHAPE), (dict(scale=float("nan")), ESHAPE),
-    (dict(scale=float("inf")), ESHAPE), (dict(row=-8), ESHAPE), (dict(head=-8), ESHAPE), (dict(row=4100), EUNSUP),
+    (dict(scale=float("inf")), ESHAPE), (dict(scale=2e30), ESHAPE), (dict(row=-8), ESHAPE), (dict(head=-8), ESHAPE),
+    (dict(row=4100), EUNSUP),
     (dict(head=4), EUNSUP), (dict(q=ODD), EUNSUP), (dict(out=ODD), EUNSUP), (dict(lse=ODD), EUNSUP),
     (dict(mask=0x10004), EUNSUP),
 ])

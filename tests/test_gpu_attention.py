@@ -101,7 +101,9 @@ def test_largest_magnitudes():
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("what", ["k", "v", "both"])
-@pytest.mark.parametrize("shape", [dict(B=2, L=8, H=8, Hkv=2, D=128), dict(B=9, L=31, H=7, Hkv=1, D=64)])
+@pytest.mark.parametrize("shape", [dict(B=2, L=8, H=8, Hkv=2, D=128), dict(B=9, L=31, H=7, Hkv=1, D=64),
+                                   dict(B=2, L=16, H=8, Hkv=2, D=80), dict(B=2, L=31, H=4, Hkv=1, D=104),
+                                   dict(B=1, L=64, H=4, Hkv=2, D=128)])
 def test_hidden_slots_have_no_effect(bad, what, shape):
     """Block slots that a row does not see hold anything; rows that see them get it."""
     L = shape["L"]
@@ -171,8 +173,9 @@ def test_length_bound_and_table_are_clamped():
     assert (out[1] == 0).all()
 
 
-def test_zero_length_bound():
-    c = Case(2, 2, 4, 4, 64, 9, [0, 0], seed=11)
+@pytest.mark.parametrize("prefix", [9, 0, None])
+def test_zero_length_bound(prefix):
+    c = Case(2, 2, 4, 4, 64, prefix, [0, 0], seed=11)
     _check(c, *_run(c, max_seq_len=0))
 
 

@@ -189,7 +189,7 @@ def test_evict_matches_oracle(kw):
 
 
 @pytest.mark.parametrize("n,budget,kind", [(20000, 5000, "mass"), (70001, 30000, "ties"), (140000, 1000, "any"),
-                                           (40000, 39999, "equal")])
+                                           (40000, 39999, "equal"), (32700, 16000, "any"), (32764, 32000, "ties")])
 def test_evict_long_caches(n, budget, kind):
     """Lengths past what one workgroup holds on chip; the oracle's choice by one stable sort."""
     e = EvictCase([n], budget, budget // 8, Hkv=1, D=8, kind=kind, seed=n)
