@@ -70,7 +70,7 @@ __device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3)
 // of different rows share each tile of 32 * NT keys, KW groups of them take
 // alternate tiles, one in LDS and the next one on its way.
 template <bool F16, int ND, int QT, int RW, int KW, int NT>
-__global__ __launch_bounds__(64 * RW * KW, RW >= 4 ? 2 : 1) void attend_kernel(AttentionArgs a, AttnPlan p) {
+__global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(AttentionArgs a, AttnPlan p) {
   constexpr int RB = ND > 2 ? 256 : 128, T = 32 * NT, NC = 2 * ND;
   constexpr int RPI = 1024 / RB;                 // rows of a wavefront's copy
   constexpr int NI = T / RPI / RW;               // copies of K (and of V) a wavefront
@@ -552,7 +552,7 @@ void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStrea
   const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
   switch (shape) {
     case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
-    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
+    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 2, 2, 1>), grid, dim3(256), 0, s, a, p); break;
     case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
     default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
   }
