@@ -66,17 +66,20 @@ __device__ __forceinline__ float swap32_max(float v) {
 template <int RB>
 __device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; }
 
-// ND: 32-wide slices of the head; QT: 32-row tiles a wavefront; RW wavefronts
-// of different rows share each tile of 32 * NT keys, KW groups of them take
-// alternate tiles, one in LDS and the next one on its way.
-template <bool F16, int ND, int QT, int RW, int KW, int NT>
+// ND: 32-wide slices of the head.  A wavefront has 32 rows; RW wavefronts of
+// different rows share each tile of 32 * NT keys, KW groups of them take
+// alternate tiles, one in LDS and the next one on its way.  (Wavefronts of 64
+// rows read each key and value from LDS once for two products, but leave no
+// registers for a second wavefront on the SIMD: 64 caches of 16 to 2048 keys, 64
+// rows each, took 93 us that way and 82 us as two wavefronts of 32 rows.)
+template <bool F16, int ND, int RW, int KW, int NT>
 __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(AttentionArgs a, AttnPlan p) {
   constexpr int RB = ND > 2 ? 256 : 128, T = 32 * NT, NC = 2 * ND;
   constexpr int RPI = 1024 / RB;                 // rows of a wavefront's copy
   constexpr int NI = T / RPI / RW;               // copies of K (and of V) a wavefront
   constexpr int kTile = T * RB;                  // bytes of K (or V) of a tile
   constexpr int kStage = 2 * kTile;
-  constexpr int kRows = RW * QT * 32;
+  constexpr int kRows = RW * 32;
   constexpr int kOutRow = ND * 32 + 4;           // floats of a row of the join
   constexpr int kJoin = KW > 1 ? KW * kRows * (kOutRow + 2) * 4 : 0;
   constexpr int kLds = 2 * kStage * KW > kJoin ? 2 * kStage * KW : kJoin;
@@ -130,18 +133,16 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   const float c = a.scale * kLog2e;
 
   // ---- this wavefront's queries, as the second operand of K Q^T
-  uint4 q[QT][NC];
-  uint64_t words[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = (rw * QT + t) * 32 + col;
-    const int row = row0 + min(r, rows - 1), bi = row / G;
+  uint4 q[NC];
+  uint64_t word;                                 // what its row sees of the block
+  {
+    const int row = row0 + min(rw * 32 + col, rows - 1), bi = row / G;
     const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
-    words[t] = masked ? a.mask[bi] : ~0ull;
+    word = masked ? a.mask[bi] : ~0ull;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int e = 16 * i + 8 * half;
-      q[t][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
+      q[i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
     }
   }
 
@@ -184,22 +185,19 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
     });
   };
 
-  floatx16 o[QT][ND];
+  floatx16 o[ND];
   // m: the subtracted logit (unscaled); mc = c * m; l: this lane's part of the sum, zero while
   // the row has seen no key (NaN logits pass the maximum by, but not the sum)
-  float m[QT], mc[QT], l[QT];
+  float m, mc, l;
   const int steps = (key1 - key0 + T * KW - 1) / (T * KW);
 
   // The second time round only where values that some rows must not see are
   // not finite: the block's own values then join by vector arithmetic, row by row.
   for (int careful = 0;; ++careful) {
+    m = -INFINITY;
+    mc = l = 0.f;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      m[t] = -INFINITY;
-      mc[t] = l[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[t][d] = floatx16{};
-    }
+    for (int d = 0; d < ND; ++d) o[d] = floatx16{};
     const int v_end = careful ? min(key1, max(base, 0)) : key1;
     int j0 = key0 + kw * T;
     if (steps > 0) {
@@ -221,7 +219,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
       // ---- S^T = K Q^T: register r of a lane is key 8 (r / 4) + 4 half + r % 4 of each 32
       // All reads first (the fences keep the compiler from putting each one in front of
       // the product that needs it), so that the products follow each other.
-      floatx16 s[QT][NT];
+      floatx16 s[NT];
       {
         uint4 kf[NT][NC];
 #pragma unroll
@@ -239,12 +237,9 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          s[n] = floatx16{};
 #pragma unroll
-          for (int t = 0; t < QT; ++t) s[t][n] = floatx16{};
-#pragma unroll
-          for (int i = 0; i < NC; ++i)
-#pragma unroll
-            for (int t = 0; t < QT; ++t) s[t][n] = mfma32<F16>(kf[n][i], q[t][i], s[t][n]);
+          for (int i = 0; i < NC; ++i) s[n] = mfma32<F16>(kf[n][i], q[i], s[n]);
         }
       }
       // The values of 16 keys, as the first operand: 8 keys of a lane's column in the
@@ -269,93 +264,84 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int first = j0 + n * 32 + 4 * half;  // the key of this lane's first register
+          const uint32_t seen = seen32(masked ? word : ~0ull, masked ? first - base : 0, key1 - first);
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            const uint32_t seen = seen32(masked ? words[t] : ~0ull, masked ? first - base : 0, key1 - first);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[t][n][r] = (seen >> (8 * (r / 4) + r % 4)) & 1 ? s[t][n][r] : -INFINITY;
-          }
+          for (int r = 0; r < 16; ++r) s[n][r] = (seen >> (8 * (r / 4) + r % 4)) & 1 ? s[n][r] : -INFINITY;
         }
       }
       // ---- softmax statistics and P^T
-      uint4 pf[QT][2 * NT];
+      float top = s[0][0];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float top = s[t][0][0];
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+      top = swap32_max(top);
+      // The subtracted logit follows the maximum only once that is 2^8 times ahead.
+      if (__any(top * c > mc + 8.f || (m == -INFINITY && top > -INFINITY))) {
+        const float up = fmaxf(m, top);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - up) * c);
+        l *= f;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][n][r]);
-        top = swap32_max(top);
-        // The subtracted logit follows the maximum only once that is 2^8 times ahead.
-        if (__any(top * c > mc[t] + 8.f || (m[t] == -INFINITY && top > -INFINITY))) {
-          const float up = fmaxf(m[t], top);
-          const float f = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[t] - up) * c);
-          l[t] *= f;
+        for (int d = 0; d < ND; ++d) o[d] *= f;
+        m = up;
+        mc = up == -INFINITY ? 0.f : up * c;
+      }
+      // Probabilities are rounded to the cache's type here, as the products take them (their
+      // sum is of the unrounded ones): as large an error as that of rounding the output.
+      uint4 pf[2 * NT];
 #pragma unroll
-          for (int d = 0; d < ND; ++d) o[t][d] *= f;
-          m[t] = up;
-          mc[t] = up == -INFINITY ? 0.f : up * c;
+      for (int n = 0; n < NT; ++n) {
+        uint32_t w[8];
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -mc));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][r + 1], c, -mc));
+          l += p0 + p1;
+          w[r / 2] = pack2<F16>(p0, p1);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          uint32_t w[8];
-#pragma unroll
-          for (int r = 0; r < 16; r += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][n][r], c, -mc[t]));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[t][n][r + 1], c, -mc[t]));
-            l[t] += p0 + p1;
-            w[r / 2] = pack2<F16>(p0, p1);
-          }
-          pf[t][2 * n] = make_uint4(w[0], w[1], w[2], w[3]);
-          pf[t][2 * n + 1] = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+        pf[2 * n] = make_uint4(w[0], w[1], w[2], w[3]);
+        pf[2 * n + 1] = make_uint4(w[4], w[5], w[6], w[7]);
       }
       // ---- out^T += V^T P^T, 16 keys at a time, the next ones' values on the way
 #pragma unroll
       for (int g = 0; g < 2 * NT; ++g) {
         if (g + 1 < 2 * NT) values(g + 1, vf[(g + 1) & 1]);
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int t = 0; t < QT; ++t) o[t][d] = mfma32<F16>(vf[g & 1][d], pf[t][g], o[t][d]);
+        for (int d = 0; d < ND; ++d) o[d] = mfma32<F16>(vf[g & 1][d], pf[g], o[d]);
       }
       if (careful && j0 + T > base) {
+#pragma unroll 1
         for (int j = max(j0, base); j < min(j0 + T, key1); ++j) {
           const int key = j - j0;
           const uint16_t* v = reinterpret_cast<const uint16_t*>(v_src) + kv_slot(a.kv, b, j);
+          float dot = 0.f;
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            float dot = 0.f;
+          for (int i = 0; i < NC; ++i) {
+            const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
+            const uint32_t kw4[4] = {kf.x, kf.y, kf.z, kf.w};
+            uint32_t qw4[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+            // converted here, not ahead of the loop: this path is rare and the registers are not
+            asm volatile("" : "+v"(qw4[0]), "+v"(qw4[1]), "+v"(qw4[2]), "+v"(qw4[3]));
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-              const uint4 kf = *reinterpret_cast<const uint4*>(kt + key * RB + (((2 * i + half) ^ row_swizzle<RB>(key)) << 4));
-              const uint32_t kw4[4] = {kf.x, kf.y, kf.z, kf.w};
-              uint32_t qw4[4] = {q[t][i].x, q[t][i].y, q[t][i].z, q[t][i].w};
-              // converted here, not ahead of the loop: this path is rare and the registers are not
-              asm volatile("" : "+v"(qw4[0]), "+v"(qw4[1]), "+v"(qw4[2]), "+v"(qw4[3]));
+            for (int w = 0; w < 4; ++w)
+              dot += half_to_f32<F16>(kw4[w] & 0xFFFF) * half_to_f32<F16>(qw4[w] & 0xFFFF) +
+                     half_to_f32<F16>(kw4[w] >> 16) * half_to_f32<F16>(qw4[w] >> 16);
+          }
+          const float w = __builtin_amdgcn_exp2f(fmaf(swap32_sum(dot), c, -mc));
+          const bool see = block_sees(word, j - base);
 #pragma unroll
-              for (int w = 0; w < 4; ++w)
-                dot += half_to_f32<F16>(kw4[w] & 0xFFFF) * half_to_f32<F16>(qw4[w] & 0xFFFF) +
-                       half_to_f32<F16>(kw4[w] >> 16) * half_to_f32<F16>(qw4[w] >> 16);
+          for (int d = 0; d < ND; ++d) {
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+              const int e = 32 * d + 8 * (r / 4);
+              if (e >= a.D) continue;
+              const uint2 x = *reinterpret_cast<const uint2*>(v + e + 4 * half);
+              const float x4[4] = {half_to_f32<F16>(x.x & 0xFFFF), half_to_f32<F16>(x.x >> 16),
+                                   half_to_f32<F16>(x.y & 0xFFFF), half_to_f32<F16>(x.y >> 16)};
+#pragma unroll
+              for (int u = 0; u < 4; ++u) o[d][r + u] = see ? fmaf(w, x4[u], o[d][r + u]) : o[d][r + u];
             }
-            dot = swap32_sum(dot);
-            if (!block_sees(words[t], j - base)) continue;
-            const float w = __builtin_amdgcn_exp2f(fmaf(dot, c, -mc[t]));
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-#pragma unroll
-              for (int r = 0; r < 16; r += 4) {
-                const int e = 32 * d + 8 * (r / 4) + 4 * half;
-                if (e >= a.D) continue;
-                const uint2 x = *reinterpret_cast<const uint2*>(v + e);
-                o[t][d][r] = fmaf(w, half_to_f32<F16>(x.x & 0xFFFF), o[t][d][r]);
-                o[t][d][r + 1] = fmaf(w, half_to_f32<F16>(x.x >> 16), o[t][d][r + 1]);
-                o[t][d][r + 2] = fmaf(w, half_to_f32<F16>(x.y & 0xFFFF), o[t][d][r + 2]);
-                o[t][d][r + 3] = fmaf(w, half_to_f32<F16>(x.y >> 16), o[t][d][r + 3]);
-              }
-              asm volatile("" ::: "memory");  // a few loads in flight
-            }
+            asm volatile("" ::: "memory");  // a few loads in flight
           }
         }
       }
@@ -363,15 +349,12 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
     if (!masked || careful) break;
     bool odd = false;
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) odd |= !(fabsf(o[t][d][r]) < INFINITY);
+      for (int r = 0; r < 16; ++r) odd |= !(fabsf(o[d][r]) < INFINITY);
     if (!__syncthreads_or(odd)) break;
   }
-#pragma unroll
-  for (int t = 0; t < QT; ++t) l[t] = swap32_sum(l[t]);
+  l = swap32_sum(l);
 
   // ---- join the key groups and write
   auto put = [&](int row, int e, float4 x) {  // elements e..e+3 of a row's normalised sum
@@ -390,38 +373,31 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
       a.lse[out] = x;
   };
   if constexpr (KW == 1) {
+    const int r0 = rw * 32 + col;
+    if (r0 >= rows) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (half == 0) put_lse(row0 + r0, l == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * kLn2);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const int r0 = (rw * QT + t) * 32 + col;
-      if (r0 >= rows) continue;
-      const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];
-      if (half == 0) put_lse(row0 + r0, l[t] == 0.f ? -INFINITY : (mc[t] + __builtin_amdgcn_logf(l[t])) * kLn2);
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const int e = 32 * d + 8 * (r / 4) + 4 * half;
-          if (e < a.D)
-            put(row0 + r0, e, make_float4(o[t][d][r] * inv, o[t][d][r + 1] * inv, o[t][d][r + 2] * inv, o[t][d][r + 3] * inv));
-        }
-    }
+      for (int r = 0; r < 16; r += 4) {
+        const int e = 32 * d + 8 * (r / 4) + 4 * half;
+        if (e < a.D) put(row0 + r0, e, make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv));
+      }
   } else {
     float* const acc = reinterpret_cast<float*>(smem);                   // [KW][kRows][kOutRow]
     float* const stat = acc + KW * kRows * kOutRow;                      // [KW][kRows][2]
     __syncthreads();
+    const int r0 = kw * kRows + rw * 32 + col;
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const int r0 = kw * kRows + (rw * QT + t) * 32 + col;
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<float4*>(acc + r0 * kOutRow + 32 * d + 8 * (r / 4) + 4 * half) =
-              make_float4(o[t][d][r], o[t][d][r + 1], o[t][d][r + 2], o[t][d][r + 3]);
-      if (half == 0) {
-        stat[r0 * 2] = l[t] == 0.f ? -INFINITY : mc[t];
-        stat[r0 * 2 + 1] = l[t];
-      }
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(acc + r0 * kOutRow + 32 * d + 8 * (r / 4) + 4 * half) =
+            make_float4(o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]);
+    if (half == 0) {
+      stat[r0 * 2] = l == 0.f ? -INFINITY : mc;
+      stat[r0 * 2 + 1] = l;
     }
     __syncthreads();
     for (int x = tid; x < rows * (ND * 8); x += 64 * RW * KW) {
@@ -551,10 +527,10 @@ template <bool F16, int ND>
 void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
   const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
   switch (shape) {
-    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
-    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 2, 2, 1>), grid, dim3(256), 0, s, a, p); break;
-    case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
-    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
+    case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
+    case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 2, 1>), grid, dim3(256), 0, s, a, p); break;
+    case 2: hipLaunchKernelGGL((attend_kernel<F16, ND, 4, 1, 2>), grid, dim3(256), 0, s, a, p); break;
+    default: hipLaunchKernelGGL((attend_kernel<F16, ND, 8, 1, 2>), grid, dim3(512), 0, s, a, p); break;
   }
 }
 
