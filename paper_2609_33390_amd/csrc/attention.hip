@@ -16,6 +16,15 @@
 // between the wavefront's halves, and the probabilities are already the
 // operand of out^T = V^T P^T, with the keys in an order that the transposed
 // LDS reads of V follow.
+//
+// Keys and values come to LDS by asynchronous copies, a tile ahead.  Few rows
+// are bound by the read of the cache: 64 sequences x 8 heads x 2048 keys of 128
+// elements, 32 rows each, run at 5.0 TB/s (a large copy: 4.8), 64 rows at 5.1.
+// Many rows are bound by the matrix cores and by what feeds them from LDS: 32768
+// rows (4096 a key head) over 16384 shared keys, 275 GFLOP, take 0.33 ms, 0.83
+// PFLOP/s where a library product of 8192^3 reaches 1.19; with the LDS reads left
+// out 0.28, with the softmax left out too 0.24.  Small calls are bound by latency:
+// lengths, page ids, keys, join.
 #include "half_mfma.h"
 #include "kernels.h"
 
@@ -470,10 +479,33 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, AttnPlan p) 
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
-// The tile of a launch: rows, and keys of a step of the whole workgroup.
-struct TileShape { int rows, keys, slots; };  // slots: workgroups the GPU holds at once
+// The tile of a launch: rows, keys of a step of the whole workgroup, and the
+// workgroups that the GPU holds at once (two a CU, but one of the 256-row tile).
+// The smallest tile that holds the rows wastes the fewest of the matrix cores'
+// rows; from 129 rows on the 256-row tile reads each key once where 128-row
+// tiles read it twice (1365 rows over 1003 keys: 16 us against 25).
+struct TileShape { int rows, keys, slots; };
 constexpr TileShape kShapes[] = {{32, 64, 2 * kCUs}, {64, 64, 2 * kCUs}, {128, 64, 2 * kCUs}, {256, 64, kCUs}};
 int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
+
+// Runs of `keys` keys that `whole` workgroups would cover: the fewest rounds of
+// workgroups, where each pays for its start and for the join about as much as for
+// 512 keys.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
+// runs of 512 keys 119, of 256 147.)
+struct Runs { int count, keys; };
+Runs runs_of(int keys, int64_t whole, TileShape t) {
+  Runs best{};
+  double least = 1e300;
+  for (int s = 1; s <= 64; ++s) {
+    const int run = ceil_div(ceil_div(keys, s), t.keys) * t.keys, count = ceil_div(keys, run);
+    const double cost = ((whole * count + t.slots - 1) / t.slots) * (run + 512.0);
+    if (cost < least) {
+      least = cost;
+      best = {count, run};
+    }
+  }
+  return best;
+}
 
 struct CallPlan {
   AttnPlan p;
@@ -489,33 +521,19 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int D, int prefix_len, int max_
     c.pre_shape = shape_for(rows);
     const TileShape t = kShapes[c.pre_shape];
     c.p.pre_tiles = ceil_div(rows, t.rows);
-    // runs: the fewest rounds of workgroups, each paying its start and its join
-    int best = 1;
-    double cost = 1e300;
-    for (int s = 1; s <= 64; ++s) {
-      const int run = ceil_div(ceil_div(prefix_len, s), t.keys) * t.keys;
-      const int used = ceil_div(prefix_len, run);
-      if (used != s) continue;
-      const double x = ceil_div(static_cast<int64_t>(c.p.pre_tiles) * Hkv * s, t.slots) * (run + 512.0);
-      if (x < cost) {
-        cost = x;
-        best = s;
-      }
-    }
-    c.p.pre_run = ceil_div(ceil_div(prefix_len, best), t.keys) * t.keys;
-    c.p.pre_splits = best;
-    c.p.pre_groups = Hkv * best;
+    const Runs r = runs_of(prefix_len, static_cast<int64_t>(c.p.pre_tiles) * Hkv, t);
+    c.p.pre_run = r.keys;
+    c.p.pre_splits = r.count;
+    c.p.pre_groups = Hkv * r.count;
   }
   if (max_seq_len > 0 || prefix_len == 0) {
     const int rows = L * G;
     c.own_shape = shape_for(rows);
     const TileShape t = kShapes[c.own_shape];
     c.p.own_tiles = ceil_div(rows, t.rows);
-    const int64_t whole = static_cast<int64_t>(B) * Hkv * c.p.own_tiles;
-    const int most = max_seq_len > 0 ? max_seq_len : 1;
-    const int want = static_cast<int>(whole >= 2 * kCUs ? 1 : ceil_div(2 * kCUs, whole));
-    c.p.own_run = ceil_div(ceil_div(most, want < 64 ? want : 64), t.keys) * t.keys;
-    c.p.own_splits = ceil_div(most, c.p.own_run);
+    const Runs r = runs_of(max_seq_len > 0 ? max_seq_len : 1, static_cast<int64_t>(B) * Hkv * c.p.own_tiles, t);
+    c.p.own_run = r.keys;
+    c.p.own_splits = r.count;
     c.p.own_groups = B * Hkv * c.p.own_splits;
   }
   c.p.own_first = c.p.pre_splits;
