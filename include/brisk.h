@@ -15,6 +15,10 @@
  * brisk_rerank_finish split the rerank at the candidates, so that its first
  * part can overlap the LM-head pass.
  *
+ * Further down stand the operators around the step: attention over a shared
+ * prefix and a paged cache, that cache's eviction, and verification of drafts
+ * from given probabilities.
+ *
  * Conventions shared by every entry point
  *   - Every pointer argument is a DEVICE pointer owned by the caller, except
  *     the brisk_corrector struct itself (host memory, read during the call)
@@ -23,7 +27,8 @@
  *     and outputs differ.  Its only global state is the fixed scratch of
  *     brisk_propose_block_noalloc (one array per GPU, and its address).
  *   - bf16 tensors are passed as uint16_t bit patterns; all matrices are
- *     row-major and densely packed (row stride = row length).
+ *     row-major and densely packed (row stride = row length) where a call
+ *     takes no strides.
  *   - Rows of a block are numbered r = b * L + (i - 1) for sequence b and
  *     in-block position i = 1..L.
  *   - `stream` is a hipStream_t (NULL = the default stream).  Work is queued
