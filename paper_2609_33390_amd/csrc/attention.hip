@@ -159,8 +159,10 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   // A copy is 1 KiB: RPI keys, RB / 16 lanes a key.  The place of a key in
   // memory is worked out once, by the lane that holds it for this wavefront's
   // copies, and handed to the key's lanes by broadcasts inside 16-lane rows.
-  const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
-  const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
+  const uint8_t* const k_src = reinterpret_cast<const uint8_t*>(
+      own ? a.kv.k + hk * a.kv.head_stride : a.pre_k + hk * a.pre_head_stride);
+  const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(
+      own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
   uint8_t* const lds = smem + kw * (2 * kStage);
   const int held = rw * NI * RPI + held_key<RB>(lane);
   const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
