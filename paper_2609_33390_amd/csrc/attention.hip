@@ -109,11 +109,17 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   const int group = bid / 8 / tiles * 8 + bid % 8, tile = bid / 8 % tiles;
   if (group >= (own ? p.own_groups : p.pre_groups)) return;
   int b = 0, hk, split, key0, key1, row0, rows;
+  const int held = rw * NI * RPI + held_key<RB>(lane);  // the key of a tile whose place this lane works out
+  int page = 0;                                  // page id of the held key, a tile ahead
   if (own) {
     // first runs of all sequences, then second ones, ...: later runs are fewer where lengths differ
     hk = group % a.Hkv;
     b = group / a.Hkv % a.B;
     split = group / a.Hkv / a.B;
+    // The first tile's pages are on their way while the length is (entries past it are not used).
+    if (a.max_seq_len > 0)
+      page = a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages +
+                        (min(split * p.own_run + kw * T + held, a.max_seq_len - 1) >> a.kv.page_shift)];
     const int n = kv_len(a.kv, b, a.max_seq_len);
     key0 = split * p.own_run;
     key1 = min(n, key0 + p.own_run);
@@ -164,10 +170,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   const uint8_t* const v_src = reinterpret_cast<const uint8_t*>(
       own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
   uint8_t* const lds = smem + kw * (2 * kStage);
-  const int held = rw * NI * RPI + held_key<RB>(lane);
   const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
   const bool whole = a.D == 32 * ND;
-  int page = 0;                                  // page id of the held key, a tile ahead
   auto look_up = [&](int j0) {
     const int j = max(min(j0 + held, key1 - 1), 0);
     if (own) page = a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (j >> a.kv.page_shift)];
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
     const int v_end = careful ? min(key1, max(base, 0)) : key1;
     int j0 = key0 + kw * T;
     if (steps > 0) {
-      look_up(j0);
+      if (careful) look_up(j0);
       stage(j0, 0, v_end);
       look_up(j0 + T * KW);
     }

@@ -402,13 +402,18 @@ __global__ __launch_bounds__(kSelectThreads) void evict_chunk_kernel(EvictArgs a
     // the histograms of the pass before, all of them and those of the chunks before this one
     const uint2* h = reinterpret_cast<const uint2*>(hist_of(PASS - 1)) + (kBins / 2 - 1 - tid);
     uint32_t c0 = 0, c1 = 0, p0 = 0, p1 = 0;
-#pragma unroll 8
-    for (int c = 0; c < chunks; ++c) {
-      const uint2 x = h[c * (kBins / 2)];
-      c0 += x.y;
-      c1 += x.x;
-      p0 += c < mine ? x.y : 0;
-      p1 += c < mine ? x.x : 0;
+    for (int c = 0; c < chunks; c += 16) {         // 16 loads in flight
+      uint2 x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u] = h[min(c + u, chunks - 1) * (kBins / 2)];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const bool in = c + u < chunks, before = c + u < mine;
+        c0 += in ? x[u].y : 0;
+        c1 += in ? x[u].x : 0;
+        p0 += before ? x[u].y : 0;
+        p1 += before ? x[u].x : 0;
+      }
     }
     find_digit(sh, c0, c1, st.left);
     const uint32_t digit = sh.digit, hi = kBins - 1 - 2 * tid;
