@@ -202,8 +202,9 @@ def _dev_tensor(t: torch.Tensor, name: str, dtype: torch.dtype, ndim: Optional[i
     dimension count or exact shape, contiguity, a HIP device, and (when
     ``device`` is given) the same device as the call's other tensors.  A
     wrong shape would otherwise let a kernel read or write past the buffer."""
-    if (shape is not None and device is not None and type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
-            and t.device == device and device.type == "cuda" and t.is_contiguous()):
+    if (type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous()
+            and (t.shape == shape if shape is not None else ndim is None or t.dim() == ndim)
+            and (device is None or t.device == device)):
         return                                     # nothing to object to: most calls end here
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -233,7 +234,7 @@ def _ws_bytes(ws: torch.Tensor, device: torch.device, need: int, name: str = "wo
         raise ValueError(f"{name} must live on a HIP device, got {ws.device}")
     if ws.device != device:
         raise ValueError(f"{name} is on {ws.device}, the call's other tensors on {device}")
-    nbytes = ws.numel() * ws.element_size()
+    nbytes = ws.nbytes
     if nbytes < need:
         raise ValueError(f"{name} holds {nbytes} bytes, the call needs {need}")
     return nbytes

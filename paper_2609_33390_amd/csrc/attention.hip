@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   constexpr int kStage = 2 * kTile;
   constexpr int kRows = RW * 32;
   constexpr int kOutRow = ND * 32 + 4;           // floats of a row of the join
-  constexpr int kJoin = KW > 1 ? KW * kRows * (kOutRow + 2) * 4 : 0;
+  constexpr int kJoin = KW > 1 ? KW * kRows * (kOutRow + 2) * 4 : RW * 8192;
   constexpr int kLds = 2 * kStage * KW > kJoin ? 2 * kStage * KW : kJoin;
   static_assert(T % (RPI * RW) == 0 && kLds <= 163840);
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds];
@@ -372,33 +372,51 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   l = swap32_sum(l);
 
   // ---- join the key groups and write
-  auto put = [&](int row, int e, float4 x) {  // elements e..e+3 of a row's normalised sum
-    const int64_t out = (static_cast<int64_t>(row / G) * a.H + hk * G + row % G);
+  auto out_row = [&](int row) { return row / G * a.H + hk * G + row % G; };
+  auto put = [&](int64_t out, int e, float4 x) {  // elements e..e+3 of a row's normalised sum
     if (p.part) {
       *reinterpret_cast<float4*>(p.part + (out * p.splits + split) * a.D + e) = x;
     } else {
       *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(x.x, x.y), pack2<F16>(x.z, x.w));
     }
   };
-  auto put_lse = [&](int row, float x) {
-    const int64_t out = (static_cast<int64_t>(row / G) * a.H + hk * G + row % G);
+  auto put_lse = [&](int64_t out, float x) {
     if (p.part)
       p.part_lse[out * p.splits + split] = x;
     else if (a.lse)
       a.lse[out] = x;
   };
   if constexpr (KW == 1) {
-    const int r0 = rw * 32 + col;
-    if (r0 >= rows) return;
+    // Through LDS, 64 elements of a wavefront's rows at a time, so that stores cover whole lines:
+    // from the registers a store would reach 32 rows with 32 bytes each (prefix of 16384 keys, 32768
+    // rows: 336 us that way).  A row's 16-byte chunks are permuted by its number.
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (half == 0) put_lse(row0 + r0, l == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * kLn2);
+    const int left = rows - rw * 32, out = out_row(row0 + min(rw * 32 + col, rows - 1));
+    if (half == 0 && col < left) put_lse(out, l == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * kLn2);
+    float4* const turn = reinterpret_cast<float4*>(smem + rw * 8192);  // [32][16]
+    __syncthreads();                               // the tiles have been read
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int e0 = 0; e0 < 32 * ND; e0 += 64) {
 #pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int e = 32 * d + 8 * (r / 4) + 4 * half;
-        if (e < a.D) put(row0 + r0, e, make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv));
+      for (int d = e0 / 32; d < ND && d < e0 / 32 + 2; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int chunk = 8 * (d % 2) + 2 * (r / 4) + half;
+          turn[col * 16 + (chunk ^ (col & 15))] =
+              make_float4(o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+        }
+      asm volatile("" ::: "memory");               // LDS works in order for a wavefront; so must the compiler
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = 4 * u + lane / 16, chunk = lane & 15, e = e0 + 4 * chunk;
+        const float4 x = turn[r * 16 + (chunk ^ (r & 15))];
+        const int to = __shfl(out, r, kWave);
+        if (r < left && e < a.D) put(to, e, x);
       }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
   } else {
     float* const acc = reinterpret_cast<float*>(smem);                   // [KW][kRows][kOutRow]
     float* const stat = acc + KW * kRows * kOutRow;                      // [KW][kRows][2]
@@ -434,8 +452,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         sum.w += f * y.w;
       }
       const float inv = L == 0.f ? 0.f : 1.f / L;
-      if (e < a.D) put(row0 + r, e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
-      if (e == 0) put_lse(row0 + r, L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2);
+      if (e < a.D) put(out_row(row0 + r), e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+      if (e == 0) put_lse(out_row(row0 + r), L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2);
     }
   }
 }
