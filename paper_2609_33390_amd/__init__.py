@@ -230,7 +230,7 @@ def _ws_bytes(ws: torch.Tensor, device: torch.device, need: int, name: str = "wo
         raise TypeError(f"{name} must be a torch.Tensor")
     if not ws.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if ws.device.type != "cuda":
+    if not ws.is_cuda:
         raise ValueError(f"{name} must live on a HIP device, got {ws.device}")
     if ws.device != device:
         raise ValueError(f"{name} is on {ws.device}, the call's other tensors on {device}")

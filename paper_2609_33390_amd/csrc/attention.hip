@@ -21,7 +21,7 @@
 // are bound by the read of the cache: 64 sequences x 8 heads x 2048 keys of 128
 // elements, 32 rows each, run at 5.0 TB/s (a large copy: 4.8), 64 rows at 5.1.
 // Many rows are bound by the matrix cores and by what feeds them from LDS: 32768
-// rows (4096 a key head) over 16384 shared keys, 275 GFLOP, take 0.33 ms, 0.83
+// rows (4096 a key head) over 16384 shared keys, 275 GFLOP, take 0.32 ms, 0.85
 // PFLOP/s where a library product of 8192^3 reaches 1.19; with the LDS reads left
 // out 0.28, with the softmax left out too 0.24.  Small calls are bound by latency:
 // lengths, page ids, keys, join.
