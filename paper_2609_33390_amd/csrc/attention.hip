@@ -83,7 +83,7 @@ __device__ __forceinline__ int v_swizzle(int key) { return RB == 256 ? (key & 3)
 // rows each, took 93 us that way and 82 us as two wavefronts of 32 rows.)
 template <bool F16, int ND, int RW, int KW, int NT>
 __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(AttentionArgs a, AttnPlan p) {
-  constexpr int RB = ND > 2 ? 256 : 128, T = 32 * NT, NC = 2 * ND;
+  constexpr int RB = lds_row_bytes(ND), T = 32 * NT, NC = 2 * ND;
   constexpr int RPI = 1024 / RB;                 // rows of a wavefront's copy
   constexpr int NI = T / RPI / RW;               // copies of K (and of V) a wavefront
   constexpr int kTile = T * RB;                  // bytes of K (or V) of a tile
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
       own ? a.kv.v + hk * a.kv.head_stride : a.pre_v + hk * a.pre_head_stride);
   uint8_t* const lds = smem + kw * (2 * kStage);
   const int pc = lane % (RB / 16), key_in = lane / (RB / 16);  // this lane's chunk, and its key in a copy
-  const bool whole = a.D == 32 * ND;
+  const bool whole = head_fills_row(a.D, ND);
   auto look_up = [&](int j0) {
     const int j = max(min(j0 + held, key1 - 1), 0);
     if (own) page = a.kv.table[static_cast<int64_t>(b) * a.kv.max_pages + (j >> a.kv.page_shift)];
@@ -579,12 +579,11 @@ void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStrea
 template <bool F16>
 void launch_all(const AttentionArgs& a, const CallPlan& c, hipStream_t s) {
   auto go = [&](int shape, const AttnPlan& p) {
-    if (a.D <= 64)
-      launch_shape<F16, 2>(shape, a, p, s);
-    else if (a.D <= 96)
-      launch_shape<F16, 3>(shape, a, p, s);
-    else
-      launch_shape<F16, 4>(shape, a, p, s);
+    switch (head_slices(a.D)) {
+      case 2: launch_shape<F16, 2>(shape, a, p, s); break;
+      case 3: launch_shape<F16, 3>(shape, a, p, s); break;
+      default: launch_shape<F16, 4>(shape, a, p, s); break;
+    }
   };
   if (c.pre_shape == c.own_shape) {
     go(c.pre_shape, c.p);

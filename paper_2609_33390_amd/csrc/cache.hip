@@ -22,7 +22,7 @@ constexpr int kScoreWaves = 4, kMaxTiles = 8;
 // QT: 32-row tiles of queries in registers.
 template <bool F16, int ND, int QT>
 __global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(ScoreArgs a, int tiles) {
-  constexpr int RB = ND > 2 ? 256 : 128, NC = 2 * ND, kTile = 32 * RB, NI = kTile / 1024, RPI = 1024 / RB;
+  constexpr int RB = lds_row_bytes(ND), NC = 2 * ND, kTile = 32 * RB, NI = kTile / 1024, RPI = 1024 / RB;
   constexpr int kScoreRows = 32 * QT;
   __shared__ __attribute__((aligned(1024))) uint8_t s_keys[kScoreWaves][2][kTile];
   __shared__ __attribute__((aligned(16))) float s_lse[kScoreWaves][kScoreRows];  // times log2 e; +inf: adds nothing
@@ -523,12 +523,11 @@ void launch_score(const ScoreArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(whole * runs)), threads(64 * kScoreWaves);
   const bool two = a.L * (a.H / a.Hkv) > 32;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, s, a, tiles); };
-  if (a.D <= 64)
-    two ? go(score_kernel<F16, 2, 2>) : go(score_kernel<F16, 2, 1>);
-  else if (a.D <= 96)
-    two ? go(score_kernel<F16, 3, 2>) : go(score_kernel<F16, 3, 1>);
-  else
-    two ? go(score_kernel<F16, 4, 2>) : go(score_kernel<F16, 4, 1>);
+  switch (head_slices(a.D)) {
+    case 2: two ? go(score_kernel<F16, 2, 2>) : go(score_kernel<F16, 2, 1>); break;
+    case 3: two ? go(score_kernel<F16, 3, 2>) : go(score_kernel<F16, 3, 1>); break;
+    default: two ? go(score_kernel<F16, 4, 2>) : go(score_kernel<F16, 4, 1>); break;
+  }
 }
 
 }  // namespace

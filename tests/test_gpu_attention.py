@@ -72,6 +72,20 @@ def test_attention_matches_oracle(kw):
     _check(c, *_run(c))
 
 
+@pytest.mark.parametrize("D", [64, 72, 88, 96, 120, 128])
+@pytest.mark.parametrize("kw", [
+    dict(B=1, L=1, H=2, Hkv=2, prefix=64, lens=[128]),                       # each row count's tile
+    dict(B=2, L=8, H=12, Hkv=2, prefix=128, lens=[64, 192], mask="causal"),
+    dict(B=2, L=30, H=6, Hkv=2, prefix=256, lens=[64, 128], mask="mixed"),
+    dict(B=4, L=64, H=8, Hkv=2, prefix=192, lens=[64, 64, 128, 320], mask="causal"),
+])
+def test_full_tiles_up_to_the_end_of_the_pool(D, kw):
+    """Whole tiles of keys, the last of them the last of its tensor, for heads that fill their rows of LDS or do not."""
+    for dtype in ("bf16", "f16"):
+        c = Case(D=D, dtype=dtype, seed=D, page=64, spare_pages=0, **kw)
+        _check(c, *_run(c))
+
+
 @pytest.mark.parametrize("std", [0.0, 30.0])
 def test_flat_and_very_sharp_weights(std):
     """All logits equal, and logits of several hundred."""
