@@ -56,7 +56,8 @@ typedef enum {
   BRISK_OK = 0,
   BRISK_ERR_NULL = -1,        /* a required pointer is NULL                   */
   BRISK_ERR_SHAPE = -2,       /* a size is out of range or inconsistent        */
-  BRISK_ERR_UNSUPPORTED = -3, /* alignment / divisibility the kernels need     */
+  BRISK_ERR_UNSUPPORTED = -3, /* alignment / divisibility the kernels need, or
+                                 buffers that must not overlap and do         */
   BRISK_ERR_WORKSPACE = -4,   /* workspace missing or smaller than required    */
   BRISK_ERR_HIP = -5,         /* a HIP launch failed                           */
   BRISK_ERR_SCRATCH = -6      /* the shape needs more than the fixed scratch  */
@@ -567,11 +568,13 @@ int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap,
  * the pages past it.
  *
  *   score_in, score_out  [B, n_kv_heads, cap] fp32;  pos_in, pos_out the same
- *               in int32; outputs must not overlap the inputs
+ *               in int32
  *   next_pos    [B] int32  position of the next token (tokens seen so far)
- *   new_len     [B] int32 out
+ *   new_len     [B] int32 out; not seq_len itself (copy it there afterwards)
  *   ws          device scratch of brisk_cache_evict_workspace_size bytes
  *
+ * No output, nor ws, may overlap another output or an input (next_pos, seq_len
+ * and block_table among them): BRISK_ERR_UNSUPPORTED.
  * Limits: the cache's; B >= 1, B * n_kv_heads <= 2^20, 1 <= cap <= 2^24,
  * B * n_kv_heads * cap <= 2^36, budget >= 1, 0 <= recent <= budget; lengths
  * are cut to cap.  Two sequences

@@ -893,7 +893,8 @@ def cache_evict(cache: KVCache, score: torch.Tensor, pos: torch.Tensor, next_pos
     the slots whose ``pos`` is among the ``recent`` latest before ``next_pos``
     [B], then those of the largest ``score``.  ``score`` fp32 and ``pos`` int32
     are [B, n_kv_heads, cap]; returns (score, pos, new_len [B]) of the slots as
-    they lie afterwards.  The cache's ``seq_len`` is left to the caller."""
+    they lie afterwards.  The cache's ``seq_len`` is left to the caller: workgroups
+    read it while others write ``new_len``, which is therefore another tensor, copied into it afterwards."""
     dev = cache.device
     _dev_tensor(score, "score", torch.float32, 3, device=dev)
     cap = score.shape[2]
@@ -912,6 +913,8 @@ def cache_evict(cache: KVCache, score: torch.Tensor, pos: torch.Tensor, next_pos
     _dev_tensor(new_len, "new_len", torch.int32, shape=(cache.B,), device=dev)
     if _overlap(score, score_out) or _overlap(pos, pos_out):
         raise ValueError("score_out and pos_out must not overlap score and pos")
+    if _overlap(new_len, cache.seq_len) or _overlap(new_len, next_pos):
+        raise ValueError("new_len must not overlap the cache's seq_len (copy it there after the call) or next_pos")
     need = _evict_workspace_size(cache.B, cache.n_kv_heads, cap, budget)
     if workspace is None:
         workspace = _workspace(dev, need, "evict")

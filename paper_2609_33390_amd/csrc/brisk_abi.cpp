@@ -65,6 +65,16 @@ int attention_shape_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_he
   return d_head % 8 != 0 ? BRISK_ERR_UNSUPPORTED : BRISK_OK;
 }
 
+// A device buffer of a call, for the question whether two of them share memory.
+struct Span {
+  const void* p;
+  uint64_t bytes;
+};
+bool overlap(Span a, Span b) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
 int evict_shape_check(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget) {
   if (B < 1 || n_kv_heads < 1 || n_kv_heads > 1024 || static_cast<int64_t>(B) * n_kv_heads > kMaxRows ||
       cap < 1 || cap > kMaxEvictCap || budget < 1 ||
@@ -131,7 +141,7 @@ const char* brisk_status_str(int status) {
     case BRISK_OK: return "ok";
     case BRISK_ERR_NULL: return "a required pointer is NULL";
     case BRISK_ERR_SHAPE: return "a size is out of range or inconsistent";
-    case BRISK_ERR_UNSUPPORTED: return "unsupported alignment or divisibility (16-byte pointers, d % 8 == 0)";
+    case BRISK_ERR_UNSUPPORTED: return "unsupported alignment or divisibility (16-byte pointers, d % 8 == 0), or overlapping buffers";
     case BRISK_ERR_WORKSPACE: return "workspace missing or too small";
     case BRISK_ERR_HIP: return "a HIP launch failed";
     case BRISK_ERR_SCRATCH: return "the shape needs more scratch than the fixed no-alloc buffer holds";
@@ -567,6 +577,18 @@ int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score
   const size_t need = brisk::evict_workspace_bytes(B, cache->n_kv_heads, cap, budget);
   if (ws_bytes < need || !ws) return BRISK_ERR_WORKSPACE;
   if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
+  // Heads and launches read the inputs while others write: a length cut in place would let
+  // a later launch take lists that nobody wrote.
+  const uint64_t slots = static_cast<uint64_t>(B) * cache->n_kv_heads * cap * 4, seqs = static_cast<uint64_t>(B) * 4;
+  const Span ins[] = {{score_in, slots}, {pos_in, slots}, {next_pos, seqs}, {cache->seq_len, seqs},
+                      {cache->block_table, seqs * cache->max_pages}};
+  const Span outs[] = {{score_out, slots}, {pos_out, slots}, {new_len, seqs}, {ws, need}};
+  for (int i = 0; i < 4; ++i) {
+    for (const Span& in : ins)
+      if (overlap(outs[i], in)) return BRISK_ERR_UNSUPPORTED;
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], outs[j])) return BRISK_ERR_UNSUPPORTED;
+  }
   a.k = cache->k_pages;
   a.v = cache->v_pages;
   a.score_in = score_in;

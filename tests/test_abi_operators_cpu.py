@@ -128,6 +128,22 @@ def test_evict_validation(kw, want):
     assert _evict(**kw) == want
 
 
+SLOTS = 4 * 8 * 2048 * 4            # bytes of a score or position array of _evict's sizes
+APART = dict(si=1 << 24, pi=2 << 24, np_=3 << 24, so=4 << 24, po=5 << 24, nl=6 << 24, ws=7 << 24, ws_bytes=1 << 24)
+LENS, TABLE = 8 << 24, 9 << 24
+
+
+@pytest.mark.parametrize("kw", [
+    dict(nl=LENS), dict(nl=LENS + 12), dict(nl=LENS - 12), dict(nl=APART["np_"]), dict(nl=TABLE + 4 * 32 * 4 - 4),
+    dict(nl=APART["si"] + SLOTS - 4), dict(nl=APART["so"] + 8), dict(nl=APART["ws"]), dict(so=APART["si"]),
+    dict(so=APART["si"] + SLOTS - 16), dict(so=APART["pi"] - 16), dict(po=APART["si"]), dict(po=APART["pi"] + 16),
+    dict(po=APART["so"]), dict(ws=APART["si"]), dict(ws=APART["pi"] + 16), dict(ws=LENS), dict(ws=TABLE), dict(ws=APART["po"]),
+])
+def test_evict_refuses_overlapping_buffers(kw):
+    """Lengths cut in place among them: later launches would take lists that nobody wrote."""
+    assert _evict(_cache(seq_len=LENS, block_table=TABLE), **{**APART, **kw}) == EUNSUP
+
+
 def _draft(**kw):
     a = dict(t=FAKE, ts=1000, d=FAKE, ds=1000, tok=FAKE, n=None, u=FAKE, e=FAKE, es=1000, B=4, L=8, V=1000, acc=FAKE,
              out=FAKE, ws=FAKE, ws_bytes=BIG)

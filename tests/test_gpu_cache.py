@@ -275,3 +275,17 @@ def test_binding_refuses_overlap_and_misfits():
         brisk.cache_score(q, lse, cache, s[:1])
     with pytest.raises(TypeError):
         brisk.cache_score(q, lse, cache, s.double())
+
+
+def test_binding_refuses_lengths_cut_in_place():
+    e = EvictCase([40, 30], 10, 2, seed=24)
+    cache = e.c.cache(brisk)
+    s, p, n = (torch.from_numpy(x).cuda() for x in (e.score, e.pos, e.next_pos))
+    both = torch.zeros(3, dtype=torch.int32, device="cuda")
+    shifted = brisk.KVCache(cache.k_pages, cache.v_pages, cache.block_table, both[:2])
+    for c, at, out in ((cache, n, cache.seq_len), (cache, n, n), (shifted, n, both[1:]), (shifted, both[1:], both[1:])):
+        with pytest.raises(ValueError, match="new_len"):
+            brisk.cache_evict(c, s, p, at, 10, 2, new_len=out)
+    with pytest.raises(brisk.BriskError) as err:                # and whatever else shares memory, by the library
+        brisk.cache_evict(cache, s, p, n, 10, 2, score_out=p.view(torch.float32))
+    assert err.value.status == -3
