@@ -35,6 +35,8 @@ namespace {
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCUs = 256;
+constexpr float kLag = 8.f;        // the subtracted logit may be this far (in base 2) behind the maximum
+constexpr float kFine = 0x1p20f;   // up to here a float holds a subtracted logit to 2^-5
 
 // What one launch works on: prefix items, then own items.
 struct AttnPlan {
@@ -204,6 +206,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   // m: the subtracted logit (unscaled); mc = c * m; l: this lane's part of the sum, zero while
   // the row has seen no key (NaN logits pass the maximum by, but not the sum)
   float m, mc, l;
+  bool wide;                                     // a row's mc is past kFine (the same in all lanes)
   const int steps = (key1 - key0 + T * KW - 1) / (T * KW);
 
   // The second time round only where values that some rows must not see are
@@ -211,6 +214,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   for (int careful = 0;; ++careful) {
     m = -INFINITY;
     mc = l = 0.f;
+    wide = false;
 #pragma unroll
     for (int d = 0; d < ND; ++d) o[d] = floatx16{};
     const int v_end = careful ? min(key1, max(base, 0)) : key1;
@@ -292,7 +296,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
       top = swap32_max(top);
       // The subtracted logit follows the maximum only once that is 2^8 times ahead.
-      if (__any(top * c > mc + 8.f || (m == -INFINITY && top > -INFINITY))) {
+      if (__any((top - m) * c > kLag)) {
         const float up = fmaxf(m, top);
         const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - up) * c);
         l *= f;
@@ -300,6 +304,18 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         for (int d = 0; d < ND; ++d) o[d] *= f;
         m = up;
         mc = up == -INFINITY ? 0.f : up * c;
+        wide = __any(fabsf(mc) > kFine);
+      }
+      // s c - mc is off by the rounding of mc, by the same for all of a row, which cancels in the
+      // quotient; but past kFine that may be more than the exponent range.
+      float sub = mc;
+      if (wide) {
+        const float from = m == -INFINITY ? 0.f : m;
+        sub = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] -= from;
       }
       // Probabilities are rounded to the cache's type here, as the products take them (their
       // sum is of the unrounded ones): as large an error as that of rounding the output.
@@ -309,8 +325,8 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         uint32_t w[8];
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -mc));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][r + 1], c, -mc));
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -sub));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][r + 1], c, -sub));
           l += p0 + p1;
           w[r / 2] = pack2<F16>(p0, p1);
         }
@@ -342,7 +358,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
               dot += half_to_f32<F16>(kw4[w] & 0xFFFF) * half_to_f32<F16>(qw4[w] & 0xFFFF) +
                      half_to_f32<F16>(kw4[w] >> 16) * half_to_f32<F16>(qw4[w] >> 16);
           }
-          const float w = __builtin_amdgcn_exp2f(fmaf(swap32_sum(dot), c, -mc));
+          const float w = __builtin_amdgcn_exp2f(fmaf(swap32_sum(dot) - (wide && m != -INFINITY ? m : 0.f), c, -sub));
           const bool see = block_sees(word, j - base);
 #pragma unroll
           for (int d = 0; d < ND; ++d) {

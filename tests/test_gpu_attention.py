@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 import torch
 
+import oracle.attention_oracle as ao
 from kv_cases import UNIT, Case
 
 pytestmark = pytest.mark.gpu
@@ -111,6 +112,57 @@ def test_largest_magnitudes():
         p = np.exp(s - s.max())
         want = p @ v[:, h] / p.sum()
         assert np.abs(out[0, :, h].double().cpu().numpy() - want).max() <= 2 * UNIT["bf16"] * (np.abs(v).max() + 1)
+
+
+@pytest.mark.parametrize("hidden", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(B=2, L=4, H=4, Hkv=2, D=128, prefix=70, lens=[100, 9]),
+    dict(B=3, L=7, H=14, Hkv=2, D=64, prefix=None, lens=[120, 64, 7]),
+    dict(B=2, L=16, H=8, Hkv=1, D=96, prefix=20, lens=[90, 30]),
+    dict(B=5, L=16, H=8, Hkv=2, D=128, prefix=70, lens=[16, 40, 60, 80, 100]),
+    dict(B=1, L=2, H=4, Hkv=2, D=80, prefix=40, lens=[100], dtype="f16"),
+])
+def test_logits_far_past_the_exponent_range(kw, hidden):
+    """Finite logits whose spacing in 32 bits is many units: the largest takes all the weight.
+
+    Every product is of two short significands, so logits are exact and the
+    winner's probability is one: its value comes out bit for bit.  One head in
+    two has logits of order one in the same tiles."""
+    c = Case(mask="causal", seed=18, **kw)
+    qs, ks = (2.0 ** 20, 2.0 ** 16) if c.dtype == "bf16" else (2.0 ** 14, 2.0 ** 14)
+    for b, n in enumerate(c.lens):
+        steps = c.rng.permutation(128)              # the own keys of a sequence differ
+        for j in range(n):
+            at = c.table[b, j // c.page], j % c.page
+            c.k[at] = 0
+            c.k[at][:, 0] = ks * (1 + steps[j] / 128)
+        if hidden:                                  # the last position's value; only its own row may notice
+            c.v[c.table[b, (n - 1) // c.page], (n - 1) % c.page] = float("inf")
+    if c.prefix is not None:                        # below every own key
+        c.prefix[0][:] = 0
+        c.prefix[0][..., 0] = ks / 2 * (1 + torch.arange(len(c.prefix[0]))[:, None] % 128 / 128)
+    c.q[..., 1:] = 0
+    c.q[..., 0] = qs * (1 + torch.arange(c.L * c.H).reshape(1, c.L, c.H) % 64 / 64)
+    c.q[:, :, ::2, 0] = 1 / ks
+    out, lse = _run(c)
+    o, z, mag, size = c.attention()
+    keep = np.ones((c.B, c.L), dtype=bool)
+    keep[:, -1] = not hidden
+    got, log = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    own_k, own_v = c.own(c.k), c.own(c.v)
+    G = c.H // c.Hkv
+    for b in range(c.B):
+        for i in np.nonzero(keep[b])[0]:
+            vis = np.nonzero(ao.sees(c.lens[b], c.L, i, c.mask[b, i]))[0]
+            for h in range(1, c.H, 2):
+                key = own_k[b][vis, h // G, 0]
+                assert (key == key.max()).sum() == 1
+                win = vis[key.argmax()]
+                assert np.array_equal(got[b, i, h], own_v[b][win, h // G]), (b, i, h, got[b, i, h][:4], log[b, i, h])
+                assert abs(log[b, i, h] - z[b, i, h]) <= 2.0 ** -21 * abs(z[b, i, h])
+    rows = np.nonzero(keep)
+    small = tuple(r[rows][:, ::2] for r in (o, z, mag, size))
+    _check(c, out.cpu()[rows][:, ::2], lse.cpu()[rows][:, ::2], small)
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
