@@ -320,6 +320,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
       // Probabilities are rounded to the cache's type here, as the products take them (their
       // sum is of the unrounded ones): as large an error as that of rounding the output.
       uint4 pf[2 * NT];
+      float sum = 0.f;  // a tile's, so that many small ones beside a large one reach l together
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         uint32_t w[8];
@@ -327,12 +328,13 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
         for (int r = 0; r < 16; r += 2) {
           const float p0 = __builtin_amdgcn_exp2f(fmaf(s[n][r], c, -sub));
           const float p1 = __builtin_amdgcn_exp2f(fmaf(s[n][r + 1], c, -sub));
-          l += p0 + p1;
+          sum += p0 + p1;
           w[r / 2] = pack2<F16>(p0, p1);
         }
         pf[2 * n] = make_uint4(w[0], w[1], w[2], w[3]);
         pf[2 * n + 1] = make_uint4(w[4], w[5], w[6], w[7]);
       }
+      l += sum;
       // ---- out^T += V^T P^T, 16 keys at a time, the next ones' values on the way
 #pragma unroll
       for (int g = 0; g < 2 * NT; ++g) {

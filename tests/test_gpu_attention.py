@@ -11,7 +11,7 @@ import pytest
 import torch
 
 import oracle.attention_oracle as ao
-from kv_cases import UNIT, Case
+from kv_cases import TYPES, UNIT, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -112,6 +112,50 @@ def test_largest_magnitudes():
         p = np.exp(s - s.max())
         want = p @ v[:, h] / p.sum()
         assert np.abs(out[0, :, h].double().cpu().numpy() - want).max() <= 2 * UNIT["bf16"] * (np.abs(v).max() + 1)
+
+
+class Sink:
+    """One key of logit 16 and value 0 among n - 1 of logit 16 - below and values of about one, read by
+    ``B`` sequences from the same pages: enough of them that every cache is one run of keys, or few, so
+    that it is split.  All rows see the same."""
+
+    def __init__(self, n, below, dtype, B, L=1, D=8, Hkv=8, page=256, seed=19):
+        rng = np.random.default_rng(seed)
+        dt = TYPES[dtype]
+        pages = -(-n // page)
+        k, v = torch.zeros(pages, page, Hkv, D, dtype=dt), torch.full((pages, page, Hkv, D), float("nan"), dtype=dt)
+        flat_k, flat_v = k.view(-1, Hkv, D), v.view(-1, Hkv, D)
+        flat_k[:, :, 0] = (16 - below) / 16
+        at = n // 3
+        flat_k[at, :, 0] = 1.0
+        flat_v[:n] = torch.from_numpy(rng.uniform(0.5, 1.5, (n, Hkv, D))).to(dt)
+        flat_v[at] = 0.0
+        q = torch.zeros(B, L, Hkv, D, dtype=dt)
+        q[..., 0] = 16.0
+        cache = brisk.KVCache(k.cuda(), v.cuda(), torch.arange(pages, dtype=torch.int32, device="cuda").repeat(B, 1),
+                              torch.full((B,), n, dtype=torch.int32, device="cuda"))
+        self.out, self.lse = brisk.block_attention(q.cuda(), cache, scale=1.0)
+        torch.cuda.synchronize()
+        s = 16.0 * flat_k[:n, 0, 0].double().numpy()
+        w = np.exp(s - s.max())
+        self.want = np.tensordot(w, flat_v[:n].double().numpy(), (0, 0)) / w.sum()
+        self.want_lse = s.max() + np.log(w.sum())
+        assert abs(w.sum() - 1 - (n - 1) * w[0]) < 1e-9
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L", [1, 40, 64])
+def test_weak_keys_beside_a_strong_one_are_counted(dtype, L):
+    """A log-sum-exp over one long run, most of it from keys whose weights are each below half a unit of the sum.
+
+    A lane adds 16 or 32 weights, then one such sum of n / 64 tiles to the total: each addition is off by at most
+    2^-25 of it.  Logits are exact."""
+    n = 65537
+    c = Sink(n, 17.4375, dtype, B=64, L=L)
+    assert abs(c.want_lse - 16.0) > 2.0 ** -10      # what the weak keys bring
+    got = c.lse.double().cpu().numpy()
+    print(f"[sink] {dtype} L={L}: lse off by {np.abs(got - c.want_lse).max():.2e}", flush=True)
+    assert np.abs(got - c.want_lse).max() <= (n / 64 + 32) * 2.0 ** -24 + 2.0 ** -20 * 17
 
 
 @pytest.mark.parametrize("hidden", [False, True])
