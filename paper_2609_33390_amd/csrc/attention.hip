@@ -35,7 +35,13 @@ namespace {
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCUs = 256;
-constexpr float kLag = 8.f;        // the subtracted logit may be this far (in base 2) behind the maximum
+// In base 2: the subtracted logit may be kLag behind the maximum, and the probabilities are held
+// kLift higher than that, which l and the log-sum-exp share.  f16 has no steps below 2^-24, so its
+// probabilities use its range from the top: at most 2^15, and a key's weight is off by at most
+// 2^-37 of the largest one's, besides its rounding to 11 bits (unlifted, 65536 keys of 2^-25 of the
+// largest weight, 0.2% together, were lost).  bf16 has the range of fp32.
+template <bool F16> constexpr float kLag = F16 ? 3.f : 8.f;
+template <bool F16> constexpr float kLift = F16 ? 12.f : 0.f;
 constexpr float kFine = 0x1p20f;   // up to here a float holds a subtracted logit to 2^-5
 
 // What one launch works on: prefix items, then own items.
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   };
 
   floatx16 o[ND];
-  // m: the subtracted logit (unscaled); mc = c * m; l: this lane's part of the sum, zero while
+  // m: the subtracted logit (unscaled); mc = c * m - kLift; l: this lane's part of the sum, zero while
   // the row has seen no key (NaN logits pass the maximum by, but not the sum)
   float m, mc, l;
   bool wide;                                     // a row's mc is past kFine (the same in all lanes)
@@ -295,15 +301,15 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
       top = swap32_max(top);
-      // The subtracted logit follows the maximum only once that is 2^8 times ahead.
-      if (__any((top - m) * c > kLag)) {
+      // The subtracted logit follows the maximum only once that is kLag ahead.
+      if (__any((top - m) * c > kLag<F16>)) {
         const float up = fmaxf(m, top);
         const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - up) * c);
         l *= f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] *= f;
         m = up;
-        mc = up == -INFINITY ? 0.f : up * c;
+        mc = up == -INFINITY ? 0.f : up * c - kLift<F16>;
         wide = __any(fabsf(mc) > kFine);
       }
       // s c - mc is off by the rounding of mc, by the same for all of a row, which cancels in the
@@ -311,14 +317,15 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
       float sub = mc;
       if (wide) {
         const float from = m == -INFINITY ? 0.f : m;
-        sub = 0.f;
+        sub = -kLift<F16>;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[n][r] -= from;
       }
       // Probabilities are rounded to the cache's type here, as the products take them (their
-      // sum is of the unrounded ones): as large an error as that of rounding the output.
+      // sum is of the unrounded ones): relative to sum p |v|, as large an error as that of rounding
+      // the output, and in f16 that of kLift.
       uint4 pf[2 * NT];
       float sum = 0.f;  // a tile's, so that many small ones beside a large one reach l together
 #pragma unroll

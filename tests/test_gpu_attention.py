@@ -158,6 +158,24 @@ def test_weak_keys_beside_a_strong_one_are_counted(dtype, L):
     assert np.abs(got - c.want_lse).max() <= (n / 64 + 32) * 2.0 ** -24 + 2.0 ** -20 * 17
 
 
+@pytest.mark.parametrize("n,below,B,L", [(65537, 17.4375, 64, 1), (65537, 17.4375, 64, 40), (65537, 17.4375, 64, 64),
+                                         (65537, 21.875, 64, 1), (200001, 17.4375, 64, 1), (65537, 9.0, 64, 1),
+                                         (65537, 17.4375, 1, 1), (65537, 17.4375, 2, 50)])
+def test_f16_probabilities_of_weak_keys(n, below, B, L):
+    """Outputs that are made of keys far below the largest weight, whose own value is zero.
+
+    Beyond the tolerance of every output (sum p |v| is the output itself here): each probability is off by at
+    most 2^-37 of the largest, each of a run's n / 16 matrix products rounds its sum by 2^-24, and the output's
+    own smallest step is 2^-24."""
+    c = Sink(n, below, "f16", B=B, L=L)
+    o = c.want
+    tol = (2 * UNIT["f16"] + 2.0 ** -15 + 2 * 2.0 ** -19 * 16 + n / 16 * 2.0 ** -24) * o + n * 2.0 ** -37 * 1.5 + 2.0 ** -25
+    err = np.abs(c.out.double().cpu().numpy() - o)
+    print(f"[sink] n={n} below={below} B={B} L={L}: output {o.max():.2e}, off by {err.max():.2e}, may be {tol.min():.2e}", flush=True)
+    assert (err <= tol).all()
+    assert tol.max() < 0.1 * o.min() or below > 20  # the bound says something
+
+
 @pytest.mark.parametrize("hidden", [False, True])
 @pytest.mark.parametrize("kw", [
     dict(B=2, L=4, H=4, Hkv=2, D=128, prefix=70, lens=[100, 9]),
