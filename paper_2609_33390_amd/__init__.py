@@ -20,6 +20,13 @@ Entry points (same names as the C ABI):
 * :func:`accept_profile` - acceptance profile, tokens per forward and the
   risk-reward position weights from many blocks' accept lengths.
 
+Every call is queued on ``stream`` (a torch stream or a handle), by default the
+current one, and takes an optional ``workspace``.  Without one it uses scratch
+of its own for that stream, or of the graph when the stream is being captured;
+a workspace that the caller passes must not serve two calls at once.  Tensors
+that are made or freed on another stream than the call's are the caller's to
+order, as with every torch operation.
+
 Around the step, on a :class:`KVCache` of paged keys and values:
 
 * :func:`block_attention` - attention of every block (or single token) over a
@@ -256,13 +263,26 @@ def _stream_ptr(device: torch.device, stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-_ws: Dict[Tuple[int, str], torch.Tensor] = {}
+_ws: Dict[Tuple[Optional[int], str, Optional[int]], torch.Tensor] = {}
+# Whether the current stream is being captured, without the Python around it.
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
 
 
-def _workspace(device: torch.device, nbytes: int, tag: str) -> torch.Tensor:
-    """Per-device cached scratch buffer (grown on demand).  Callers that run the
-    same entry point concurrently on several streams must pass their own."""
-    key = (device.index if device.index is not None else torch.cuda.current_device(), tag)
+def _workspace(device: torch.device, nbytes: int, tag: str, stream) -> torch.Tensor:
+    """Scratch of a call on ``stream`` (as the entry points take it): a buffer of
+    the device, entry point and stream, grown on demand, so that calls on
+    different streams share none.  It is allocated on the stream that uses it,
+    so a smaller one is given back in that stream's order.  A call under
+    capture gets memory of the graph instead: replays must not share a buffer
+    with other calls, and it must live as long as the graph."""
+    if stream is not None and _stream_ptr(device, stream) != _stream_ptr(device, None):
+        if not hasattr(stream, "cuda_stream"):     # a handle; 0 is the default stream
+            stream = torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
+            return _workspace(device, nbytes, tag, None)
+    if _capturing():
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    key = (device.index, tag, _stream_ptr(device, None))  # a tensor's device has its index
     buf = _ws.get(key)
     if buf is None or buf.numel() < nbytes:
         buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
@@ -302,7 +322,7 @@ def propose_block(hidden: torch.Tensor, lm_head: torch.Tensor, K: int, *,
     _dev_tensor(cand_logit, "cand_logit", torch.float32, shape=(rows, K), device=dev)
     _dev_tensor(cand_id, "cand_id", torch.int32, shape=(rows, K), device=dev)
     need = propose_workspace_size(rows, d, V, K)
-    ws = workspace if workspace is not None else _workspace(dev, need, "propose")
+    ws = workspace if workspace is not None else _workspace(dev, need, "propose", stream)
     st = lib().brisk_propose_block(_ptr(hidden), _ptr(lm_head), rows, d, V, K, _ptr(cand_logit),
                                    _ptr(cand_id), _ptr(ws), _ws_bytes(ws, dev, need),
                                    _stream_ptr(dev, stream))
@@ -424,7 +444,7 @@ def rerank_workspace_size(corr: Corrector, B: int, L: int, K: int) -> int:
 
 
 def _rerank_args(corr, hidden, ctx_hidden, anchor_tok, lm_head, tok_embed, cand_logit, cand_id, B, L,
-                 want_scores, selected, refined, gamma, resid, workspace):
+                 want_scores, selected, refined, gamma, resid, workspace, stream):
     rows = B * L
     _dev_tensor(hidden, "hidden", torch.bfloat16, 2)
     dev = hidden.device
@@ -459,7 +479,7 @@ def _rerank_args(corr, hidden, ctx_hidden, anchor_tok, lm_head, tok_embed, cand_
         if t is not None:
             _dev_tensor(t, name, torch.float32, shape=shp, device=dev)
     need = rerank_workspace_size(corr, B, L, K)
-    ws = workspace if workspace is not None else _workspace(dev, need, "rerank")
+    ws = workspace if workspace is not None else _workspace(dev, need, "rerank", stream)
     ws_n = _ws_bytes(ws, dev, need)
     out = {"selected": selected}
     for k, v in (("refined", refined), ("gamma", gamma), ("resid", resid)):
@@ -478,7 +498,7 @@ def rerank(corr: Corrector, hidden: torch.Tensor, ctx_hidden: torch.Tensor, anch
     "resid" when ``want_scores`` (or when the caller passes those buffers)."""
     K, d, V, dev, ws, ws_n, out = _rerank_args(corr, hidden, ctx_hidden, anchor_tok, lm_head, tok_embed,
                                                cand_logit, cand_id, B, L, want_scores, selected, refined,
-                                               gamma, resid, workspace)
+                                               gamma, resid, workspace, stream)
     st = lib().brisk_rerank(ctypes.byref(corr.c_struct), _ptr(hidden), _ptr(ctx_hidden),
                             _ptr(anchor_tok), _ptr(lm_head), _ptr(tok_embed), _ptr(cand_logit),
                             _ptr(cand_id), B, L, K, d, V, _ptr(out["selected"]), _ptr(out.get("refined")),
@@ -500,7 +520,7 @@ def rerank_verify(corr: Corrector, hidden: torch.Tensor, ctx_hidden: torch.Tenso
     Returns the rerank outputs plus "accept_len" and "correction" [B] int32."""
     K, d, V, dev, ws, ws_n, out = _rerank_args(corr, hidden, ctx_hidden, anchor_tok, lm_head, tok_embed,
                                                cand_logit, cand_id, B, L, want_scores, selected, refined,
-                                               gamma, resid, workspace)
+                                               gamma, resid, workspace, stream)
     _dev_tensor(verifier, "verifier", torch.int32, shape=(B, L), device=dev)
     if accept_len is None:
         accept_len = torch.empty(B, dtype=torch.int32, device=dev)
@@ -560,7 +580,7 @@ def rerank_finish(corr: Corrector, hidden: torch.Tensor, ctx_hidden: torch.Tenso
     returns what that call returns."""
     K, d, V, dev, ws, ws_n, out = _rerank_args(corr, hidden, ctx_hidden, anchor_tok, lm_head, tok_embed,
                                                cand_logit, cand_id, B, L, want_scores, selected, refined,
-                                               gamma, resid, workspace)
+                                               gamma, resid, workspace, stream)
     if verifier is not None:
         _dev_tensor(verifier, "verifier", torch.int32, shape=(B, L), device=dev)
         if accept_len is None:
@@ -614,7 +634,7 @@ def accept_profile(accept_len: torch.Tensor, M: int, *, eps: float = 0.0,
     _check(lib().brisk_accept_profile_workspace_size(n, M, ctypes.byref(nbytes)),
            "brisk_accept_profile_workspace_size")
     if workspace is None:
-        workspace = _workspace(dev, nbytes.value, "profile")
+        workspace = _workspace(dev, nbytes.value, "profile", stream)
     ws_n = _ws_bytes(workspace, dev, nbytes.value)
     out = {k: torch.empty(M, dtype=torch.float64, device=dev) for k in ("a", "w_raw", "w")}
     out["tpf_fpt"] = torch.empty(2, dtype=torch.float64, device=dev)
@@ -649,7 +669,7 @@ def propose_verify(hidden: torch.Tensor, lm_head: torch.Tensor, rows_prop: int, 
     nbytes = _sz(0)
     _check(lib().brisk_propose_verify_workspace_size(rows_prop, rows_ver, d, V, K, ctypes.byref(nbytes)),
            "brisk_propose_verify_workspace_size")
-    ws = workspace if workspace is not None else _workspace(dev, nbytes.value, "propose")
+    ws = workspace if workspace is not None else _workspace(dev, nbytes.value, "propose", stream)
     st = lib().brisk_propose_verify(_ptr(hidden), _ptr(lm_head), rows_prop, rows_ver, d, V, K,
                                     _ptr(cand_logit) if rows_prop else None,
                                     _ptr(cand_id) if rows_prop else None,
@@ -721,7 +741,7 @@ def spec_verify(ver_hidden: torch.Tensor, lm_head: torch.Tensor, proposal: torch
     nbytes = _sz(0)
     _check(lib().brisk_spec_verify_workspace_size(B, L, V, K, ctypes.byref(nbytes)),
            "brisk_spec_verify_workspace_size")
-    ws = workspace if workspace is not None else _workspace(dev, nbytes.value, "spec")
+    ws = workspace if workspace is not None else _workspace(dev, nbytes.value, "spec", stream)
     ws_n = _ws_bytes(ws, dev, nbytes.value)
     out = {"accept_len": torch.empty(B, dtype=torch.int32, device=dev),
            "correction": torch.empty(B, dtype=torch.int32, device=dev),
@@ -842,7 +862,7 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
     most = cache.max_seq_len if max_seq_len is None else max_seq_len
     need = block_attention_workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
     if workspace is None:
-        workspace = _workspace(dev, need, "attention")
+        workspace = _workspace(dev, need, "attention", stream)
     st = lib().brisk_block_attention(cache._ref, None if pre is None else ctypes.byref(pre), _ptr(q),
                                      row, head, _ptr(block_mask), B, L, H, most, D ** -0.5 if scale is None else scale,
                                      _ptr(out), _ptr(lse), _ptr(workspace), _ws_bytes(workspace, dev, need),
@@ -917,7 +937,7 @@ def cache_evict(cache: KVCache, score: torch.Tensor, pos: torch.Tensor, next_pos
         raise ValueError("new_len must not overlap the cache's seq_len (copy it there after the call) or next_pos")
     need = _evict_workspace_size(cache.B, cache.n_kv_heads, cap, budget)
     if workspace is None:
-        workspace = _workspace(dev, need, "evict")
+        workspace = _workspace(dev, need, "evict", stream)
     st = lib().brisk_cache_evict(cache._ref, cache.B, _ptr(score), _ptr(pos), cap, _ptr(next_pos),
                                  budget, recent, _ptr(score_out), _ptr(pos_out), _ptr(new_len), _ptr(workspace),
                                  _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
@@ -1002,7 +1022,7 @@ def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok:
         _dev_tensor(token, "token", torch.int32, shape=(B,), device=dev)
     need = _draft_workspace_size(B, V)
     if workspace is None:
-        workspace = _workspace(dev, need, "draft")
+        workspace = _workspace(dev, need, "draft", stream)
     st = lib().brisk_draft_verify(_ptr(target_prob), t_stride, _ptr(draft_prob) if L else None, d_stride,
                                   _ptr(draft_tok) if L else None, _ptr(draft_len), _ptr(u_accept) if L else None,
                                   _ptr(noise), n_stride, B, L, V, _ptr(accept_len), _ptr(token), _ptr(workspace),
