@@ -774,7 +774,7 @@ class KVCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor):
         for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
             _half_tensor(t, n, 4)
-        if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride() or v_pages.dtype != k_pages.dtype:
+        if v_pages.shape != k_pages.shape or _steps(v_pages) != _steps(k_pages) or v_pages.dtype != k_pages.dtype:
             raise ValueError("k_pages and v_pages must agree in shape, strides and dtype")
         dev = k_pages.device
         if v_pages.device != dev:
@@ -786,7 +786,7 @@ class KVCache:
         n_pages, self.page_size, self.n_kv_heads, self.d_head = k_pages.shape
         self.B, max_pages = block_table.shape
         self.max_seq_len = max_pages * self.page_size
-        page, slot, head, _ = k_pages.stride()
+        page, slot, head, _ = _steps(k_pages)
         self._c = _KVCacheC(_HALF[self.dtype], self.n_kv_heads, self.d_head, self.page_size, n_pages, max_pages, page,
                             slot, head, _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(seq_len))
         self._ref = ctypes.byref(self._c)
@@ -794,6 +794,11 @@ class KVCache:
     @property
     def c_struct(self) -> _KVCacheC:
         return self._c
+
+
+def _steps(t: torch.Tensor) -> Tuple[int, ...]:
+    """Strides, where a dimension of one element, whose stride nothing uses, has 0."""
+    return tuple(0 if n == 1 else s for n, s in zip(t.shape, t.stride()))
 
 
 def _half_tensor(t: torch.Tensor, name: str, ndim: int, like: Optional[KVCache] = None) -> None:
@@ -823,7 +828,7 @@ def _block_queries(q: torch.Tensor, cache: KVCache, block_mask: Optional[torch.T
         raise ValueError("the rows of q must be evenly spaced: stride(0) == L * stride(1)")
     if block_mask is not None:
         _dev_tensor(block_mask, "block_mask", torch.int64, shape=(B, L), device=cache.device)
-    return B, L, H, (sl if L > 1 else sb if B > 1 else H * sh), (sh if H > 1 else D)
+    return B, L, H, (sl if L > 1 else sb if B > 1 else 0), (sh if H > 1 else 0)
 
 
 def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
@@ -847,10 +852,10 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
         for t, n in ((k, "prefix keys"), (v, "prefix values")):
             _half_tensor(t, n, 3, cache)
         P = k.shape[0]
-        if k.shape[1:] != (cache.n_kv_heads, D) or v.shape != k.shape or (P and v.stride() != k.stride()):
+        if k.shape[1:] != (cache.n_kv_heads, D) or v.shape != k.shape or (P and _steps(v) != _steps(k)):
             raise ValueError(f"prefix must be two tensors [P, {cache.n_kv_heads}, {D}] of the same strides")
         if P:
-            pre = _KVPrefixC(P, k.stride(0), k.stride(1), _ptr(k), _ptr(v))
+            pre = _KVPrefixC(P, *_steps(k)[:2], _ptr(k), _ptr(v))
     if out is None:
         out = torch.empty(B, L, H, D, dtype=cache.dtype, device=dev)
     else:

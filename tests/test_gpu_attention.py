@@ -284,6 +284,30 @@ def test_strided_queries_and_given_buffers():
     _check(one, *a)
 
 
+@pytest.mark.parametrize("kw,q_ones,kv_ones", [
+    (dict(B=1, L=1, H=1, Hkv=1, D=64, prefix=1, lens=[1], page=1, spare_pages=0), (0, 1, 2), (0, 1, 2)),
+    (dict(B=3, L=1, H=4, Hkv=1, D=64, prefix=20, lens=[9, 0, 40], page=16), (1,), (2,)),
+    (dict(B=2, L=3, H=1, Hkv=1, D=128, prefix=1, lens=[9, 40], page=1, mask="causal"), (2,), (1, 2)),
+    (dict(B=1, L=5, H=6, Hkv=2, D=128, prefix=30, lens=[16], page=16, mask="causal", spare_pages=0), (0,), (0,)),
+])
+def test_strides_of_single_elements_do_not_matter(kw, q_ones, kv_ones):
+    """Dimensions of one element come with whatever stride a slice or a transpose left them, keys' and values' apart."""
+    c = Case(seed=33, **kw)
+
+    def odd(t, dims, step):
+        return torch.as_strided(t, t.shape, [step + i if i in dims else s for i, s in enumerate(t.stride())])
+
+    cache = c.cache(brisk)
+    assert all(cache.k_pages.shape[i] == 1 for i in kv_ones) and all(c.q.shape[i] == 1 for i in q_ones)
+    cache = brisk.KVCache(odd(cache.k_pages, kv_ones, 3), odd(cache.v_pages, kv_ones, 77), cache.block_table, cache.seq_len)
+    pre = c.gpu_prefix()
+    ones = tuple(i for i in (0, 1) if pre[0].shape[i] == 1)
+    out = brisk.block_attention(odd(c.q.cuda(), q_ones, 5), cache, prefix=(odd(pre[0], ones, 3), odd(pre[1], ones, 77)),
+                                block_mask=c.gpu_mask())
+    torch.cuda.synchronize()
+    _check(c, *out)
+
+
 def test_length_bound_and_table_are_clamped():
     """Lengths beyond the bound are cut to it, negative ones count as none, bad page ids stay inside the pool."""
     c = Case(2, 1, 4, 4, 64, None, [40, 24], seed=10, junk=0.0)
