@@ -576,7 +576,8 @@ int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap,
  *   ws          device scratch of brisk_cache_evict_workspace_size bytes
  *
  * No output, nor ws, may overlap another output or an input (next_pos, seq_len
- * and block_table among them): BRISK_ERR_UNSUPPORTED.
+ * and block_table among them), and no two places of the pages one another (as
+ * where heads are one expanded head): BRISK_ERR_UNSUPPORTED.
  * Limits: the cache's; B >= 1, B * n_kv_heads <= 2^20, 1 <= cap <= 2^24,
  * B * n_kv_heads * cap <= 2^36, budget >= 1, 0 <= recent <= budget; lengths
  * are cut to cap.  Two sequences

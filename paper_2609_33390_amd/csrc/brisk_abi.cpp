@@ -3,7 +3,9 @@
 // an error return has launched nothing and touched no output.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
+#include <iterator>
 
 #include "brisk.h"
 #include "kernels.h"
@@ -63,6 +65,22 @@ int attention_shape_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_he
   const int st = block_rows_check(B, L, n_heads, n_kv_heads);
   if (st != BRISK_OK) return st;
   return d_head % 8 != 0 ? BRISK_ERR_UNSUPPORTED : BRISK_OK;
+}
+
+// Whether no two places of the pages are the same memory, as far as nested strides tell: each
+// dimension, from the smallest stride on, steps past all that the ones before span.
+bool places_apart(const brisk_kv_cache* c) {
+  struct Dim {
+    int64_t size, stride;
+  } d[] = {{c->n_kv_heads, c->head_stride}, {c->page_size, c->slot_stride}, {c->n_pages, c->page_stride}};
+  std::sort(std::begin(d), std::end(d), [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  __int128 span = c->d_head;  // elements, from the first place to the end of the last
+  for (const Dim& x : d) {
+    if (x.size == 1) continue;
+    if (x.stride < span) return false;
+    span += static_cast<__int128>(x.size - 1) * x.stride;
+  }
+  return true;
 }
 
 // A device buffer of a call, for the question whether two of them share memory.
@@ -572,7 +590,7 @@ int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score
   if (st != BRISK_OK) return st;
   if (recent < 0 || recent > budget) return BRISK_ERR_SHAPE;
   if (!aligned4(score_in) || !aligned4(pos_in) || !aligned4(next_pos) || !aligned4(score_out) ||
-      !aligned4(pos_out) || !aligned4(new_len))
+      !aligned4(pos_out) || !aligned4(new_len) || !places_apart(cache))
     return BRISK_ERR_UNSUPPORTED;
   const size_t need = brisk::evict_workspace_bytes(B, cache->n_kv_heads, cap, budget);
   if (ws_bytes < need || !ws) return BRISK_ERR_WORKSPACE;

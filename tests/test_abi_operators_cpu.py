@@ -144,6 +144,19 @@ def test_evict_refuses_overlapping_buffers(kw):
     assert _evict(_cache(seq_len=LENS, block_table=TABLE), **{**APART, **kw}) == EUNSUP
 
 
+@pytest.mark.parametrize("kw,bad", [
+    (dict(head_stride=0), True), (dict(slot_stride=0), True), (dict(page_stride=0), True),       # expanded dimensions
+    (dict(head_stride=120), True), (dict(slot_stride=1016), True), (dict(page_stride=64 * 1024 - 8), True),
+    (dict(page_stride=64 * 1024, slot_stride=128, head_stride=64 * 128), False),                  # head-major pages
+    (dict(page_stride=128, slot_stride=12800, head_stride=64 * 12800), False),                    # pages innermost
+    (dict(n_kv_heads=1, head_stride=0), False), (dict(page_size=1, slot_stride=0), False),
+    (dict(n_pages=1, page_stride=0), False), (dict(page_stride=1 << 62), False),
+])
+def test_evict_refuses_pages_that_share_memory(kw, bad):
+    """Where two heads are one in memory each would move rows under the other; reading them is fine."""
+    assert _evict(_cache(**kw), ws_bytes=0) == (EUNSUP if bad else EWS)
+
+
 def _draft(**kw):
     a = dict(t=FAKE, ts=1000, d=FAKE, ds=1000, tok=FAKE, n=None, u=FAKE, e=FAKE, es=1000, B=4, L=8, V=1000, acc=FAKE,
              out=FAKE, ws=FAKE, ws_bytes=BIG)

@@ -289,3 +289,16 @@ def test_binding_refuses_lengths_cut_in_place():
     with pytest.raises(brisk.BriskError) as err:                # and whatever else shares memory, by the library
         brisk.cache_evict(cache, s, p, n, 10, 2, score_out=p.view(torch.float32))
     assert err.value.status == -3
+
+
+def test_evict_refuses_expanded_heads():
+    """Two heads that are one in memory: each would move rows under the other."""
+    e = EvictCase([40, 30], 10, 2, seed=25)
+    one = e.c.cache(brisk)
+    k, v = (x[:, :, :1].expand(-1, -1, 2, -1) for x in (one.k_pages, one.v_pages))
+    before = k.clone()
+    with pytest.raises(brisk.BriskError) as err:
+        e.run(brisk.KVCache(k, v, one.block_table, one.seq_len))
+    assert err.value.status == -3
+    torch.cuda.synchronize()
+    assert torch.equal(k.clone().view(torch.int16), before.view(torch.int16))
