@@ -540,8 +540,9 @@ int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* pr
  *   lse         [B*L, n_heads] fp32
  *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array
  *
- * Limits as brisk_block_attention; 1 <= cap <= 2^30, B * n_kv_heads * cap <=
- * 2^36; lengths are cut to cap.
+ * Limits as brisk_block_attention; 1 <= cap <= 2^30, and the launch holds fewer
+ * than 2^24 workgroups: B * n_kv_heads * ceil(cap / 1024) < 2^24; lengths are
+ * cut to cap.
  * Deterministic (fixed-order sums, no atomics).
  */
 int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_row_stride,
@@ -579,9 +580,11 @@ int brisk_cache_evict_workspace_size(int32_t B, int32_t n_kv_heads, int32_t cap,
  * and block_table among them), and no two places of the pages one another (as
  * where heads are one expanded head): BRISK_ERR_UNSUPPORTED.
  * Limits: the cache's; B >= 1, B * n_kv_heads <= 2^20, 1 <= cap <= 2^24,
- * B * n_kv_heads * cap <= 2^36, budget >= 1, 0 <= recent <= budget; lengths
- * are cut to cap.  Two sequences
- * must not share a page that holds slots below budget of either.
+ * B * n_kv_heads * cap <= 2^36, budget >= 1, 0 <= recent <= budget, and what
+ * a launch holds: B * n_kv_heads * ceil(min(budget, cap - budget) / 64) < 2^24
+ * and, past 32768 slots, B * n_kv_heads * ceil(cap / 4096) < 2^22 (at most 64
+ * counted of the last quotient).  Lengths are cut to cap.  Two sequences must
+ * not share a page that holds slots below budget of either.
  */
 int brisk_cache_evict(const brisk_kv_cache* cache, int32_t B, const float* score_in,
                       const int32_t* pos_in, int32_t cap, const int32_t* next_pos, int32_t budget,

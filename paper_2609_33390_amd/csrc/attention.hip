@@ -542,11 +542,13 @@ int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 1
 // 512 keys.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
 // runs of 512 keys 119, of 256 147.)
 struct Runs { int count, keys; };
+constexpr int64_t kMostRuns = 1 << 20;
 Runs runs_of(int keys, int64_t whole, TileShape t) {
   Runs best{};
   double least = 1e300;
   for (int s = 1; s <= 64; ++s) {
     const int run = ceil_div(ceil_div(keys, s), t.keys) * t.keys, count = ceil_div(keys, run);
+    if (s > 1 && whole * count > kMostRuns) break;  // thousands of rounds: nothing to fill, and a launch has its limit
     const double cost = ((whole * count + t.slots - 1) / t.slots) * (run + 512.0);
     if (cost < least) {
       least = cost;

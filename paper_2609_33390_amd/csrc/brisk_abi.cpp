@@ -96,7 +96,7 @@ bool overlap(Span a, Span b) {
 int evict_shape_check(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget) {
   if (B < 1 || n_kv_heads < 1 || n_kv_heads > 1024 || static_cast<int64_t>(B) * n_kv_heads > kMaxRows ||
       cap < 1 || cap > kMaxEvictCap || budget < 1 ||
-      static_cast<int64_t>(B) * n_kv_heads * cap > kMaxScores)
+      static_cast<int64_t>(B) * n_kv_heads * cap > kMaxScores || !brisk::evict_launchable(B, n_kv_heads, cap, budget))
     return BRISK_ERR_SHAPE;
   return BRISK_OK;
 }
@@ -545,7 +545,8 @@ int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_
   st = block_rows_check(B, L, n_heads, cache->n_kv_heads);
   if (st != BRISK_OK) return st;
   if (cap < 1 || cap > kMaxSlots || static_cast<int64_t>(B) * cache->n_kv_heads * cap > kMaxScores ||
-      q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) || scale > kMaxScale)
+      q_row_stride < 0 || q_head_stride < 0 || !(scale > 0.f) || scale > kMaxScale ||
+      !brisk::score_launchable(B, cache->n_kv_heads, cap))
     return BRISK_ERR_SHAPE;
   if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned8(block_mask) ||
       !aligned4(lse) || !aligned4(score_in) || !aligned4(score_out))

@@ -475,8 +475,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_chunk_kernel(EvictArgs a
 }
 
 // Moves listed rows, 16 lanes a row and kRowsInFlight rows at once.
-constexpr int kRowsInFlight = 4, kMoveRows = 16 * kRowsInFlight;
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
+constexpr int kMoveThreads = 256, kRowsInFlight = 4, kMoveRows = kMoveThreads / 16 * kRowsInFlight;
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   const int heads = a.B * a.Hkv, bh = blockIdx.x % heads, r0 = blockIdx.x / heads * kMoveRows;
   const int count = a.count[bh];
   if (r0 >= count) return;
@@ -511,18 +511,27 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
   }
 }
 
+// A launch has fewer than 2^32 threads.
+bool launchable(int64_t workgroups, int threads) { return workgroups * threads < int64_t{1} << 32; }
+
 // Tiles of a wavefront: eight, so that its start and its queries are paid once
 // for 256 keys, unless that leaves CUs without a workgroup.
+struct ScoreRuns { int tiles, runs; };
+ScoreRuns score_runs(int64_t whole, int cap) {
+  auto runs_of = [&](int t) { return (cap + kScoreWaves * t * 32 - 1) / (kScoreWaves * t * 32); };
+  int tiles = kMaxTiles;
+  while (tiles > 1 && whole * runs_of(tiles) < 512) tiles /= 2;
+  return {tiles, runs_of(tiles)};
+}
+
 template <bool F16>
 void launch_score(const ScoreArgs& a, hipStream_t s) {
   const int64_t whole = static_cast<int64_t>(a.B) * a.Hkv;
-  int tiles = kMaxTiles;
-  auto runs_of = [&](int t) { return (a.cap + kScoreWaves * t * 32 - 1) / (kScoreWaves * t * 32); };
-  while (tiles > 1 && whole * runs_of(tiles) < 512) tiles /= 2;
-  const int runs = runs_of(tiles);
+  const auto [tiles, runs] = score_runs(whole, a.cap);
   const dim3 grid(static_cast<uint32_t>(whole * runs)), threads(64 * kScoreWaves);
   const bool two = a.L * (a.H / a.Hkv) > 32;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, s, a, tiles); };
+  const int per = tiles;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, s, a, per); };
   switch (head_slices(a.D)) {
     case 2: two ? go(score_kernel<F16, 2, 2>) : go(score_kernel<F16, 2, 1>); break;
     case 3: two ? go(score_kernel<F16, 3, 2>) : go(score_kernel<F16, 3, 1>); break;
@@ -531,6 +540,11 @@ void launch_score(const ScoreArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+bool score_launchable(int B, int Hkv, int cap) {
+  const int64_t whole = static_cast<int64_t>(B) * Hkv;
+  return launchable(whole * score_runs(whole, cap).runs, 64 * kScoreWaves);
+}
 
 void launch_cache_score(const ScoreArgs& a, bool f16, hipStream_t s) {
   if (f16)
@@ -560,6 +574,12 @@ struct EvictSpace {
 };
 }  // namespace
 
+bool evict_launchable(int B, int Hkv, int cap, int budget) {
+  const int64_t heads = static_cast<int64_t>(B) * Hkv;
+  const int moves = (evict_list_len(cap, budget) + kMoveRows - 1) / kMoveRows;
+  return launchable(heads * (cap > kLdsSlots ? evict_chunks(cap) : 1), kSelectThreads) && launchable(heads * moves, kMoveThreads);
+}
+
 size_t evict_workspace_bytes(int B, int Hkv, int cap, int budget) {
   return EvictSpace(B, Hkv, cap, budget).words * sizeof(uint32_t);
 }
@@ -587,7 +607,7 @@ void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s) {
   }
   if (a.list_len > 0) {
     const uint32_t runs = (a.list_len + kMoveRows - 1) / kMoveRows;
-    hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(evict_move_kernel, dim3(heads * runs), dim3(kMoveThreads), 0, s, a);
   }
 }
 

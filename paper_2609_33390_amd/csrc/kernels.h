@@ -113,6 +113,7 @@ struct ScoreArgs {
   int B, L, H, Hkv, D, cap;
   float scale, decay;
 };
+bool score_launchable(int B, int Hkv, int cap);    // one launch holds the call's workgroups
 void launch_cache_score(const ScoreArgs& a, bool f16, hipStream_t s);
 
 struct EvictArgs {
@@ -128,6 +129,7 @@ struct EvictArgs {
   int B, Hkv, D, cap, budget, recent, list_len;
 };
 int evict_list_len(int cap, int budget);
+bool evict_launchable(int B, int Hkv, int cap, int budget);
 size_t evict_workspace_bytes(int B, int Hkv, int cap, int budget);
 void launch_cache_evict(EvictArgs a, void* ws, hipStream_t s);
 

@@ -157,6 +157,29 @@ def test_evict_refuses_pages_that_share_memory(kw, bad):
     assert _evict(_cache(**kw), ws_bytes=0) == (EUNSUP if bad else EWS)
 
 
+def test_calls_that_no_launch_holds_are_refused():
+    """2^32 threads or more: refused as a shape, before anything is launched."""
+    one = dict(n_kv_heads=1, max_pages=1 << 14, page_size=1 << 16)
+    assert _score(_cache(**one), B=1 << 24, L=1, H=1, cap=1) == ESHAPE
+    assert _score(_cache(**one), B=1 << 14, L=1, H=1, cap=1 << 20) == ESHAPE
+    assert _score(_cache(**one), B=1 << 16, L=1, H=1, cap=1 << 20) == ESHAPE
+    size = brisk.lib().brisk_cache_evict_workspace_size
+    for B, Hkv, cap, budget, want in ((1 << 10, 8, 1 << 21, 1 << 20, ESHAPE), (1 << 10, 8, 1 << 18, 1 << 17, ESHAPE),
+                                      (1 << 10, 8, (1 << 18) - 128, 1 << 16, 0), (1 << 10, 8, 1 << 21, 1000, 0),
+                                      (1 << 20, 1, 33000, 1, ESHAPE), (1 << 18, 1, 33000, 1, 0)):
+        n = ctypes.c_size_t(77)
+        assert size(B, Hkv, cap, budget, ctypes.byref(n)) == want, (B, Hkv, cap, budget)
+        assert (n.value == 77) == (want != 0)
+        if want:
+            assert _evict(_cache(n_kv_heads=Hkv), B=B, cap=cap, budget=budget, **{k: APART[k] for k in APART}) == want
+
+
+def test_attention_splits_no_finer_than_a_launch_holds():
+    """Millions of workgroups are not split further, however long their caches may be."""
+    most = (1 << 23) + 1                            # whole caches: one run of each row, no workspace
+    assert brisk.block_attention_workspace_size(most, 1, 1, 1, 8, 0, 1 << 30) == 0
+
+
 def _draft(**kw):
     a = dict(t=FAKE, ts=1000, d=FAKE, ds=1000, tok=FAKE, n=None, u=FAKE, e=FAKE, es=1000, B=4, L=8, V=1000, acc=FAKE,
              out=FAKE, ws=FAKE, ws_bytes=BIG)
