@@ -769,7 +769,8 @@ class KVCache:
     ``block_table`` [B, max_pages] int32 lists each sequence's pages and
     ``seq_len`` [B] int32 the slots it holds, the block in flight included.
     The tensors stay the caller's: lengths and pages may be written between
-    calls."""
+    calls.  Which tensors they are is fixed (the library has their addresses):
+    new lengths are copied into ``seq_len``, and an attribute assigned is refused."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor):
         for t, n in ((k_pages, "k_pages"), (v_pages, "v_pages")):
@@ -790,6 +791,12 @@ class KVCache:
         self._c = _KVCacheC(_HALF[self.dtype], self.n_kv_heads, self.d_head, self.page_size, n_pages, max_pages, page,
                             slot, head, _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(seq_len))
         self._ref = ctypes.byref(self._c)
+        self._fixed = True
+
+    def __setattr__(self, name: str, value) -> None:
+        if getattr(self, "_fixed", False):
+            raise AttributeError(f"{name}: a KVCache keeps its tensors; copy into them or make another cache")
+        object.__setattr__(self, name, value)
 
     @property
     def c_struct(self) -> _KVCacheC:

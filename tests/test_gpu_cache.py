@@ -302,3 +302,16 @@ def test_evict_refuses_expanded_heads():
     assert err.value.status == -3
     torch.cuda.synchronize()
     assert torch.equal(k.clone().view(torch.int16), before.view(torch.int16))
+
+
+def test_a_cache_keeps_its_tensors():
+    """Lengths assigned instead of copied would not reach the library: refused."""
+    e = EvictCase([40, 30], 10, 2, seed=26)
+    cache, (_, _, n) = e.run()
+    old = cache.seq_len
+    for name in ("seq_len", "k_pages", "v_pages", "block_table"):
+        with pytest.raises(AttributeError, match=name):
+            setattr(cache, name, n)
+    assert cache.seq_len is old and cache.c_struct.seq_len == old.data_ptr()
+    old.copy_(n)
+    assert cache.seq_len.tolist() == [10, 10]
