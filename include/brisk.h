@@ -447,7 +447,8 @@ int brisk_accept_profile(const int32_t* accept_len, int32_t n_blocks, int32_t M,
  * Operators around the step: the attention that makes a block's hidden states
  * from a shared prefix and a paged cache, the weights and the eviction that
  * keep that cache short, and verification from given probabilities (Section
- * 2.1 strided decoding, Section 3.3 verification, Algorithm 1(b)).
+ * 2.1 strided decoding, Section 3.3 verification, Algorithm 1(b)).  Where a
+ * call does not say otherwise, its outputs must not overlap its inputs.
  * ---------------------------------------------------------------------------
  */
 typedef enum { BRISK_BF16 = 0, BRISK_F16 = 1 } brisk_dtype;
@@ -538,7 +539,9 @@ int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* pr
  * together); a row with lse = -inf adds nothing.
  *
  *   lse         [B*L, n_heads] fp32
- *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array
+ *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array,
+ *               but score_out may not overlap score_in otherwise, nor the other
+ *               inputs (BRISK_ERR_UNSUPPORTED where the call can tell)
  *
  * Limits as brisk_block_attention; 1 <= cap <= 2^30, and the launch holds fewer
  * than 2^24 workgroups: B * n_kv_heads * ceil(cap / 1024) < 2^24; lengths are

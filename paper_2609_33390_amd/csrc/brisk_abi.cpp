@@ -551,6 +551,13 @@ int brisk_cache_score(const brisk_kv_cache* cache, const uint16_t* q, int64_t q_
   if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned8(block_mask) ||
       !aligned4(lse) || !aligned4(score_in) || !aligned4(score_out))
     return BRISK_ERR_UNSUPPORTED;
+  // A wavefront reads its own slots of score_in before it writes them, but others' at any time.
+  const uint64_t slots = static_cast<uint64_t>(B) * cache->n_kv_heads * cap * 4, seqs = static_cast<uint64_t>(B) * 4;
+  const Span out{score_out, slots};
+  if ((score_out != score_in && overlap(out, {score_in, slots})) || overlap(out, {lse, seqs * L * n_heads}) ||
+      overlap(out, {cache->seq_len, seqs}) || overlap(out, {cache->block_table, seqs * cache->max_pages}) ||
+      (block_mask && overlap(out, {block_mask, 2 * seqs * L})))
+    return BRISK_ERR_UNSUPPORTED;
   a.q = q;
   a.q_row_stride = q_row_stride;
   a.q_head_stride = q_head_stride;

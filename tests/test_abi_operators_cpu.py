@@ -109,6 +109,16 @@ def test_score_validation(kw, want):
     assert _score(**kw) == want
 
 
+@pytest.mark.parametrize("kw", [
+    dict(so=(1 << 24) + 16), dict(so=(1 << 24) - 16), dict(so=2 << 24), dict(so=(2 << 24) + 4 * 16 * 32 * 4 - 4),
+    dict(so=3 << 24), dict(so=4 << 24), dict(so=5 << 24),
+])
+def test_score_refuses_overlapping_buffers(kw):
+    """The whole array may be updated in place, but not one shifted against itself."""
+    apart = dict(si=1 << 24, lse=2 << 24, mask=5 << 24)
+    assert _score(_cache(seq_len=3 << 24, block_table=4 << 24), **{**apart, **kw}) == EUNSUP
+
+
 def _evict(c=None, **kw):
     a = dict(B=4, si=FAKE, pi=FAKE, cap=2048, np_=FAKE, budget=512, recent=16, so=FAKE, po=FAKE, nl=FAKE, ws=FAKE, ws_bytes=BIG)
     a.update(kw)
