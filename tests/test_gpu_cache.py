@@ -215,6 +215,27 @@ def test_evict_long_caches(n, budget, kind):
         assert torch.equal(flat(y.cpu()).view(torch.int16)[:n], want.view(torch.int16)[:n])
 
 
+@pytest.mark.parametrize("kw", [
+    # long, shorter than a chunk, all kept, empty: heads of each over scratch that holds anything
+    dict(lens=[40000, 33, 5000, 0], budget=4500, recent=100, Hkv=3, kind="ties", extra=3),
+    dict(lens=[700, 33500, 20000], budget=20000, recent=0, Hkv=2, kind="any", layout="hnd", dtype="f16"),
+    dict(lens=[32769, 32769, 8193], budget=8192, recent=8192, Hkv=2, kind="mass", page=64),
+    dict(lens=[34000, 36864, 12288], budget=1, recent=1, Hkv=4, kind="equal"),
+])
+def test_evict_batches_of_long_caches(kw):
+    """The passes over long caches with several heads and sequences, some of which keep all."""
+    import ctypes
+    e = EvictCase(D=8, seed=len(str(kw)), **kw)
+    c = e.c
+    n = ctypes.c_size_t()
+    assert e.cap > 32768
+    assert brisk.lib().brisk_cache_evict_workspace_size(c.B, c.Hkv, e.cap, e.budget, ctypes.byref(n)) == 0
+    ws = torch.full((n.value,), 0xFF, dtype=torch.uint8, device="cuda")
+    print(f"[evict] {kw}", flush=True)
+    cache, got = e.run(workspace=ws)
+    _check_evict(e, cache, got)
+
+
 def test_evict_twice_and_inside_its_buffers():
     """The inputs stay as they are, so a second call gives the same; nothing outside the buffers is written."""
     from test_gpu_canary import Guarded
