@@ -536,7 +536,8 @@ int brisk_block_attention(const brisk_kv_cache* cache, const brisk_kv_prefix* pr
  *                        that see j of exp(scale * <q, k_j> - lse)
  * and 0 for n <= j < cap.  q, block_mask, lse and L as given to and left by
  * brisk_block_attention (so the weights are those over prefix and cache
- * together); a row with lse = -inf adds nothing.
+ * together); a row with lse = -inf adds nothing.  A weight carries the rounding
+ * of its row's lse in fp32: a factor within about 1 +- 2^-22 |lse|.
  *
  *   lse         [B*L, n_heads] fp32
  *   score_in, score_out  [B, n_kv_heads, cap] fp32; they may be the same array,
@@ -610,7 +611,8 @@ int brisk_draft_verify_workspace_size(int32_t B, int32_t V, size_t* bytes);
  *   w = [target_prob[b, a] - draft_prob[b, a]]_+ when a < n, or
  *       target_prob[b, a] when a = n or when that difference is positive nowhere;
  *   token[b] = argmax_v w_v / noise[b, v] over the v with w_v > 0, the lower
- *       id on ties; -1 when there is none.
+ *       id on ties; -1 when no such ratio is positive (in fp32: one that
+ *       underflows to 0, or is NaN, is not).
  * With noise drawn from Exp(1), token follows the law w / sum w, so committed
  * tokens keep the target's law.
  *

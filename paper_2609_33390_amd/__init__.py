@@ -1011,7 +1011,7 @@ def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok:
     [B, V] Exp(1) variates, ``draft_len`` [B] for drafts of different lengths.
     Returns (accept_len [B], token [B]) int32: the accepted prefix of each draft
     and the token after it, drawn from [p - q]_+ after a rejection and from the
-    target's next row after a full acceptance (-1 if no weight is positive)."""
+    target's next row after a full acceptance (-1 if no weight over its variate is positive)."""
     _dev_tensor(draft_tok, "draft_tok", torch.int32, 2)
     B, L = draft_tok.shape
     dev = draft_tok.device

@@ -19,7 +19,7 @@
 //
 // Keys and values come to LDS by asynchronous copies, a tile ahead.  Few rows
 // are bound by the read of the cache: 64 sequences x 8 heads x 2048 keys of 128
-// elements, 32 rows each, run at 5.0 TB/s (a large copy: 4.8), 64 rows at 5.1.
+// elements, 32 rows each, run at 5.1 TB/s (a large copy: 4.9), 64 rows at 5.0.
 // Many rows are bound by the matrix cores and by what feeds them from LDS: 32768
 // rows (4096 a key head) over 16384 shared keys, 275 GFLOP, take 0.32 ms, 0.85
 // PFLOP/s where a library product of 8192^3 reaches 1.19; with the LDS reads left
@@ -39,7 +39,7 @@ constexpr int kCUs = 256;
 // kLift higher than that, which l and the log-sum-exp share.  f16 has no steps below 2^-24, so its
 // probabilities use its range from the top: at most 2^15, and a key's weight is off by at most
 // 2^-37 of the largest one's, besides its rounding to 11 bits (unlifted, 65536 keys of 2^-25 of the
-// largest weight, 0.2% together, were lost).  bf16 has the range of fp32.
+// largest weight, 0.2% of it together, count as nothing).  bf16 has the range of fp32.
 template <bool F16> constexpr float kLag = F16 ? 3.f : 8.f;
 template <bool F16> constexpr float kLift = F16 ? 12.f : 0.f;
 constexpr float kFine = 0x1p20f;   // up to here a float holds a subtracted logit to 2^-5
@@ -538,8 +538,9 @@ constexpr TileShape kShapes[] = {{32, 64, 2 * kCUs}, {64, 64, 2 * kCUs}, {128, 6
 int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
 
 // Runs of `keys` keys that `whole` workgroups would cover: the fewest rounds of
-// workgroups, where each pays for its start and for the join about as much as for
-// 512 keys.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
+// workgroups, each counted as its keys and 512 for its start.  What that constant is
+// hardly matters (64 to 1500 plan the timing cases alike): the rule fills a round,
+// and weighs neither rows nor the bytes of the partial sums.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
 // runs of 512 keys 119, of 256 147.)
 struct Runs { int count, keys; };
 constexpr int64_t kMostRuns = 1 << 20;
