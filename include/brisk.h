@@ -16,8 +16,8 @@
  * part can overlap the LM-head pass.
  *
  * Further down stand the operators around the step: attention over a shared
- * prefix and a paged cache, that cache's eviction, and verification of drafts
- * from given probabilities.
+ * prefix and a paged cache, that cache's eviction, verification of drafts
+ * from given probabilities, and a cache held in 4 bits.
  *
  * Conventions shared by every entry point
  *   - Every pointer argument is a DEVICE pointer owned by the caller, except
@@ -633,6 +633,100 @@ int brisk_draft_verify(const float* target_prob, int64_t target_stride, const fl
                        const float* u_accept, const float* noise, int64_t noise_stride, int32_t B,
                        int32_t L, int32_t V, int32_t* accept_len, int32_t* token, void* ws,
                        size_t ws_bytes, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * A key/value cache in 4 bits: writing tokens to it, reading them back, and the
+ * attention over it.  It holds 4.25 bits an element (heads of 64 or 128) where
+ * brisk_kv_cache holds 16.
+ *
+ * Each head of each token, key and value apart, is held as z + s c:
+ *   z   = min_d x_d
+ *   s   = type(fl((max_d x_d - z) / 15)), 0 where that is no normal bf16 number
+ *         (in fp16, where it rounds to 0)
+ *   c_d = min(rne(fl(x_d - z) / s), 15), 0 where s = 0
+ * with fl the rounding to fp32, type that to the cache's type (both to nearest
+ * even) and rne the nearest whole number, the even one on ties.  Elements are off
+ * by at most (1/2 + 2^-5) s where s is a normal number.  A head with an element, or
+ * a range, that is not finite is held as z = NaN, s = 0.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * A paged cache in 4 bits (host struct of a device pointer and sizes).  Slot j
+ * of sequence b lies in page block_table[b, j / page_size] at place
+ * j % page_size; a page's part for key/value head h is the page_size (w + 8) bytes
+ * from byte page * page_stride + h * head_stride of `pages` on, w = 64 for d_head
+ * <= 64, else 128.  What the bytes mean is the library's own: they are written
+ * by brisk_kv4_write and read by brisk_kv4_read and brisk_kv4_attention, and may be
+ * copied whole.  Page ids are clamped into [0, n_pages), lengths into what the
+ * table addresses.
+ *
+ * Limits: 1 <= n_kv_heads <= 1024; d_head a multiple of 8 in [8, 128];
+ * page_size a power of two in [16, 65536]; n_pages, max_pages >= 1; max_pages *
+ * page_size <= 2^30; strides non-negative multiples of 16; pages 16-byte aligned.
+ */
+typedef struct brisk_kv4_cache {
+  int32_t dtype;             /* brisk_dtype of what is written, read, and of queries and outputs */
+  int32_t n_kv_heads, d_head, page_size, n_pages, max_pages;
+  int64_t page_stride, head_stride;                /* in bytes                */
+  uint8_t* pages;
+  const int32_t* block_table;  /* [B, max_pages]                              */
+  const int32_t* seq_len;      /* [B] slots held, the block's own included    */
+} brisk_kv4_cache;
+
+/* Bytes of a page's part for one head (written to *bytes). */
+int brisk_kv4_page_bytes(int32_t page_size, int32_t d_head, size_t* bytes);
+
+/*
+ * Writes tokens to the cache.  Token t < count[b] of sequence b goes to slot
+ * first[b] + t; slots outside [0, max_pages * page_size) are passed over, and all
+ * other slots keep what they hold.  seq_len is not read: the caller sets it
+ * before or after.
+ *
+ *   k, v        element b * seq_stride + t * row_stride + h * head_stride starts
+ *               the d_head contiguous elements of a head, in the cache's type;
+ *               strides non-negative multiples of 8
+ *   first       [B] int32;  count [B] int32, nullable (T of every sequence; values are
+ *               clamped into [0, T])
+ *
+ * No two tokens of a call may go to the same place (nor, then, two sequences share
+ * a page that both write to).  Limits: the cache's; B >= 1, 1 <= T <= 2^30, and
+ * what a launch holds: B * n_kv_heads * ((T + 30) / 16) < 2^25.  The pages must
+ * overlap none of the inputs, nor two parts of them one another (heads less than a
+ * part apart): BRISK_ERR_UNSUPPORTED where the call can tell.
+ */
+int brisk_kv4_write(const brisk_kv4_cache* cache, const uint16_t* k, const uint16_t* v,
+                    int64_t seq_stride, int64_t row_stride, int64_t head_stride, int32_t B, int32_t T,
+                    const int32_t* first, const int32_t* count, void* stream);
+
+/*
+ * Reads T slots of every sequence back, from slot first[b] on (0 where first is
+ * NULL): k and v [B, T, n_kv_heads, d_head] get type(fl(z + s c)), and 0 for slots
+ * outside [0, seq_len[b]).  Limits as brisk_kv4_write.
+ */
+int brisk_kv4_read(const brisk_kv4_cache* cache, int32_t B, int32_t T, const int32_t* first,
+                   uint16_t* k, uint16_t* v, void* stream);
+
+/* Workspace bytes brisk_kv4_attention needs (written to *bytes). */
+int brisk_kv4_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads,
+                                       int32_t d_head, int32_t prefix_len, int32_t max_seq_len,
+                                       size_t* bytes);
+
+/*
+ * brisk_block_attention with the sequences' own keys and values, those of the
+ * block among them, in 4 bits: z + s c as held, without a rounding to the cache's
+ * type.  The prefix is in 2 bytes, as there (the batch holds it once).  Arguments,
+ * masks, empty rows, hidden slots and the roundings of the results are those of
+ * brisk_block_attention (weights are rounded to the cache's type where they meet
+ * the codes).
+ *
+ * Limits as there, with B * L * n_heads <= 2^22.  Deterministic.
+ */
+int brisk_kv4_attention(const brisk_kv4_cache* cache, const brisk_kv_prefix* prefix, const uint16_t* q,
+                        int64_t q_row_stride, int64_t q_head_stride, const uint64_t* block_mask,
+                        int32_t B, int32_t L, int32_t n_heads, int32_t max_seq_len, float scale,
+                        uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,12 @@ Around the step, on a :class:`KVCache` of paged keys and values:
 * :func:`cache_evict` - eviction by that weight, in place;
 * :func:`draft_verify` - verification of drafted tokens against given
   probabilities, with the random numbers given.
+
+On a :class:`KVCache4`, whose keys and values are held in 4 bits:
+
+* :func:`kv4_write` - new tokens' keys and values into it;
+* :func:`kv4_read` - what it holds, as 2-byte keys and values;
+* :func:`kv4_attention` - :func:`block_attention` over it.
 """
 from __future__ import annotations
 
@@ -49,6 +55,7 @@ import torch
 __all__ = ["BriskError", "Corrector", "propose_block", "propose_block_noalloc", "propose_lmhead", "propose_merge", "rerank", "rerank_verify", "rerank_hoist", "rerank_finish", "verify_accept", "accept_profile",
            "propose_verify", "verify_commit", "corrector_loss", "spec_verify",
            "KVCache", "block_attention", "cache_score", "cache_evict", "draft_verify",
+           "KVCache4", "kv4_page_bytes", "kv4_write", "kv4_read", "kv4_attention",
            "lib", "LIB_PATH", "ABI_SYMBOLS", "propose_workspace_size", "rerank_workspace_size"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbrisk.so")
@@ -63,7 +70,9 @@ ABI_SYMBOLS = ("brisk_status_str", "brisk_abi_version", "brisk_propose_workspace
                "brisk_accept_profile", "brisk_corrector_tables_size", "brisk_corrector_prepare",
                "brisk_block_attention_workspace_size", "brisk_block_attention", "brisk_cache_score",
                "brisk_cache_evict_workspace_size", "brisk_cache_evict",
-               "brisk_draft_verify_workspace_size", "brisk_draft_verify")
+               "brisk_draft_verify_workspace_size", "brisk_draft_verify",
+               "brisk_kv4_page_bytes", "brisk_kv4_write", "brisk_kv4_read",
+               "brisk_kv4_attention_workspace_size", "brisk_kv4_attention")
 PSI_FIELDS = ("A_h", "A_e", "P_h", "P_e", "pos_emb", "P_phi", "W_z", "W_h", "W_s", "W_c", "w_g")
 
 _p = ctypes.c_void_p
@@ -89,6 +98,12 @@ class _KVCacheC(ctypes.Structure):
     _fields_ = ([(n, _i32) for n in ("dtype", "n_kv_heads", "d_head", "page_size", "n_pages", "max_pages")]
                 + [(n, ctypes.c_int64) for n in ("page_stride", "slot_stride", "head_stride")]
                 + [(n, _p) for n in ("k_pages", "v_pages", "block_table", "seq_len")])
+
+
+class _KVCache4C(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("dtype", "n_kv_heads", "d_head", "page_size", "n_pages", "max_pages")]
+                + [(n, ctypes.c_int64) for n in ("page_stride", "head_stride")]
+                + [(n, _p) for n in ("pages", "block_table", "seq_len")])
 
 
 class _KVPrefixC(ctypes.Structure):
@@ -187,6 +202,17 @@ def lib() -> ctypes.CDLL:
             L.brisk_draft_verify.restype = ctypes.c_int
             L.brisk_draft_verify.argtypes = [_p, _i64, _p, _i64, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p,
                                              _sz, _p]
+            _cache4 = ctypes.POINTER(_KVCache4C)
+            L.brisk_kv4_page_bytes.restype = ctypes.c_int
+            L.brisk_kv4_page_bytes.argtypes = [_i32, _i32, _szp]
+            L.brisk_kv4_write.restype = ctypes.c_int
+            L.brisk_kv4_write.argtypes = [_cache4, _p, _p, _i64, _i64, _i64, _i32, _i32, _p, _p, _p]
+            L.brisk_kv4_read.restype = ctypes.c_int
+            L.brisk_kv4_read.argtypes = [_cache4, _i32, _i32, _p, _p, _p, _p]
+            L.brisk_kv4_attention_workspace_size.restype = ctypes.c_int
+            L.brisk_kv4_attention_workspace_size.argtypes = [_i32] * 7 + [_szp]
+            L.brisk_kv4_attention.restype = ctypes.c_int
+            L.brisk_kv4_attention.argtypes = [_cache4] + L.brisk_block_attention.argtypes[1:]
             _lib = L
         return _lib
 
@@ -852,6 +878,14 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
     ``max_seq_len`` a host bound of the lengths.  Returns (out [B, L, H, D],
     lse [B, L, H] fp32); a row that sees no key gets zeros and -inf."""
     B, L, H, row, head = _block_queries(q, cache, block_mask)
+    return _attend(lib().brisk_block_attention, "brisk_block_attention", block_attention_workspace_size, "attention", q,
+                   cache, prefix, block_mask, scale, max_seq_len, out, lse, workspace, stream, (B, L, H, row, head))
+
+
+def _attend(entry, where, workspace_size, tag, q, cache, prefix, block_mask, scale, max_seq_len, out, lse, workspace,
+            stream, rows) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention over either cache: the arguments past the queries checked, outputs and scratch made, the call."""
+    B, L, H, row, head = rows
     dev, D = cache.device, cache.d_head
     pre, P = None, 0
     if prefix is not None:
@@ -872,14 +906,13 @@ def block_attention(q: torch.Tensor, cache: KVCache, *, prefix: Optional[Tuple[t
     else:
         _dev_tensor(lse, "lse", torch.float32, shape=(B, L, H), device=dev)
     most = cache.max_seq_len if max_seq_len is None else max_seq_len
-    need = block_attention_workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
+    need = workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
     if workspace is None:
-        workspace = _workspace(dev, need, "attention", stream)
-    st = lib().brisk_block_attention(cache._ref, None if pre is None else ctypes.byref(pre), _ptr(q),
-                                     row, head, _ptr(block_mask), B, L, H, most, D ** -0.5 if scale is None else scale,
-                                     _ptr(out), _ptr(lse), _ptr(workspace), _ws_bytes(workspace, dev, need),
-                                     _stream_ptr(dev, stream))
-    _check(st, "brisk_block_attention")
+        workspace = _workspace(dev, need, tag, stream)
+    st = entry(cache._ref, None if pre is None else ctypes.byref(pre), _ptr(q), row, head, _ptr(block_mask), B, L, H,
+               most, D ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(workspace),
+               _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
+    _check(st, where)
     return out, lse
 
 
@@ -1041,3 +1074,136 @@ def draft_verify(target_prob: torch.Tensor, draft_prob: torch.Tensor, draft_tok:
                                   _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
     _check(st, "brisk_draft_verify")
     return accept_len, token
+
+
+# ------------------------------------------------------- the cache in 4 bits
+@functools.lru_cache(maxsize=1024)
+def kv4_page_bytes(page_size: int, d_head: int) -> int:
+    """Bytes of a page's part for one head: the last dimension of a :class:`KVCache4`'s pages."""
+    out = _sz()
+    _check(lib().brisk_kv4_page_bytes(page_size, d_head, ctypes.byref(out)), "brisk_kv4_page_bytes")
+    return out.value
+
+
+class KVCache4:
+    """Paged keys and values of a batch of sequences, held in 4 bits.
+
+    ``pages`` is [n_pages, n_kv_heads, kv4_page_bytes(page_size, d_head)] uint8,
+    contiguous in its last dimension (pages and heads may lie further apart);
+    ``dtype`` (bfloat16 or float16) is that of the keys and values written and
+    read and of the queries.  ``block_table`` [B, max_pages] int32 lists each
+    sequence's pages and ``seq_len`` [B] int32 the slots it holds, the block in
+    flight included.  The tensors stay the caller's, as with :class:`KVCache`:
+    lengths and pages may be written between calls, which tensors they are is
+    fixed."""
+
+    def __init__(self, pages: torch.Tensor, block_table: torch.Tensor, seq_len: torch.Tensor, d_head: int,
+                 dtype: torch.dtype = torch.bfloat16):
+        if not isinstance(pages, torch.Tensor):
+            raise TypeError("pages must be a torch.Tensor")
+        if pages.dtype != torch.uint8:
+            raise TypeError(f"pages must be torch.uint8, got {pages.dtype}")
+        if dtype not in _HALF:
+            raise TypeError(f"dtype must be bfloat16 or float16, got {dtype}")
+        if pages.dim() != 3:
+            raise ValueError(f"pages must have 3 dims, got shape {tuple(pages.shape)}")
+        if pages.numel() and pages.stride(-1) != 1:
+            raise ValueError("pages must be contiguous in its last dimension")
+        if not pages.is_cuda:
+            raise ValueError(f"pages must live on a HIP device, got {pages.device}")
+        n_pages, self.n_kv_heads, part = pages.shape
+        slot = kv4_page_bytes(16, d_head) // 16
+        if part % slot or kv4_page_bytes(part // slot, d_head) != part:
+            raise ValueError(f"pages of {part} bytes a head hold no whole number of slots of {slot} bytes")
+        dev = pages.device
+        _dev_tensor(block_table, "block_table", torch.int32, 2, device=dev)
+        _dev_tensor(seq_len, "seq_len", torch.int32, shape=(block_table.shape[0],), device=dev)
+        self.pages, self.block_table, self.seq_len = pages, block_table, seq_len
+        self.device, self.dtype, self.d_head, self.page_size = dev, dtype, d_head, part // slot
+        self.B, max_pages = block_table.shape
+        self.max_seq_len = max_pages * self.page_size
+        self._c = _KVCache4C(_HALF[dtype], self.n_kv_heads, d_head, self.page_size, n_pages, max_pages,
+                             *_steps(pages)[:2], _ptr(pages), _ptr(block_table), _ptr(seq_len))
+        self._ref = ctypes.byref(self._c)
+        self._fixed = True
+
+    def __setattr__(self, name: str, value) -> None:
+        if getattr(self, "_fixed", False):
+            raise AttributeError(f"{name}: a KVCache4 keeps its tensors; copy into them or make another cache")
+        object.__setattr__(self, name, value)
+
+    @property
+    def c_struct(self) -> _KVCache4C:
+        return self._c
+
+
+def _cache4(cache) -> None:
+    if not isinstance(cache, KVCache4):
+        raise TypeError(f"cache must be a KVCache4, got {type(cache).__name__}")
+
+
+def kv4_write(k: torch.Tensor, v: torch.Tensor, cache: KVCache4, first: torch.Tensor, *,
+              count: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Quantises new tokens into the cache: token t < ``count[b]`` (all T without
+    it) of ``k``, ``v`` [B, T, n_kv_heads, d_head] goes to slot ``first[b]`` + t.
+    ``k`` and ``v`` may be strided, as columns of a fused projection, by the same
+    strides.  ``first`` and ``count`` are [B] int32.  Slots that the table does
+    not address are passed over; the cache's ``seq_len`` is neither read nor written."""
+    _cache4(cache)
+    for t, n in ((k, "k"), (v, "v")):
+        _half_tensor(t, n, 4, cache)
+    B, T, Hkv, D = k.shape
+    if B != cache.B or Hkv != cache.n_kv_heads or D != cache.d_head:
+        raise ValueError(f"k is {tuple(k.shape)}, the cache holds {cache.B} sequences of {cache.n_kv_heads} heads of "
+                         f"{cache.d_head}")
+    if v.shape != k.shape or _steps(v) != _steps(k):
+        raise ValueError("k and v must agree in shape and strides")
+    dev = cache.device
+    _dev_tensor(first, "first", torch.int32, shape=(B,), device=dev)
+    if count is not None:
+        _dev_tensor(count, "count", torch.int32, shape=(B,), device=dev)
+    st = lib().brisk_kv4_write(cache._ref, _ptr(k), _ptr(v), *_steps(k)[:3], B, T, _ptr(first), _ptr(count),
+                               _stream_ptr(dev, stream))
+    _check(st, "brisk_kv4_write")
+
+
+def kv4_read(cache: KVCache4, T: int, *, first: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
+             v: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values [B, T, n_kv_heads, d_head] as the cache holds them, of slots
+    ``first[b]`` (0 without it) to ``first[b]`` + T - 1; zeros for slots that a
+    sequence does not hold."""
+    _cache4(cache)
+    dev, shape = cache.device, (cache.B, T, cache.n_kv_heads, cache.d_head)
+    if first is not None:
+        _dev_tensor(first, "first", torch.int32, shape=(cache.B,), device=dev)
+    out = []
+    for t, n in ((k, "k"), (v, "v")):
+        if t is None:
+            t = torch.empty(shape, dtype=cache.dtype, device=dev)
+        else:
+            _dev_tensor(t, n, cache.dtype, shape=shape, device=dev)
+        out.append(t)
+    st = lib().brisk_kv4_read(cache._ref, cache.B, T, _ptr(first), _ptr(out[0]), _ptr(out[1]), _stream_ptr(dev, stream))
+    _check(st, "brisk_kv4_read")
+    return out[0], out[1]
+
+
+def kv4_attention(q: torch.Tensor, cache: KVCache4, *, prefix: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                  block_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                  max_seq_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None
+                  ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """:func:`block_attention` over a cache held in 4 bits: the same arguments and
+    results; the prefix is in the cache's 2-byte type."""
+    _cache4(cache)
+    return _attend(lib().brisk_kv4_attention, "brisk_kv4_attention", _kv4_workspace_size, "attention4", q, cache, prefix,
+                   block_mask, scale, max_seq_len, out, lse, workspace, stream, _block_queries(q, cache, block_mask))
+
+
+@functools.lru_cache(maxsize=1024)
+def _kv4_workspace_size(B: int, L: int, n_heads: int, n_kv_heads: int, d_head: int, prefix_len: int,
+                        max_seq_len: int) -> int:
+    out = _sz()
+    _check(lib().brisk_kv4_attention_workspace_size(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len,
+                                                    ctypes.byref(out)), "brisk_kv4_attention_workspace_size")
+    return out.value

@@ -18,7 +18,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libbrisk.so")
 SOURCES = ["lmhead_topk.hip", "corrector.hip", "verify.hip", "profile.hip", "loss.hip", "attention.hip", "cache.hip",
-           "draft_verify.hip", "brisk_abi.cpp"]
+           "draft_verify.hip", "kv4_cache.hip", "kv4_attention.hip", "brisk_abi.cpp"]
 ARCH = "gfx950"
 # Packed-fp32 instructions stay off: the compiler must not form them itself.
 GPU_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

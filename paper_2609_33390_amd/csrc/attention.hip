@@ -25,6 +25,7 @@
 // PFLOP/s where a library product of 8192^3 reaches 1.19; with the LDS reads left
 // out 0.28, with the softmax left out too 0.24.  Small calls are bound by latency:
 // lengths, page ids, keys, join.
+#include "attention_plan.h"
 #include "half_mfma.h"
 #include "kernels.h"
 
@@ -34,7 +35,6 @@ namespace {
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-constexpr int kCUs = 256;
 // In base 2: the subtracted logit may be kLag behind the maximum, and the probabilities are held
 // kLift higher than that, which l and the log-sum-exp share.  f16 has no steps below 2^-24, so its
 // probabilities use its range from the top: at most 2^15, and a key's weight is off by at most
@@ -54,28 +54,12 @@ struct AttnPlan {
   int own_first;         // index of the first own split
 };
 
-template <bool F16>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  if constexpr (F16) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, h2{static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
-  } else {
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, b2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
-  }
-}
-
 // Which of 32 keys a row sees: bit x is set when x < left and the key's place
 // in the block, at + x, is negative (before the block) or set in `word`.
 __device__ __forceinline__ uint32_t seen32(uint64_t word, int at, int left) {
   uint64_t bits = at >= 64 ? 0 : at >= 0 ? word >> at : at > -32 ? (word << -at) | ((1ull << -at) - 1) : ~0ull;
   bits = left >= 32 ? bits : left <= 0 ? 0 : bits & ((1ull << left) - 1);
   return static_cast<uint32_t>(bits);
-}
-
-__device__ __forceinline__ float swap32_max(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // Values take another permutation than keys, for the transposed b64 reads of
@@ -526,8 +510,6 @@ __global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, AttnPlan p) 
   if (lane == 0 && a.lse) a.lse[row] = L == 0.f ? -INFINITY : sub + __builtin_amdgcn_logf(L) * kLn2;
 }
 
-int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
-
 // The tile of a launch: rows, keys of a step of the whole workgroup, and the
 // workgroups that the GPU holds at once (two a CU, but one of the 256-row tile).
 // The smallest tile that holds the rows wastes the fewest of the matrix cores'
@@ -536,28 +518,6 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 struct TileShape { int rows, keys, slots; };
 constexpr TileShape kShapes[] = {{32, 64, 2 * kCUs}, {64, 64, 2 * kCUs}, {128, 64, 2 * kCUs}, {256, 64, kCUs}};
 int shape_for(int64_t rows) { return rows <= 32 ? 0 : rows <= 64 ? 1 : rows <= 128 ? 2 : 3; }
-
-// Runs of `keys` keys that `whole` workgroups would cover: the fewest rounds of
-// workgroups, each counted as its keys and 512 for its start.  What that constant is
-// hardly matters (64 to 1500 plan the timing cases alike): the rule fills a round,
-// and weighs neither rows nor the bytes of the partial sums.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
-// runs of 512 keys 119, of 256 147.)
-struct Runs { int count, keys; };
-constexpr int64_t kMostRuns = 1 << 20;
-Runs runs_of(int keys, int64_t whole, TileShape t) {
-  Runs best{};
-  double least = 1e300;
-  for (int s = 1; s <= 64; ++s) {
-    const int run = ceil_div(ceil_div(keys, s), t.keys) * t.keys, count = ceil_div(keys, run);
-    if (s > 1 && whole * count > kMostRuns) break;  // thousands of rounds: nothing to fill, and a launch has its limit
-    const double cost = ((whole * count + t.slots - 1) / t.slots) * (run + 512.0);
-    if (cost < least) {
-      least = cost;
-      best = {count, run};
-    }
-  }
-  return best;
-}
 
 struct CallPlan {
   AttnPlan p;
@@ -573,7 +533,7 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int D, int prefix_len, int max_
     c.pre_shape = shape_for(rows);
     const TileShape t = kShapes[c.pre_shape];
     c.p.pre_tiles = ceil_div(rows, t.rows);
-    const Runs r = runs_of(prefix_len, static_cast<int64_t>(c.p.pre_tiles) * Hkv, t);
+    const Runs r = runs_of(prefix_len, static_cast<int64_t>(c.p.pre_tiles) * Hkv, t.keys, t.slots);
     c.p.pre_run = r.keys;
     c.p.pre_splits = r.count;
     c.p.pre_groups = Hkv * r.count;
@@ -583,7 +543,8 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int D, int prefix_len, int max_
     c.own_shape = shape_for(rows);
     const TileShape t = kShapes[c.own_shape];
     c.p.own_tiles = ceil_div(rows, t.rows);
-    const Runs r = runs_of(max_seq_len > 0 ? max_seq_len : 1, static_cast<int64_t>(B) * Hkv * c.p.own_tiles, t);
+    const Runs r = runs_of(max_seq_len > 0 ? max_seq_len : 1, static_cast<int64_t>(B) * Hkv * c.p.own_tiles, t.keys,
+                           t.slots);
     c.p.own_run = r.keys;
     c.p.own_splits = r.count;
     c.p.own_groups = B * Hkv * c.p.own_splits;
@@ -605,6 +566,12 @@ void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStrea
 }
 
 template <bool F16>
+void launch_join(const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
+  const int64_t rows = static_cast<int64_t>(a.B) * a.L * a.H;
+  hipLaunchKernelGGL(join_kernel<F16>, dim3(ceil_div(rows, 4)), dim3(256), 0, s, a, p);
+}
+
+template <bool F16>
 void launch_all(const AttentionArgs& a, const CallPlan& c, hipStream_t s) {
   auto go = [&](int shape, const AttnPlan& p) {
     switch (head_slices(a.D)) {
@@ -621,10 +588,7 @@ void launch_all(const AttentionArgs& a, const CallPlan& c, hipStream_t s) {
     if (c.pre_shape >= 0) go(c.pre_shape, pre);
     if (c.own_shape >= 0) go(c.own_shape, own);
   }
-  if (c.p.part) {
-    const int64_t rows = static_cast<int64_t>(a.B) * a.L * a.H;
-    hipLaunchKernelGGL(join_kernel<F16>, dim3(ceil_div(rows, 4)), dim3(256), 0, s, a, c.p);
-  }
+  if (c.p.part) launch_join<F16>(a, c.p, s);
 }
 
 }  // namespace
@@ -648,6 +612,35 @@ void launch_attention(const AttentionArgs& a, bool f16, void* ws, hipStream_t s)
     launch_all<true>(a, c, s);
   else
     launch_all<false>(a, c, s);
+}
+
+// The prefix's part of a call whose own keys are another kernel's: runs 0 .. prefix_splits - 1 of `splits`.
+int attention_prefix_splits(int B, int L, int H, int Hkv, int prefix_len) {
+  return make_plan(B, L, H, Hkv, 0, prefix_len, 0).p.pre_splits;
+}
+
+void launch_attention_prefix(const AttentionArgs& a, bool f16, float* part, float* part_lse, int splits, hipStream_t s) {
+  CallPlan c = make_plan(a.B, a.L, a.H, a.Hkv, a.D, a.prefix_len, 0);
+  c.p.part = part;
+  c.p.part_lse = part_lse;
+  c.p.splits = splits;
+  auto go = [&](auto type) {
+    constexpr bool kF16 = type;
+    switch (head_slices(a.D)) {
+      case 2: launch_shape<kF16, 2>(c.pre_shape, a, c.p, s); break;
+      case 3: launch_shape<kF16, 3>(c.pre_shape, a, c.p, s); break;
+      default: launch_shape<kF16, 4>(c.pre_shape, a, c.p, s); break;
+    }
+  };
+  f16 ? go(std::true_type{}) : go(std::false_type{});
+}
+
+void launch_attention_join(const AttentionArgs& a, bool f16, float* part, float* part_lse, int splits, hipStream_t s) {
+  AttnPlan p{};
+  p.part = part;
+  p.part_lse = part_lse;
+  p.splits = splits;
+  f16 ? launch_join<true>(a, p, s) : launch_join<false>(a, p, s);
 }
 
 }  // namespace brisk

@@ -49,6 +49,29 @@ int cache_check(const brisk_kv_cache* c, brisk::KvView* view) {
   return BRISK_OK;
 }
 
+// The same of the cache in 4 bits.
+constexpr int32_t kMaxKv4Rows = 1 << 22;  // a launch holds fewer than 2^32 threads
+int kv4_check(const brisk_kv4_cache* c, brisk::Kv4View* view) {
+  if (!c || !c->pages || !c->block_table || !c->seq_len) return BRISK_ERR_NULL;
+  if ((c->dtype != BRISK_BF16 && c->dtype != BRISK_F16) || c->n_kv_heads < 1 || c->n_kv_heads > 1024 ||
+      c->d_head < 8 || c->d_head > 128 || c->page_size < brisk::kKv4Block || c->page_size > 65536 ||
+      c->n_pages < 1 || c->max_pages < 1 ||
+      static_cast<int64_t>(c->max_pages) * c->page_size > (int64_t{1} << 30) || c->page_stride < 0 ||
+      c->head_stride < 0)
+    return BRISK_ERR_SHAPE;
+  if (c->d_head % 8 != 0 || (c->page_size & (c->page_size - 1)) != 0 || c->page_stride % 16 != 0 ||
+      c->head_stride % 16 != 0 || !aligned16(c->pages) || !aligned4(c->block_table) || !aligned4(c->seq_len))
+    return BRISK_ERR_UNSUPPORTED;
+  int shift = 0;
+  while ((1 << shift) < c->page_size) ++shift;
+  *view = {c->pages, c->block_table, c->seq_len, c->page_stride, c->head_stride, shift, c->n_pages, c->max_pages};
+  return BRISK_OK;
+}
+
+int64_t kv4_part_bytes(int32_t page_size, int32_t d_head) {
+  return static_cast<int64_t>(page_size) * brisk::kv4_slot_bytes(brisk::kv4_width(d_head));
+}
+
 // Rows of a block's queries: [B * L, n_heads] with head groups of the cache.
 int block_rows_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads) {
   if (B < 1 || L < 1 || L > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 ||
@@ -91,6 +114,18 @@ struct Span {
 bool overlap(Span a, Span b) {
   const uint64_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
   return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
+// Tokens of a call on the 4-bit cache, and what its launch holds.
+int kv4_tokens_check(const brisk_kv4_cache* c, int32_t B, int32_t T) {
+  return B < 1 || T < 1 || T > kMaxSlots || !brisk::kv4_launchable(B, c->n_kv_heads, T) ? BRISK_ERR_SHAPE : BRISK_OK;
+}
+
+int kv4_attention_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                        int32_t prefix_len, int32_t max_seq_len) {
+  const int st = attention_shape_check(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len);
+  if (st != BRISK_OK) return st;
+  return static_cast<int64_t>(B) * L * n_heads > kMaxKv4Rows ? BRISK_ERR_SHAPE : BRISK_OK;
 }
 
 int evict_shape_check(int32_t B, int32_t n_kv_heads, int32_t cap, int32_t budget) {
@@ -660,6 +695,149 @@ int brisk_draft_verify(const float* target_prob, int64_t target_stride, const fl
   const brisk::DraftArgs a{target_prob, draft_prob, target_stride, draft_stride, draft_tok, draft_len,
                            u_accept, noise, noise_stride, B, L, V, accept_len, token};
   brisk::launch_draft_verify(a, ws, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_kv4_page_bytes(int32_t page_size, int32_t d_head, size_t* bytes) {
+  if (!bytes) return BRISK_ERR_NULL;
+  if (page_size < brisk::kKv4Block || page_size > 65536 || d_head < 8 || d_head > 128) return BRISK_ERR_SHAPE;
+  if (d_head % 8 != 0 || (page_size & (page_size - 1)) != 0) return BRISK_ERR_UNSUPPORTED;
+  *bytes = static_cast<size_t>(kv4_part_bytes(page_size, d_head));
+  return BRISK_OK;
+}
+
+int brisk_kv4_write(const brisk_kv4_cache* cache, const uint16_t* k, const uint16_t* v,
+                    int64_t seq_stride, int64_t row_stride, int64_t head_stride, int32_t B, int32_t T,
+                    const int32_t* first, const int32_t* count, void* stream) {
+  brisk::Kv4WriteArgs a{};
+  int st = kv4_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  if (!k || !v || !first) return BRISK_ERR_NULL;
+  st = kv4_tokens_check(cache, B, T);
+  if (st != BRISK_OK) return st;
+  if (seq_stride < 0 || row_stride < 0 || head_stride < 0) return BRISK_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || seq_stride % 8 != 0 || row_stride % 8 != 0 || head_stride % 8 != 0 ||
+      !aligned4(first) || !aligned4(count))
+    return BRISK_ERR_UNSUPPORTED;
+  // Wavefronts write some slots while others read their tokens, lengths and pages.
+  const int64_t part = kv4_part_bytes(cache->page_size, cache->d_head);
+  const bool pages_outside = cache->page_stride >= cache->head_stride;
+  const int64_t inner = pages_outside ? cache->head_stride : cache->page_stride;
+  const int64_t outer = pages_outside ? cache->page_stride : cache->head_stride;
+  const int64_t inner_n = pages_outside ? cache->n_kv_heads : cache->n_pages;
+  const int64_t outer_n = pages_outside ? cache->n_pages : cache->n_kv_heads;
+  if ((inner_n > 1 && inner < part) ||
+      (outer_n > 1 && outer < static_cast<__int128>(inner_n > 1 ? (inner_n - 1) * static_cast<__int128>(inner) : 0) + part))
+    return BRISK_ERR_UNSUPPORTED;
+  const uint64_t seqs = static_cast<uint64_t>(B) * 4;
+  const uint64_t reach = static_cast<uint64_t>(inner_n - 1) * inner + static_cast<uint64_t>(outer_n - 1) * outer + part;
+  const uint64_t span = 2 * (static_cast<uint64_t>(B - 1) * seq_stride + static_cast<uint64_t>(T - 1) * row_stride +
+                             static_cast<uint64_t>(cache->n_kv_heads - 1) * head_stride + cache->d_head);
+  const Span out{cache->pages, reach};
+  if (overlap(out, {k, span}) || overlap(out, {v, span}) || overlap(out, {first, seqs}) ||
+      (count && overlap(out, {count, seqs})) || overlap(out, {cache->seq_len, seqs}) ||
+      overlap(out, {cache->block_table, seqs * cache->max_pages}))
+    return BRISK_ERR_UNSUPPORTED;
+  a.k = k;
+  a.v = v;
+  a.seq_stride = seq_stride;
+  a.row_stride = row_stride;
+  a.head_stride = head_stride;
+  a.first = first;
+  a.count = count;
+  a.B = B;
+  a.T = T;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->d_head;
+  brisk::launch_kv4_write(a, cache->dtype == BRISK_F16, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_kv4_read(const brisk_kv4_cache* cache, int32_t B, int32_t T, const int32_t* first,
+                   uint16_t* k, uint16_t* v, void* stream) {
+  brisk::Kv4ReadArgs a{};
+  int st = kv4_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  if (!k || !v) return BRISK_ERR_NULL;
+  st = kv4_tokens_check(cache, B, T);
+  if (st != BRISK_OK) return st;
+  if (!aligned16(k) || !aligned16(v) || !aligned4(first)) return BRISK_ERR_UNSUPPORTED;
+  const uint64_t seqs = static_cast<uint64_t>(B) * 4;
+  const uint64_t bytes = 2 * static_cast<uint64_t>(B) * T * cache->n_kv_heads * cache->d_head;
+  const Span outs[] = {{k, bytes}, {v, bytes}};
+  for (const Span& out : outs)
+    if ((first && overlap(out, {first, seqs})) || overlap(out, {cache->seq_len, seqs}) ||
+        overlap(out, {cache->block_table, seqs * cache->max_pages}))
+      return BRISK_ERR_UNSUPPORTED;
+  if (overlap(outs[0], outs[1])) return BRISK_ERR_UNSUPPORTED;
+  a.first = first;
+  a.k = k;
+  a.v = v;
+  a.B = B;
+  a.T = T;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->d_head;
+  brisk::launch_kv4_read(a, cache->dtype == BRISK_F16, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+int brisk_kv4_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads,
+                                       int32_t d_head, int32_t prefix_len, int32_t max_seq_len,
+                                       size_t* bytes) {
+  if (!bytes) return BRISK_ERR_NULL;
+  const int st = kv4_attention_check(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len);
+  if (st != BRISK_OK) return st;
+  *bytes = brisk::kv4_attention_workspace_bytes(B, L, n_heads, n_kv_heads, d_head, prefix_len, max_seq_len);
+  return BRISK_OK;
+}
+
+int brisk_kv4_attention(const brisk_kv4_cache* cache, const brisk_kv_prefix* prefix, const uint16_t* q,
+                        int64_t q_row_stride, int64_t q_head_stride, const uint64_t* block_mask,
+                        int32_t B, int32_t L, int32_t n_heads, int32_t max_seq_len, float scale,
+                        uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  brisk::Kv4AttentionArgs a{};
+  int st = kv4_check(cache, &a.kv);
+  if (st != BRISK_OK) return st;
+  const int32_t prefix_len = prefix ? prefix->len : 0;
+  if (!q || !out || (prefix_len > 0 && (!prefix->k || !prefix->v))) return BRISK_ERR_NULL;
+  st = kv4_attention_check(B, L, n_heads, cache->n_kv_heads, cache->d_head, prefix_len, max_seq_len);
+  if (st != BRISK_OK) return st;
+  if (max_seq_len > static_cast<int64_t>(cache->max_pages) * cache->page_size || q_row_stride < 0 ||
+      q_head_stride < 0 || !(scale > 0.f) || scale > kMaxScale ||
+      (prefix && (prefix->slot_stride < 0 || prefix->head_stride < 0)))
+    return BRISK_ERR_SHAPE;
+  if (!aligned16(q) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0 || !aligned16(out) ||
+      !aligned4(lse) || !aligned8(block_mask))
+    return BRISK_ERR_UNSUPPORTED;
+  brisk::AttentionArgs pre{};
+  if (prefix_len > 0) {
+    if (!aligned16(prefix->k) || !aligned16(prefix->v) || prefix->slot_stride % 8 != 0 ||
+        prefix->head_stride % 8 != 0)
+      return BRISK_ERR_UNSUPPORTED;
+    pre.pre_k = prefix->k;
+    pre.pre_v = prefix->v;
+    pre.pre_slot_stride = prefix->slot_stride;
+    pre.pre_head_stride = prefix->head_stride;
+  }
+  const size_t need = brisk::kv4_attention_workspace_bytes(B, L, n_heads, cache->n_kv_heads, cache->d_head,
+                                                           prefix_len, max_seq_len);
+  if (ws_bytes < need || (need > 0 && !ws)) return BRISK_ERR_WORKSPACE;
+  if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
+  a.q = pre.q = q;
+  a.q_row_stride = pre.q_row_stride = q_row_stride;
+  a.q_head_stride = pre.q_head_stride = q_head_stride;
+  a.mask = pre.mask = block_mask;
+  a.out = pre.out = out;
+  a.lse = pre.lse = lse;
+  a.B = pre.B = B;
+  a.L = pre.L = L;
+  a.H = pre.H = n_heads;
+  a.Hkv = pre.Hkv = cache->n_kv_heads;
+  a.D = pre.D = cache->d_head;
+  a.max_seq_len = max_seq_len;
+  pre.prefix_len = prefix_len;
+  a.scale = pre.scale = scale;
+  brisk::launch_kv4_attention(a, pre, cache->dtype == BRISK_F16, ws, static_cast<hipStream_t>(stream));
   return launch_status();
 }
 

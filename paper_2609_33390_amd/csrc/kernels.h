@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "brisk.h"
+#include "kv4_view.h"
 #include "kv_view.h"
 
 namespace brisk {
@@ -100,6 +101,44 @@ struct AttentionArgs {
 };
 size_t attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len);
 void launch_attention(const AttentionArgs& a, bool f16, void* ws, hipStream_t s);
+
+// Parts of it for a cache of another format: the runs that the prefix is read in, the launch that leaves
+// their sums at runs 0 .. of `splits` (null part: the output itself), and the join of all runs.
+int attention_prefix_splits(int B, int L, int H, int Hkv, int prefix_len);
+void launch_attention_prefix(const AttentionArgs& a, bool f16, float* part, float* part_lse, int splits, hipStream_t s);
+void launch_attention_join(const AttentionArgs& a, bool f16, float* part, float* part_lse, int splits, hipStream_t s);
+
+// ---- the cache in 4 bits -------------------------------------------------------
+struct Kv4WriteArgs {
+  Kv4View kv;
+  const uint16_t *k, *v;
+  int64_t seq_stride, row_stride, head_stride;     // elements
+  const int32_t *first, *count;                    // [B], count nullable
+  int B, T, Hkv, D;
+};
+struct Kv4ReadArgs {
+  Kv4View kv;
+  const int32_t* first;                            // [B], nullable
+  uint16_t *k, *v;                                 // [B, T, Hkv, D]
+  int B, T, Hkv, D;
+};
+bool kv4_launchable(int B, int Hkv, int T);        // one launch holds the call's workgroups
+void launch_kv4_write(const Kv4WriteArgs& a, bool f16, hipStream_t s);
+void launch_kv4_read(const Kv4ReadArgs& a, bool f16, hipStream_t s);
+
+struct Kv4AttentionArgs {
+  Kv4View kv;
+  const uint16_t* q;
+  int64_t q_row_stride, q_head_stride;             // elements
+  const uint64_t* mask;                            // [B, L], nullable
+  uint16_t* out;
+  float* lse;                                      // nullable
+  int B, L, H, Hkv, D, max_seq_len;
+  float scale;
+};
+size_t kv4_attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len);
+// `pre` holds the same call as the attention over a 2-byte prefix sees it (no cache).
+void launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, hipStream_t s);
 
 // ---- received attention weight, eviction ---------------------------------------
 struct ScoreArgs {

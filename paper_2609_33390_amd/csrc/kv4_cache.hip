@@ -1,0 +1,297 @@
+// Writing tokens to the 4-bit cache, and reading them back.
+//
+//   z = min_d x_d,  s = type((max_d x_d - z) / 15),  c_d = min(rne((x_d - z) / s), 15)
+//
+// A wavefront takes 16 slots of a head, aligned to the cache's blocks.  Lane
+// (q, key) = (lane / 16, lane % 16) holds a quarter of the key and a quarter of the
+// value, in the pieces that the block's layout keeps together.
+#include "kernels.h"
+#include "kv4_common.h"
+
+namespace brisk {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+// x of lane ^ 1 and lane ^ 2.
+__device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return __builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0xB1, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return __builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4E, 0xF, 0xF, false); }
+
+// Lane u of each four gets what lane v had in w[u], as w[v].
+__device__ __forceinline__ void quad_transpose(uint32_t (&w)[4], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const uint32_t get = quad_xor1(odd ? w[i] : w[i + 1]);
+    w[i] = odd ? get : w[i];
+    w[i + 1] = odd ? w[i + 1] : get;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t get = quad_xor2(high ? w[i] : w[i + 2]);
+    w[i] = high ? get : w[i];
+    w[i + 2] = high ? w[i + 2] : get;
+  }
+}
+
+// Over the four lanes that share a slot.
+__device__ __forceinline__ float quarters_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// How a head is held.  The quotient t / s is taken as t (1 / s) with the reciprocal in two parts,
+// good to 2^-46: rounded to 32 bits that is a tie between two codes only where the quotient
+// is one, since t has 24 bits and s at most 11 (a quotient that is none is at least 2^-24 of
+// itself away from one, and 2^-35 of itself past the middle of its rounding).
+struct Scheme {
+  float low, inv, inv_rest;
+  uint32_t pair;
+};
+
+template <bool F16>
+__device__ __forceinline__ Scheme scheme_of(float lowest, float highest, float poison) {
+  Scheme h;
+  const float range = highest - lowest;
+  uint32_t step = f32_to_half<F16>(range / 15.f);
+  // not a number where an element is not finite, or their range
+  const bool bad = !(range + poison < INFINITY);
+  if (!F16 && step < 0x0080) step = 0;             // steps below the normal numbers: the head is its lowest value
+  const uint32_t low = bad ? (F16 ? 0x7E00u : 0x7FC0u) : f32_to_half<F16>(lowest);
+  if (bad) step = 0;
+  h.pair = step | low << 16;
+  const float s = half_to_f32<F16>(step);
+  h.low = lowest;
+  h.inv = step ? 1.f / s : 0.f;
+  h.inv_rest = fmaf(-s, h.inv, step ? 1.f : 0.f) * h.inv;
+  return h;
+}
+
+// The code as a float.  0 for every element of a head without a step (NaN compares false).
+__device__ __forceinline__ float code_of(float x, const Scheme& h) {
+  const float t = x - h.low, y = fmaf(t, h.inv, t * h.inv_rest);
+  return __builtin_rintf(fminf(y, 15.f));
+}
+
+template <bool F16>
+__device__ __forceinline__ void widen(uint32_t w, float& lo, float& hi) {
+  lo = half_to_f32<F16>(w & 0xFFFF);
+  hi = F16 ? half_to_f32<F16>(w >> 16) : __uint_as_float(w & 0xFFFF0000u);
+}
+
+// Place in a block of the word of a key's elements e .. e + 7.
+template <int W>
+__device__ __forceinline__ int key_word(int key, int e) {
+  return (16 * (e / (W / 4)) + key) * (W / 8) + e % (W / 4) / 8 * 4;
+}
+
+template <bool F16, int W>
+__global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, int blocks, int64_t items) {
+  constexpr int NK = W / 32, NV = W / 16;
+  const int lane = threadIdx.x & 63, q = lane >> 4, key = lane & 15;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (item >= items) return;
+  const int h = item % a.Hkv, b = item / a.Hkv / blocks, nth = item / a.Hkv % blocks;
+  const int64_t first = a.first[b], count = a.count ? min(max(a.count[b], 0), a.T) : a.T;
+  const int64_t cap = static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift;
+  const int64_t j0 = (first >= 0 ? first / kKv4Block : (first - (kKv4Block - 1)) / kKv4Block) * kKv4Block + 16 * static_cast<int64_t>(nth);
+  if (j0 < 0 || j0 >= cap || j0 >= first + count) return;
+  const int64_t tok = j0 + key - first;            // this lane's token
+  const bool valid = tok >= 0 && tok < count;
+  if (!__any(valid)) return;
+  const int64_t src = b * a.seq_stride + tok * a.row_stride + h * a.head_stride;
+  uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(j0));
+
+  uint4 kw[NK];
+  uint2 vw[NV];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const int e = 32 * i + 8 * q;
+    kw[i] = valid && e < a.D ? *reinterpret_cast<const uint4*>(a.k + src + e) : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int e = 16 * i + 4 * q;
+    vw[i] = valid && e < a.D ? *reinterpret_cast<const uint2*>(a.v + src + e) : make_uint2(0, 0);
+  }
+
+  {  // ---- the key: elements 32 i + 8 q + 0 .. 7
+    float x[NK][8], lo = INFINITY, hi = -INFINITY, poison = 0.f;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const uint32_t w4[4] = {kw[i].x, kw[i].y, kw[i].z, kw[i].w};
+      const bool in = 32 * i + 8 * q < a.D;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        widen<F16>(w4[e / 2], x[i][e], x[i][e + 1]);
+        lo = fminf(lo, in ? fminf(x[i][e], x[i][e + 1]) : INFINITY);
+        hi = fmaxf(hi, in ? fmaxf(x[i][e], x[i][e + 1]) : -INFINITY);
+        poison = fmaf(x[i][e], 0.f, fmaf(x[i][e + 1], 0.f, poison));
+      }
+    }
+    poison = swap32_sum(swap16_sum(poison));
+    const Scheme s = scheme_of<F16>(-quarters_max(-lo), quarters_max(hi), poison);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      // element e is nibble e / 2 of half e % 2
+      float half[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) half[e % 2] = fmaf(code_of(x[i][e], s), static_cast<float>(1 << (4 * (e / 2))), half[e % 2]);
+      uint32_t w = static_cast<uint32_t>(half[0]) | static_cast<uint32_t>(half[1]) << 16;
+      if (32 * i + 8 * q >= a.D || (s.pair & 0xFFFF) == 0) w = 0;
+      if (valid) *reinterpret_cast<uint32_t*>(blk + key_word<W>(key, 32 * i + 8 * q)) = w << 3 | w >> 29;
+    }
+    if (valid && q == 0) *reinterpret_cast<uint32_t*>(blk + 16 * W + 4 * key) = s.pair;
+  }
+
+  {  // ---- the value: elements x + 16 (4 y + j) for x = 4 q + 0 .. 3
+    float lo = INFINITY, hi = -INFINITY, poison = 0.f, x[NV][4];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const bool in = 16 * i + 4 * q < a.D;
+      widen<F16>(vw[i].x, x[i][0], x[i][1]);
+      widen<F16>(vw[i].y, x[i][2], x[i][3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lo = fminf(lo, in ? x[i][e] : INFINITY);
+        hi = fmaxf(hi, in ? x[i][e] : -INFINITY);
+        poison = fmaf(x[i][e], 0.f, poison);
+      }
+    }
+    poison = swap32_sum(swap16_sum(poison));
+    const Scheme s = scheme_of<F16>(-quarters_max(-lo), quarters_max(hi), poison);
+    uint32_t w[4];                                 // for each x the 16 bits of y = 0 and, above them, of y = 1
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float half[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float c = 16 * i + 4 * q < a.D ? code_of(x[i][e], s) : 0.f;
+        half[i / 4] = fmaf(c, static_cast<float>(1 << (4 * (i % 4))), half[i / 4]);
+      }
+      w[e] = (s.pair & 0xFFFF) == 0 ? 0 : static_cast<uint32_t>(half[0]) | static_cast<uint32_t>(half[1]) << 16;
+    }
+    uint8_t* const val = blk + 8 * W;
+    const int t = key >> 2, u = key & 3;
+    if (__all(valid)) {
+      quad_transpose(w, lane);                     // now of x = 4 q + u, slots 4 t + 0 .. 3
+      uint8_t* const to = val + (16 * t + 4 * q + u) * (W / 8);
+      const uint2 y0 = make_uint2((w[0] & 0xFFFF) | w[1] << 16, (w[2] & 0xFFFF) | w[3] << 16);
+      if constexpr (W == 128)
+        *reinterpret_cast<uint4*>(to) = make_uint4(y0.x, y0.y, w[0] >> 16 | (w[1] & 0xFFFF0000u), w[2] >> 16 | (w[3] & 0xFFFF0000u));
+      else
+        *reinterpret_cast<uint2*>(to) = y0;
+    } else if (valid) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int y = 0; y < W / 64; ++y)
+          *reinterpret_cast<uint16_t*>(val + (16 * t + 4 * q + e) * (W / 8) + 8 * y + 2 * u) = static_cast<uint16_t>(w[e] >> (16 * y));
+    }
+    if (valid && q == 1) *reinterpret_cast<uint32_t*>(blk + 16 * W + 64 + 4 * key) = s.pair;
+  }
+}
+
+// z + s c, rounded to the cache's type.
+template <bool F16>
+__device__ __forceinline__ uint32_t value_of(uint32_t code, float step, float low) {
+  return f32_to_half<F16>(fmaf(step, static_cast<float>(code), low));
+}
+
+template <bool F16, int W>
+__global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, int blocks, int64_t items) {
+  constexpr int NK = W / 32, NV = W / 16;
+  const int lane = threadIdx.x & 63, q = lane >> 4, key = lane & 15;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (item >= items) return;
+  const int h = item % a.Hkv, b = item / a.Hkv / blocks, nth = item / a.Hkv % blocks;
+  const int64_t first = a.first ? a.first[b] : 0;
+  const int n = kv4_len(a.kv, b, static_cast<int>(static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift));
+  const int64_t j0 = (first >= 0 ? first / kKv4Block : (first - (kKv4Block - 1)) / kKv4Block) * kKv4Block + 16 * static_cast<int64_t>(nth);
+  const int64_t tok = j0 + key - first;
+  if (!__any(tok >= 0 && tok < a.T)) return;
+  const bool wanted = tok >= 0 && tok < a.T, held = wanted && j0 + key >= 0 && j0 + key < n;
+  const int64_t dst = ((b * static_cast<int64_t>(a.T) + tok) * a.Hkv + h) * a.D;
+  // slots that nobody holds read the place of one that the table addresses, and are not used
+  const uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(min(max(j0, int64_t{0}), (static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift) - 16)));
+
+  uint32_t kc[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) kc[i] = *reinterpret_cast<const uint32_t*>(blk + key_word<W>(key, 32 * i + 8 * q));
+  const int t = key >> 2, u = key & 3;
+  const uint8_t* const from = blk + 8 * W + (16 * t + 4 * q + u) * (W / 8);
+  uint4 vc = make_uint4(0, 0, 0, 0);
+  if constexpr (W == 128) {
+    vc = *reinterpret_cast<const uint4*>(from);
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(from);
+    vc = make_uint4(x.x, x.y, 0, 0);
+  }
+  const uint32_t kp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 4 * key);
+  const uint32_t vp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 64 + 4 * key);
+
+  {
+    const float s = kv4_step<F16>(kp), z = kv4_low<F16>(kp);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const uint32_t w = kc[i] >> 3 | kc[i] << 29;
+      uint32_t o[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        o[p] = held ? value_of<F16>((w >> (4 * p)) & 15, s, z) | value_of<F16>((w >> (4 * p + 16)) & 15, s, z) << 16 : 0;
+      const int e = 32 * i + 8 * q;
+      if (wanted && e < a.D) *reinterpret_cast<uint4*>(a.k + dst + e) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+  }
+  {
+    // of x = 4 q + u, slots 4 t + 0 .. 3: to this lane's slot, x = 4 q + 0 .. 3
+    uint32_t w[4] = {(vc.x & 0xFFFF) | vc.z << 16, vc.x >> 16 | (vc.z & 0xFFFF0000u),
+                     (vc.y & 0xFFFF) | vc.w << 16, vc.y >> 16 | (vc.w & 0xFFFF0000u)};
+    quad_transpose(w, lane);
+    const float s = kv4_step<F16>(vp), z = kv4_low<F16>(vp);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      uint32_t o[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        o[p] = held ? value_of<F16>((w[2 * p] >> (4 * i)) & 15, s, z) | value_of<F16>((w[2 * p + 1] >> (4 * i)) & 15, s, z) << 16 : 0;
+      const int e = 16 * i + 4 * q;
+      if (wanted && e < a.D) *reinterpret_cast<uint2*>(a.v + dst + e) = make_uint2(o[0], o[1]);
+    }
+  }
+}
+
+// Blocks of 16 slots that T tokens can touch, wherever they begin.
+int blocks_of(int T) { return (T + 2 * kKv4Block - 2) / kKv4Block; }
+
+}  // namespace
+
+bool kv4_launchable(int B, int Hkv, int T) { return static_cast<int64_t>(B) * Hkv * blocks_of(T) < (int64_t{1} << 25); }
+
+template <class Args, class Fn>
+static void launch_blocks(const Args& a, Fn kernel, hipStream_t s) {
+  const int blocks = blocks_of(a.T);
+  const int64_t items = static_cast<int64_t>(a.B) * a.Hkv * blocks;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((items + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, s, a, blocks, items);
+}
+
+void launch_kv4_write(const Kv4WriteArgs& a, bool f16, hipStream_t s) {
+  const bool wide = kv4_width(a.D) == 128;
+  if (f16)
+    launch_blocks(a, wide ? kv4_write_kernel<true, 128> : kv4_write_kernel<true, 64>, s);
+  else
+    launch_blocks(a, wide ? kv4_write_kernel<false, 128> : kv4_write_kernel<false, 64>, s);
+}
+
+void launch_kv4_read(const Kv4ReadArgs& a, bool f16, hipStream_t s) {
+  const bool wide = kv4_width(a.D) == 128;
+  if (f16)
+    launch_blocks(a, wide ? kv4_read_kernel<true, 128> : kv4_read_kernel<true, 64>, s);
+  else
+    launch_blocks(a, wide ? kv4_read_kernel<false, 128> : kv4_read_kernel<false, 64>, s);
+}
+
+}  // namespace brisk

@@ -1,0 +1,308 @@
+"""GPU checks of brisk_kv4_attention against the float64 oracle on the values that
+the cache holds (the tolerances are derived where they are computed)."""
+import numpy as np
+import pytest
+import torch
+
+from kv4_cases import Case4, pages_for
+from kv_cases import TYPES, UNIT, Case
+
+pytestmark = pytest.mark.gpu
+
+brisk = pytest.importorskip("paper_2609_33390_amd")
+
+
+def _run(c, **kw):
+    print(f"[kv4 attention] B={c.B} L={c.L} H={c.H}/{c.Hkv} D={c.D} page={c.page} lens={c.lens[:8]} "
+          f"prefix={None if c.prefix is None else len(c.prefix[0])} {c.dtype}", flush=True)
+    out, lse = brisk.kv4_attention(c.q.cuda(), c.cache, prefix=c.gpu_prefix(), block_mask=c.gpu_mask(), scale=c.scale, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("kw", [
+    # single tokens: lengths of none, one and many, with and without a prefix
+    dict(B=1, L=1, H=4, Hkv=4, D=128, prefix=None, lens=[1]),
+    dict(B=3, L=1, H=8, Hkv=2, D=128, prefix=None, lens=[0, 1, 300]),
+    dict(B=3, L=1, H=8, Hkv=2, D=128, prefix=0, lens=[0, 0, 0]),
+    dict(B=5, L=1, H=28, Hkv=4, D=128, prefix=129, lens=[0, 1, 31, 32, 33]),
+    dict(B=2, L=1, H=16, Hkv=1, D=64, prefix=1, lens=[65, 2000], page=128, dtype="f16"),
+    dict(B=6, L=1, H=32, Hkv=32, D=128, prefix=None, lens=[15, 16, 17, 47, 48, 49], dtype="f16"),
+    # 16 rows and one more, 32 and one more
+    dict(B=2, L=4, H=8, Hkv=2, D=128, prefix=None, lens=[70, 129], mask="causal"),
+    dict(B=2, L=17, H=2, Hkv=2, D=128, prefix=None, lens=[70, 129], mask="causal"),
+    dict(B=2, L=32, H=2, Hkv=2, D=64, prefix=None, lens=[70, 129], mask="mixed", dtype="f16"),
+    dict(B=2, L=33, H=2, Hkv=2, D=64, prefix=None, lens=[70, 129], mask="mixed"),
+    # blocks: shorter than the block, ending inside tiles and pages
+    dict(B=4, L=16, H=8, Hkv=2, D=128, prefix=None, lens=[3, 16, 17, 95], mask="causal"),
+    dict(B=4, L=16, H=8, Hkv=8, D=128, prefix=None, lens=[3, 16, 17, 95], mask="random"),
+    dict(B=3, L=16, H=8, Hkv=2, D=128, prefix=77, lens=[0, 15, 257], mask="mixed", page=64),
+    dict(B=2, L=33, H=6, Hkv=6, D=80, prefix=64, lens=[33, 130], mask="random", page=32),
+    dict(B=2, L=64, H=4, Hkv=2, D=96, prefix=63, lens=[64, 200], mask="random", dtype="f16"),
+    dict(B=1, L=64, H=8, Hkv=1, D=128, prefix=200, lens=[700], mask="mixed"),
+    # rows that see nothing
+    dict(B=2, L=7, H=4, Hkv=4, D=64, prefix=None, lens=[7, 5], mask="hidden"),
+    dict(B=2, L=7, H=4, Hkv=4, D=64, prefix=None, lens=[9, 7], mask="hidden", dtype="f16"),
+    dict(B=2, L=20, H=4, Hkv=4, D=128, prefix=None, lens=[20, 40], mask="hidden"),
+    # narrow and odd heads
+    dict(B=2, L=5, H=3, Hkv=1, D=8, prefix=20, lens=[40, 11], mask="causal"),
+    dict(B=2, L=3, H=10, Hkv=5, D=24, prefix=33, lens=[40, 129], mask="causal", dtype="f16"),
+    dict(B=1, L=20, H=14, Hkv=2, D=104, prefix=None, lens=[400], mask="causal", page=32),
+    dict(B=2, L=4, H=4, Hkv=2, D=72, prefix=300, lens=[100, 50]),
+    dict(B=2, L=9, H=4, Hkv=2, D=40, prefix=None, lens=[100, 50], mask="causal", dtype="f16"),
+    # many rows
+    dict(B=20, L=8, H=8, Hkv=2, D=128, prefix=100, lens=[8 + 7 * b for b in range(20)], mask="mixed", page=32),
+    dict(B=9, L=31, H=7, Hkv=1, D=128, prefix=93, lens=[31 + 11 * b for b in range(9)], mask="causal"),
+    dict(B=3, L=64, H=8, Hkv=1, D=64, prefix=None, lens=[64, 65, 190], mask="causal", dtype="f16"),
+    # long caches of few rows, split and joined
+    dict(B=1, L=1, H=8, Hkv=8, D=128, prefix=None, lens=[9001], page=64),
+    dict(B=1, L=1, H=2, Hkv=2, D=64, prefix=None, lens=[20011], page=64, dtype="f16"),
+    dict(B=2, L=8, H=8, Hkv=2, D=64, prefix=1000, lens=[6000, 37], mask="causal", page=256),
+    dict(B=1, L=24, H=4, Hkv=2, D=128, prefix=None, lens=[3001], mask="causal", dtype="f16"),
+])
+def test_attention_matches_oracle(kw):
+    c = Case4(brisk, seed=len(str(kw)), **kw)
+    c.check(*_run(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 96, 128])
+def test_as_the_attention_over_what_is_read_back(D, dtype):
+    """block_attention over the same values in 2 bytes: apart by its roundings of them and its own."""
+    B, L, H, Hkv, lens = 4, 8, 8, 2, [0, 8, 130, 517]
+    c = Case4(brisk, B, L, H, Hkv, D, 50, lens, mask="mixed", dtype=dtype, seed=D)
+    out, lse = _run(c)
+    k, v = brisk.kv4_read(c.cache, c.cache.max_seq_len)
+    pages = lambda x: x.reshape(B * c.cache.max_seq_len // 16, 16, Hkv, D)                     # noqa: E731
+    table = torch.arange(B * c.cache.max_seq_len // 16, dtype=torch.int32, device="cuda").view(B, -1)
+    plain = brisk.KVCache(pages(k), pages(v), table, c.seq_len)
+    out2, lse2 = brisk.block_attention(c.q.cuda(), plain, prefix=c.gpu_prefix(), block_mask=c.gpu_mask(), scale=c.scale)
+    # a key's rounding moves a logit by at most u scale sum |q k|, a value's the sum by u |v|
+    u = UNIT[dtype]
+    size = c.scale * c.q.double().abs().sum(-1).max().item() * max(k.abs().max().item(), 4.5)
+    big = max(v.abs().max().item(), 4.5)
+    assert ((lse - lse2).abs()[torch.isfinite(lse)] <= u * size + 2.0 ** -17 * size).all()
+    assert (out.float() - out2.float()).abs().max().item() <= big * (2 * u * size + 6 * u)
+
+
+@pytest.mark.parametrize("L", [1, 5])
+@pytest.mark.parametrize("std", [0.0, 30.0])
+def test_flat_and_very_sharp_weights(std, L):
+    c = Case4(brisk, 2, L, 8, 2, 128, 90, [60, 200], mask="causal", q_std=std, seed=5)
+    c.check(*_run(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L", [1, 9])
+def test_values_of_any_size(L, dtype):
+    """Value heads whose steps span the type's range, the largest early, late, and beside small ones."""
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(L)
+    lo, hi = (-60, 100) if dtype == "bf16" else (-12, 12)
+    for at in (0, 150, 299):
+        size = torch.exp2(torch.randint(lo, lo + 8, (1, 300, 4, 1), generator=g).double())
+        size[:, at] = 2.0 ** hi
+        v = (torch.randn(1, 300, 4, 64, generator=g, dtype=torch.float64) * size).to(dt)
+        k = torch.randn(1, 300, 4, 64, generator=g).to(dt)
+        c = Case4(brisk, 1, L, 8, 4, 64, None, [300], mask="causal", dtype=dtype, seed=at, k=k, v=v)
+        c.check(*_run(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L", [2, 20])
+def test_hidden_slots_may_hold_anything(L, dtype):
+    """A block's slots that some rows do not see hold NaN, infinite and huge heads: those rows are as if they were not there."""
+    dt = TYPES[dtype]
+    top = torch.finfo(dt).max
+    lens = [L, 90]
+    c = Case4(brisk, 2, L, 4, 2, 64, None, lens, mask="causal", dtype=dtype, seed=3)
+    clean = _run(c)
+    for bad in (float("nan"), float("inf"), top):
+        k, v = c.k.clone(), c.v.clone()
+        for b, n in enumerate(lens):
+            k[b, n - 1], v[b, n - 1] = bad, bad
+            v[b, n - 1, :, ::2] = 0.0               # a large step
+        d = Case4(brisk, 2, L, 4, 2, 64, None, lens, mask="causal", dtype=dtype, seed=3, k=k, v=v)
+        d.q = c.q                                    # (the generator of a case with given tokens draws other queries)
+        out, lse = _run(d)
+        o, z, tol, ltol = c.expect()
+        # all rows but the last position's
+        got = (out[:, :L - 1].double().cpu().numpy(), lse[:, :L - 1].double().cpu().numpy())
+        assert (np.abs(got[0] - o[:, :L - 1]) <= tol[:, :L - 1] + 2.0 ** -12).all()
+        assert (np.abs(got[1] - z[:, :L - 1]) <= ltol[:, :L - 1]).all()
+        if bad != top:
+            assert out[:, L - 1].isnan().all()
+    assert not clean[0].isnan().any()
+
+
+def test_pages_past_a_sequence_may_hold_anything():
+    """Unwritten places, inside the last page and in pages of nobody, hold every byte value in turn."""
+    for fill in (0x00, 0x7F, 0x80, 0xFF, 0x7C):
+        c = Case4(brisk, 3, 4, 8, 2, 128, None, [5, 33, 100], mask="causal", page=64, seed=8, fill=fill)
+        c.check(*_run(c))
+
+
+def test_logits_far_past_the_exponent_range():
+    """Logits of +-1e7 and more: differences of them still decide."""
+    for L, dtype in ((1, "bf16"), (6, "bf16"), (1, "f16"), (6, "f16")):
+        c = Case4(brisk, 1, L, 4, 1, 64, None, [77], dtype=dtype, seed=11)
+        c.scale = 1e6
+        out, lse = _run(c)
+        o, z, tol, ltol = c.expect()
+        # where the best key leads by more than the logits' errors the row is that key's value
+        sure = []
+        from kv4_cases import hold
+        kz, ks, kc = (np.broadcast_to(y, c.k.shape)[0, :77, 0] for y in hold(c.k, dtype))
+        for i in range(L):
+            for h in range(4):
+                s = np.sort(c.scale * ((kz + ks * kc) @ c.q.double().numpy()[0, i, h]))
+                sure.append(s[-1] - s[-2] > 2 * ltol[0, i, h] + 40)
+        sure = np.array(sure).reshape(1, L, 4)
+        assert sure.any()
+        err = np.abs(out.double().cpu().numpy() - o)
+        assert (err[sure] <= UNIT[dtype] * (np.abs(o) + 16)[sure]).all()
+        assert (np.abs(lse.double().cpu().numpy() - z) <= ltol).all()
+
+
+def test_weak_keys_in_long_runs_count():
+    """One key of weight 1 and value 0 among 40000 of weight 2^-20: 3.7 percent are theirs."""
+    for dtype in ("bf16", "f16"):
+        dt, n, D = TYPES[dtype], 40000, 64
+        k, v = torch.zeros(1, n, 1, D, dtype=dt), torch.ones(1, n, 1, D, dtype=dt)
+        v[..., 1::2] = 0.5
+        k[:, :, 0, 0] = 0.0
+        k[:, n // 3, 0, 0] = 15.0                    # of a step of 1: held as it is (16 would be held as 15 type(16 / 15))
+        v[:, n // 3] = 0.0
+        c = Case4(brisk, 1, 1, 1, 1, D, None, [n], dtype=dtype, k=k, v=v, page=64)
+        c.q.zero_()
+        c.q[..., 0] = 1.0
+        c.scale = 20 * np.log(2.0) / 15
+        out, lse = _run(c)
+        total = 1 + (n - 1) * 2.0 ** -20
+        weak = (n - 1) * 2.0 ** -20 / total
+        got = out[0, 0, 0].double().cpu().numpy()
+        assert np.abs(got[0::2] - weak).max() <= 3 * UNIT[dtype] * weak + 2.0 ** -20
+        assert np.abs(got[1::2] - weak / 2).max() <= 3 * UNIT[dtype] * weak + 2.0 ** -20
+        assert abs(lse.item() - (c.scale * 15 + np.log(total))) <= 2.0 ** -18 * 14
+
+
+def test_length_bound_and_table_are_clamped():
+    c = Case4(brisk, 3, 2, 8, 2, 128, None, [90, 40, 7], mask="causal", seed=4)
+    want = c.expect()
+    c.seq_len.copy_(torch.tensor([1 << 30, 40, 7], dtype=torch.int32))
+    out, lse = _run(c, max_seq_len=90)
+    c.check(out, lse, want)
+    c.seq_len.copy_(torch.tensor([-5, 0, 7], dtype=torch.int32))
+    out, lse = _run(c)
+    assert (out[:2] == 0).all() and (lse[:2] == -np.inf).all() and torch.isfinite(lse[2]).all()
+
+
+@pytest.mark.parametrize("prefix", [0, None, 40])
+def test_zero_length_bound(prefix):
+    c = Case4(brisk, 3, 2, 8, 2, 64, prefix, [0, 0, 0], mask="none", seed=4)
+    c.check(*_run(c, max_seq_len=0))
+
+
+def test_strided_queries_outputs_and_no_lse_bands():
+    """Queries as columns of a projection; outputs between bands that stay."""
+    c = Case4(brisk, 3, 5, 8, 2, 80, 30, [5, 60, 200], mask="causal", seed=12)
+    want = c.expect()
+    x = torch.randn(3, 5, 12, 80).to(torch.bfloat16).cuda()
+    x[:, :, :8] = c.q.cuda()
+    raw = torch.full((2048 + 3 * 5 * 8 * 80,), 9.0, dtype=torch.bfloat16, device="cuda")
+    z = torch.full((128 + 3 * 5 * 8,), 9.0, device="cuda")
+    out, lse = raw[1024:-1024].view(3, 5, 8, 80), z[64:-64].view(3, 5, 8)
+    brisk.kv4_attention(x[:, :, :8], c.cache, prefix=c.gpu_prefix(), block_mask=c.gpu_mask(), scale=c.scale, out=out, lse=lse)
+    c.check(out, lse, want)
+    assert (raw[:1024] == 9).all() and (raw[-1024:] == 9).all() and (z[:64] == 9).all() and (z[-64:] == 9).all()
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 4 GiB, a sequence in its first and last pages."""
+    page, Hkv, D, n = 64, 8, 128, 128
+    part = brisk.kv4_page_bytes(page, D)
+    n_pages = (1 << 32) // (Hkv * part) + 3
+    pages = torch.empty(n_pages, Hkv, part, dtype=torch.uint8, device="cuda")
+    small = Case4(brisk, 1, 3, 16, Hkv, D, None, [n], mask="causal", page=page, seed=14)
+    cache = brisk.KVCache4(pages, torch.tensor([[n_pages - 1, 0]], dtype=torch.int32, device="cuda"), small.seq_len, D)
+    brisk.kv4_write(small.k.cuda(), small.v.cuda(), cache, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    a = brisk.kv4_attention(small.q.cuda(), cache, block_mask=small.gpu_mask())
+    b = brisk.kv4_attention(small.q.cuda(), small.cache, block_mask=small.gpu_mask())
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_runs_are_deterministic_and_graphs_keep_their_own_scratch():
+    """Two graphs of one shape, replayed in turn with eager calls between: each replay is the eager result."""
+    c = [Case4(brisk, 2, 4, 8, 2, 128, 300, [500, 1900], mask="causal", seed=s) for s in (1, 2)]
+    q = [x.q.cuda() for x in c]
+    pre, mask = [x.gpu_prefix() for x in c], [x.gpu_mask() for x in c]
+    call = lambda i: brisk.kv4_attention(q[i], c[i].cache, prefix=pre[i], block_mask=mask[i], scale=c[i].scale)  # noqa: E731
+    eager = [call(i) for i in range(2)]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call(i))
+        graphs.append(g)
+    for turn in range(4):
+        for i in range(2):
+            outs[i][0].zero_()
+            graphs[i].replay()
+            again = call(1 - i)
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i][0], eager[i][0]) and torch.equal(outs[i][1], eager[i][1])
+            assert torch.equal(again[0], eager[1 - i][0])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    other = brisk.kv4_attention(q[0], c[0].cache, prefix=pre[0], block_mask=mask[0], scale=c[0].scale, stream=s)
+    mine = call(1)
+    torch.cuda.synchronize()
+    assert torch.equal(other[0], eager[0][0]) and torch.equal(mine[0], eager[1][0])
+
+
+def test_write_attend_and_grow():
+    """Decoding as it is done: a prompt, then blocks of which some tokens are kept, against the oracle at every step."""
+    B, L, H, Hkv, D, page = 3, 5, 8, 2, 64, 16
+    rng = np.random.default_rng(0)
+    full = Case4(brisk, B, L, H, Hkv, D, 20, [90] * B, mask="causal", seed=21)
+    pages = pages_for(brisk, 24, Hkv, D, page)
+    table = torch.from_numpy(rng.permutation(24)[:18].reshape(B, 6).astype(np.int32)).cuda()
+    n = torch.tensor([30, 1, 47], dtype=torch.int32, device="cuda")
+    cache = brisk.KVCache4(pages, table, n, D)
+    k, v = full.k.cuda(), full.v.cuda()
+    zero = torch.zeros_like(n)
+    brisk.kv4_write(k[:, :47], v[:, :47], cache, zero, count=n)
+    lens = n.cpu().numpy().copy()
+    for step in range(4):
+        # the block of a sequence of n tokens: its tokens n .. n + L - 1, all of them drafts that some of are kept
+        at = n.long()[:, None] + torch.arange(L, device="cuda")
+        rows = torch.arange(B, device="cuda")[:, None]
+        brisk.kv4_write(k[rows, at], v[rows, at], cache, n)
+        n += L
+        full.lens = (lens + L).tolist()
+        out, lse = brisk.kv4_attention(full.q.cuda(), cache, prefix=full.gpu_prefix(), block_mask=full.gpu_mask(), scale=full.scale)
+        full.check(out, lse)
+        kept = rng.integers(1, L + 1, B)
+        lens = lens + kept
+        n.copy_(torch.from_numpy(lens.astype(np.int32)))
+
+
+def test_refusals_of_the_binding():
+    c = Case4(brisk, 2, 3, 8, 2, 64, 10, [30, 40], mask="causal", seed=1)
+    q, pre, mask = c.q.cuda(), c.gpu_prefix(), c.gpu_mask()
+    for bad in (dict(q=q.half()), dict(prefix=(pre[0].half(), pre[1])), dict(block_mask=mask.int()),
+                dict(out=torch.empty_like(q).float()), dict(cache=None)):
+        with pytest.raises(TypeError):
+            brisk.kv4_attention(**{**dict(q=q, cache=c.cache), **bad})
+    for bad in (dict(q=q[:1]), dict(q=q[..., :56]), dict(prefix=(pre[0][:, :1], pre[1])), dict(block_mask=mask[:1]),
+                dict(out=torch.empty_like(q)[:, :2]), dict(lse=torch.empty(2, 3, 4, device="cuda")),
+                dict(workspace=torch.empty(4, dtype=torch.uint8, device="cuda"), prefix=pre), dict(q=q.cpu())):
+        with pytest.raises(ValueError):
+            brisk.kv4_attention(**{**dict(q=q, cache=c.cache), **bad})
+    for bad in (dict(q=q[:, :, :7]), dict(scale=-1.0), dict(max_seq_len=1 << 20), dict(q=q[:, :0])):
+        with pytest.raises(brisk.BriskError):
+            brisk.kv4_attention(**{**dict(q=q, cache=c.cache), **bad})
+    plain = Case(1, 1, 4, 2, 64, None, [5]).cache(brisk)
+    with pytest.raises(TypeError):
+        brisk.kv4_attention(torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16, device="cuda"), plain)

@@ -1,0 +1,330 @@
+"""GPU checks of brisk_kv4_write and brisk_kv4_read against the float64 oracle.
+
+How a head is held is defined to the bit (each of its roundings is to nearest
+even), so what is read back has to be equal."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.kv4_oracle as k4
+from kv4_cases import LEAST, hold, pages_for, read_back, rounder
+from kv_cases import TYPES
+
+pytestmark = pytest.mark.gpu
+
+brisk = pytest.importorskip("paper_2609_33390_amd")
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _cache(B, Hkv, D, page, cols, dtype="bf16", lens=None, seed=0, fill=0xFF):
+    """A cache whose sequences own `cols` pages each, in no order."""
+    order = torch.randperm(B * cols + 1, generator=torch.Generator().manual_seed(seed))[:B * cols]
+    table = order.to(torch.int32).view(B, cols).cuda()
+    n = _i32([cols * page] * B if lens is None else lens)
+    return brisk.KVCache4(pages_for(brisk, B * cols + 1, Hkv, D, page, fill), table, n, D, TYPES[dtype])
+
+
+def _tokens(B, T, Hkv, D, dtype="bf16", seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(B, T, Hkv, D, generator=g) * torch.exp(torch.randn(Hkv, D, generator=g))).to(TYPES[dtype])
+            for _ in range(2)]
+
+
+def _same(a, b):
+    """Equal values, NaN with NaN."""
+    return torch.equal(torch.nan_to_num(a.float(), nan=1e38), torch.nan_to_num(b.float(), nan=1e38)) and \
+        torch.equal(a.isnan(), b.isnan())
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=1, T=1, Hkv=1, D=128), dict(B=3, T=1, Hkv=8, D=128), dict(B=2, T=16, Hkv=2, D=64, page=64),
+    dict(B=2, T=37, Hkv=3, D=80, dtype="f16", page=32), dict(B=1, T=300, Hkv=4, D=128, dtype="f16", page=128),
+    dict(B=5, T=64, Hkv=2, D=96), dict(B=2, T=33, Hkv=5, D=8), dict(B=2, T=17, Hkv=1, D=24, dtype="f16"),
+    dict(B=1, T=50, Hkv=2, D=72, page=1024), dict(B=1, T=40, Hkv=1, D=120), dict(B=2, T=20, Hkv=2, D=56, dtype="f16"),
+])
+def test_what_is_read_is_what_the_definition_holds(kw):
+    page, dtype = kw.pop("page", 16), kw.pop("dtype", "bf16")
+    B, T, Hkv, D = kw["B"], kw["T"], kw["Hkv"], kw["D"]
+    print(f"[kv4] {kw} page={page} {dtype}", flush=True)
+    cache = _cache(B, Hkv, D, page, -(-T // page), dtype)
+    k, v = _tokens(B, T, Hkv, D, dtype, seed=T)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0] * B))
+    rk, rv = brisk.kv4_read(cache, T)
+    assert torch.equal(rk.cpu(), read_back(k, dtype)) and torch.equal(rv.cpu(), read_back(v, dtype))
+    for x, y in ((k, rk), (v, rv)):               # and that is as near as a step allows
+        _, s, _ = hold(x, dtype)
+        assert (np.abs(x.double().numpy() - y.double().cpu().numpy()) <= (0.5 + 2.0 ** -5) * s + 2.0 ** -8 * np.abs(x.double().numpy())).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_ties_between_codes(dtype):
+    """Heads on grids whose elements lie exactly between two codes, below and above them by one ulp."""
+    dt, rng = TYPES[dtype], np.random.default_rng(3)
+    rows = []
+    for _ in range(512):
+        s = float(2.0 ** rng.integers(-8, 8)) * (1 + rng.integers(0, 8) / 8)
+        z = s * float(rng.integers(-40, 40)) / 2
+        c = rng.integers(0, 31, 64) / 2.0
+        c[:2] = 0, 15
+        x = torch.from_numpy(z + s * c).to(dt)
+        near = x.clone().view(torch.int16)
+        near[2:] += torch.from_numpy(rng.integers(-1, 2, 62)).to(torch.int16) * (x[2:] != 0)
+        rows.append(near.view(dt))
+    k = torch.stack(rows).view(1, 64, 8, 64)
+    cache = _cache(1, 8, 64, 16, 4, dtype)
+    brisk.kv4_write(k.cuda(), k.flip(-1).contiguous().cuda(), cache, _i32([0]))
+    rk, rv = brisk.kv4_read(cache, 64)
+    assert torch.equal(rk.cpu(), read_back(k, dtype)) and torch.equal(rv.cpu(), read_back(k.flip(-1).contiguous(), dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 80, 128])
+def test_every_pair_of_numbers(dtype, D):
+    """Elements of any exponent beside each other, subnormal numbers and both zeros among them."""
+    dt = TYPES[dtype]
+    g = torch.Generator().manual_seed(5)
+    bits = torch.randint(-32768, 32768, (1, 512, 4, D), generator=g).to(torch.int16)
+    bits[:, 256:] &= 0x83FF                         # small numbers only
+    bits[:, 300:310] &= ~0x7FFF                     # zeros of both signs
+    k = bits.view(dt).clone()
+    v = k.roll(7, 1)
+    cache = _cache(1, 4, D, 32, 16, dtype)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0]))
+    rk, rv = brisk.kv4_read(cache, 512)
+    assert _same(rk.cpu(), read_back(k, dtype)) and _same(rv.cpu(), read_back(v, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_heads_that_are_not_finite_or_flat(dtype):
+    dt, D = TYPES[dtype], 128
+    top = torch.finfo(dt).max
+    k, v = _tokens(1, 16, 2, D, dtype)
+    k[0, 0, 0, 5], k[0, 1, 0, 127], k[0, 2, 1, 0], v[0, 3, 0, 64] = float("nan"), float("inf"), -float("inf"), float("nan")
+    k[0, 4], v[0, 4], k[0, 5], v[0, 5] = 3.5, -0.0, top, -top        # flat
+    k[0, 6, :, 0], k[0, 6, :, 1] = top, -top                          # the range is not finite in fp32 (bf16 only)
+    v[0, 7], v[0, 7, :, 3] = 1.0, 1.0 + torch.finfo(dt).eps
+    cache = _cache(1, 2, D, 16, 1, dtype)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0]))
+    rk, rv = (x.cpu() for x in brisk.kv4_read(cache, 16))
+    assert _same(rk, read_back(k, dtype)) and _same(rv, read_back(v, dtype))
+    assert rk[0, 0, 0].isnan().all() and rk[0, 1, 0].isnan().all() and rk[0, 2, 1].isnan().all() and rv[0, 3, 0].isnan().all()
+    assert not rk[0, 0, 1].isnan().any() and not rv[0, 0].isnan().any()
+    assert (rk[0, 4] == 3.5).all() and (rv[0, 4] == 0).all() and (rk[0, 5] == top).all() and (rv[0, 5] == -top).all()
+    assert rk[0, 6].isnan().all() == (dtype == "bf16")
+
+
+def test_tokens_go_where_they_are_told_and_nothing_else_changes():
+    """Blocks that begin anywhere, of different counts: written twice over a cache that holds others."""
+    B, T, Hkv, D, page, cols = 7, 21, 2, 80, 32, 4
+    cache = _cache(B, Hkv, D, page, cols, "f16")
+    k0, v0 = _tokens(B, page * cols, Hkv, D, "f16", 1)
+    brisk.kv4_write(k0.cuda(), v0.cuda(), cache, _i32([0] * B))
+    k, v = _tokens(B, T, Hkv, D, "f16", 2)
+    first, count = [0, 1, 31, 64, 90, 100, 127], [21, 0, 1, 16, 21, 7, 21]
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32(first), count=_i32(count))
+    wk, wv = read_back(k0, "f16"), read_back(v0, "f16")
+    for b in range(B):
+        for t in range(count[b]):
+            if first[b] + t < page * cols:
+                wk[b, first[b] + t], wv[b, first[b] + t] = read_back(k[b, t], "f16"), read_back(v[b, t], "f16")
+    rk, rv = brisk.kv4_read(cache, page * cols)
+    assert torch.equal(rk.cpu(), wk) and torch.equal(rv.cpu(), wv)
+    spare = [p for p in range(B * cols + 1) if p not in cache.block_table.cpu().flatten().tolist()]
+    assert (cache.pages[spare] == 0xFF).all()     # a page of nobody
+
+
+@pytest.mark.parametrize("W", [64, 128])
+def test_a_token_writes_its_own_bytes_only(W):
+    """Every byte of a block belongs to one slot: 16 single tokens leave what one call leaves, and each changes
+    bytes that no other one does."""
+    k, v = _tokens(1, 16, 1, W, seed=9)
+    whole = _cache(1, 1, W, 16, 1, fill=0)
+    brisk.kv4_write(k.cuda(), v.cuda(), whole, _i32([0]))
+    one = _cache(1, 1, W, 16, 1, fill=0)
+    seen = torch.zeros_like(one.pages, dtype=torch.int32)
+    for t in torch.randperm(16, generator=torch.Generator().manual_seed(1)).tolist():
+        before = one.pages.clone()
+        brisk.kv4_write(k[:, t:t + 1].cuda(), v[:, t:t + 1].cuda(), one, _i32([t]))
+        seen += (one.pages != before).int()
+    assert torch.equal(one.pages, whole.pages)
+    assert seen.max() == 1
+
+
+@pytest.mark.parametrize("first,count", [(-5, None), (-40, None), (60, None), (64, None), (2 ** 31 - 8, None), (-2 ** 31, None),
+                                         (0, -3), (0, 99), (50, 2 ** 31 - 1)])
+def test_slots_outside_the_table_are_passed_over(first, count):
+    B, T, Hkv, D = 1, 20, 2, 64
+    cache = _cache(B, Hkv, D, 16, 4)
+    k, v = _tokens(B, T, Hkv, D, seed=4)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([first]), count=None if count is None else _i32([count]))
+    want = torch.full((1, 64, Hkv, D), float("nan"), dtype=torch.bfloat16)
+    for t in range(T if count is None else max(0, min(T, count))):
+        if 0 <= first + t < 64:
+            want[0, first + t] = read_back(k[0, t], "bf16")
+    assert _same(brisk.kv4_read(cache, 64)[0].cpu(), want)
+    # a read from there gives what is held, and zeros
+    got = brisk.kv4_read(cache, T, first=_i32([first]))[0].cpu()
+    at = [want[0, first + t] if 0 <= first + t < 64 else torch.zeros(Hkv, D, dtype=torch.bfloat16) for t in range(T)]
+    assert _same(got[0], torch.stack(at))
+
+
+def test_read_ends_with_the_sequence():
+    lens = [0, 1, 15, 16, 17, 63, 64, -4, 1000]
+    cache = _cache(len(lens), 3, 96, 16, 4, lens=lens)
+    k, v = _tokens(len(lens), 64, 3, 96, seed=6)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0] * len(lens)))
+    for T in (1, 16, 64, 70):
+        rk, rv = brisk.kv4_read(cache, T)
+        for b, n in enumerate(lens):
+            n = max(0, min(n, 64))
+            for r, x in ((rk, k), (rv, v)):
+                assert torch.equal(r[b, :n].cpu(), read_back(x[b, :min(n, T)], "bf16")) and (r[b, n:] == 0).all()
+
+
+def test_strided_tokens_and_pages():
+    """Columns of a fused projection into one layer of a pool of several, heads apart; what lies between stays."""
+    B, T, H, Hkv, D, page, n_pages = 3, 19, 6, 2, 64, 16, 7
+    part = brisk.kv4_page_bytes(page, D)
+    pool = torch.full((n_pages, 3, Hkv, part + 32), 0x5A, dtype=torch.uint8, device="cuda")
+    pages = pool[:, 1, :, :part]
+    table = torch.tensor([[3, 0], [5, 6], [1, 4]], dtype=torch.int32, device="cuda")
+    cache = brisk.KVCache4(pages, table, _i32([19] * B), D)
+    x = torch.randn(B, T + 3, H + 2 * Hkv, D, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    g = x.cuda()[:, 2:2 + T]
+    brisk.kv4_write(g[:, :, H:H + Hkv], g[:, :, H + Hkv:], cache, _i32([0] * B))
+    rk, rv = brisk.kv4_read(cache, T)
+    h = x[:, 2:2 + T]
+    assert torch.equal(rk.cpu(), read_back(h[:, :, H:H + Hkv].contiguous(), "bf16"))
+    assert torch.equal(rv.cpu(), read_back(h[:, :, H + Hkv:].contiguous(), "bf16"))
+    assert (pool[:, 0] == 0x5A).all() and (pool[:, 2] == 0x5A).all() and (pool[..., part:] == 0x5A).all()
+    assert (pool[2] == 0x5A).all()
+    # pages inside heads
+    other = torch.full((Hkv, n_pages, part), 0x5A, dtype=torch.uint8, device="cuda").transpose(0, 1)
+    c2 = brisk.KVCache4(other, table, _i32([19] * B), D)
+    brisk.kv4_write(g[:, :, H:H + Hkv], g[:, :, H + Hkv:], c2, _i32([0] * B))
+    assert torch.equal(brisk.kv4_read(c2, T)[0], rk)
+
+
+def test_expanded_tokens():
+    """One token's heads for all sequences and positions: strides of 0."""
+    cache = _cache(3, 2, 64, 16, 2)
+    k = torch.randn(1, 1, 1, 64, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    e = k.cuda().expand(3, 20, 2, 64)
+    brisk.kv4_write(e, e, cache, _i32([0, 5, 12]))
+    rk, rv = brisk.kv4_read(cache, 20, first=_i32([0, 5, 12]))
+    want = read_back(k, "bf16").expand(3, 20, 2, 64)
+    assert torch.equal(rk.cpu(), want) and torch.equal(rv.cpu(), want)
+
+
+def test_page_ids_are_clamped():
+    cache = _cache(1, 1, 64, 16, 3)
+    n_pages = cache.pages.shape[0]
+    cache.block_table.copy_(torch.tensor([[-7, 1, 1 << 30]], dtype=torch.int32))
+    k, v = _tokens(1, 48, 1, 64)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0]))
+    cache.block_table.copy_(torch.tensor([[0, 1, n_pages - 1]], dtype=torch.int32))
+    assert torch.equal(brisk.kv4_read(cache, 48)[0].cpu(), read_back(k, "bf16"))
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 4 GiB, its first and last pages in use."""
+    page, Hkv, D = 64, 8, 128
+    part = brisk.kv4_page_bytes(page, D)
+    n_pages = (1 << 32) // (Hkv * part) + 3
+    pages = torch.empty(n_pages, Hkv, part, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[n_pages - 1, 0]], dtype=torch.int32, device="cuda")
+    cache = brisk.KVCache4(pages, table, _i32([128]), D)
+    k, v = _tokens(1, 128, Hkv, D, seed=3)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0]))
+    rk, rv = brisk.kv4_read(cache, 128)
+    assert torch.equal(rk.cpu(), read_back(k, "bf16")) and torch.equal(rv.cpu(), read_back(v, "bf16"))
+
+
+def test_guard_bands():
+    """Outputs and pages between bands that stay as they were."""
+    B, T, Hkv, D = 2, 37, 3, 72
+    part = brisk.kv4_page_bytes(16, D)
+    band = 4096
+    raw = torch.full((band * 2 + 6 * Hkv * part,), 0xA5, dtype=torch.uint8, device="cuda")
+    pages = raw[band:-band].view(6, Hkv, part)
+    table = torch.tensor([[5, 0, 2], [1, 4, 3]], dtype=torch.int32, device="cuda")
+    cache = brisk.KVCache4(pages, table, _i32([37, 20]), D)
+    k, v = _tokens(B, T, Hkv, D)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([0, 11]))
+    outs = [torch.full((band + B * T * Hkv * D,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    shaped = [o[band // 2:-(band // 2)].view(B, T, Hkv, D) for o in outs]
+    brisk.kv4_read(cache, T, k=shaped[0], v=shaped[1])
+    assert (raw[:band] == 0xA5).all() and (raw[-band:] == 0xA5).all()
+    for o in outs:
+        assert (o[:band // 2] == 7).all() and (o[-(band // 2):] == 7).all()
+    assert torch.equal(shaped[0][0].cpu(), read_back(k[0], "bf16"))
+
+
+def test_other_stream_and_graph():
+    """On a stream of the caller's, and captured: every replay writes and reads the tokens of its time."""
+    cache = _cache(2, 2, 64, 16, 2)
+    k, v = (x.cuda() for x in _tokens(2, 9, 2, 64))
+    first = _i32([3, 14])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    brisk.kv4_write(k, v, cache, first, stream=s)
+    rk, rv = brisk.kv4_read(cache, 9, first=first, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(rk.cpu(), read_back(k.cpu(), "bf16"))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        brisk.kv4_write(k, v, cache, first)
+        rk, rv = brisk.kv4_read(cache, 9, first=first)
+    for i in range(4):
+        a, b = _tokens(2, 9, 2, 64, seed=20 + i)
+        k.copy_(a)
+        v.copy_(b)
+        first.copy_(_i32([i, 20 - i]))
+        graph.replay()
+        assert torch.equal(rk.cpu(), read_back(a, "bf16")) and torch.equal(rv.cpu(), read_back(b, "bf16"))
+
+
+def test_refusals_of_the_binding():
+    cache = _cache(2, 2, 64, 16, 2)
+    k, v = (x.cuda() for x in _tokens(2, 5, 2, 64))
+    first = _i32([0, 0])
+    for bad in (dict(k=k.half()), dict(v=v.half()), dict(first=first.long())):
+        with pytest.raises(TypeError):
+            brisk.kv4_write(**{**dict(k=k, v=v, cache=cache, first=first), **bad})
+    for bad in (dict(k=k[:1]), dict(k=k[:, :, :1]), dict(v=v[:, :4]), dict(k=k[..., :56]), dict(first=first[:1]),
+                dict(count=first[:1]), dict(v=v.transpose(1, 2).contiguous().transpose(1, 2)), dict(k=k.transpose(2, 3)),
+                dict(k=k.cpu()), dict(first=first.cpu())):
+        with pytest.raises(ValueError):
+            brisk.kv4_write(**{**dict(k=k, v=v, cache=cache, first=first), **bad})
+    with pytest.raises(brisk.BriskError):
+        brisk.kv4_write(k[:, :0], v[:, :0], cache, first)
+    with pytest.raises(brisk.BriskError):
+        brisk.kv4_read(cache, 0)
+    for bad in (dict(k=k[:, :4]), dict(v=v[:1]), dict(first=first[:1])):
+        with pytest.raises(ValueError):
+            brisk.kv4_read(cache, 5, **bad)
+    with pytest.raises(TypeError):
+        brisk.kv4_read(cache, 5, k=k.half())
+    pages, table, n = cache.pages, cache.block_table, cache.seq_len
+    for bad, err in (((pages[..., :-8], table, n, 64), ValueError), ((pages, table.long(), n, 64), TypeError),
+                     ((pages, table, n[:1], 64), ValueError), ((pages, table, n, 128), ValueError),
+                     ((pages, table, n, 60), brisk.BriskError), ((pages, table, n, 64, torch.float32), TypeError)):
+        with pytest.raises(err):
+            brisk.KVCache4(*bad)
+    with pytest.raises(AttributeError):
+        cache.seq_len = n.clone()
+    # two heads of a pool that are one in memory
+    one = pages[:, :1].expand(-1, 2, -1)
+    with pytest.raises(brisk.BriskError):
+        brisk.kv4_write(k, v, brisk.KVCache4(one, table, n, 64), first)
+
+
+def test_definition_of_the_oracle():
+    """The oracle's own codes, on heads worked out by hand."""
+    x = np.array([[0.0, 15.0, 7.5, 6.5, 0.4, 0.6, 14.4, 1.0]])
+    z, s, c = k4.hold(x, rounder("bf16"), LEAST["bf16"])
+    assert z == 0 and s == 1 and c.tolist() == [[0, 15, 8, 6, 0, 1, 14, 1]]
