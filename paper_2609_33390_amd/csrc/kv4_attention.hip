@@ -14,8 +14,6 @@
 // Codes come from memory to registers in operand order, 32 slots of a head a step
 // of a wavefront, the next ones' on the way; the wavefronts of a workgroup take
 // steps in turn and join through LDS.
-#include <type_traits>
-
 #include "attention_plan.h"
 #include "kernels.h"
 #include "kv4_common.h"
@@ -97,30 +95,16 @@ __device__ __forceinline__ float swap16_max(float v) {
 }
 __device__ __forceinline__ uint32_t part_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// What a wavefront loads of 32 slots: two blocks.  M = 16 rows: a lane has chunk `lane` of
-// each block.  M = 32: it has two chunks of the keys of its own slot, and of each block its half
-// of two chunks of values.
-template <int W, int M>
-struct Slots {
-  static constexpr int NQ = M == 16 ? 2 : 4;       // groups of four slots, of which this lane has the logits
-  static constexpr int NV = M == 16 ? W / 32 : 4;
-  uint32_t k[2][W / 32], v[2][NV];
-  uint4 kp[NQ], vp[NQ];
-  uint32_t mark;                                   // the pair of value `lane % 32`
-};
-
-// M rows a workgroup, KW wavefronts.
-template <bool F16, int W, int M, int KW>
-__global__ __launch_bounds__(64 * KW, M == 16 ? 4 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
-  constexpr int NQ = Slots<W, M>::NQ, NS = 4 * NQ, NO = M == 16 ? W / 16 : W / 32, NF = W / 32;
-  constexpr int R = M == 16 ? 4 : 16;              // registers of an accumulator
-  constexpr int kStep = 32;                        // slots of a wavefront's step
+// RT tiles of 16 rows a workgroup, KW wavefronts.
+template <bool F16, int W, int RT, int KW>
+__global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
+  constexpr int M = 16 * RT, NF = W / 32, NO = W / 16, kStep = 32;   // kStep: slots of a wavefront's step
   constexpr int kOutRow = W + 4;
-  using Acc = std::conditional_t<M == 16, floatx4, floatx16>;
   __shared__ __attribute__((aligned(16))) float acc[KW * M * kOutRow];
   __shared__ float stat[KW * M * 2];
+  __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys and values
 
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, t = lane >> 4, x = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.H / a.Hkv;
   const int bid = blockIdx.x, group = bid / 8 / p.tiles * 8 + bid % 8, tile = bid / 8 % p.tiles;
@@ -141,236 +125,254 @@ __global__ __launch_bounds__(64 * KW, M == 16 ? 4 : 2) void kv4_attend_kernel(Kv
   }
   const bool masked = a.mask != nullptr;
 
-  // M = 16: quarter t, row or slot or element x.  M = 32: half t, x = col % 16.
-  const int col = M == 16 ? lane & 15 : lane & 31, t = M == 16 ? lane >> 4 : lane >> 5, x = lane & 15;
-
-  // ---- queries, as the second operand of K Q^T, and their sums
-  constexpr int NQF = M == 16 ? NF : 2 * NF;
-  uint4 q[NQF];
-  uint64_t word;
-  float qsum = 0.f;
-  {
-    const int row = row0 + min(col, rows - 1), bi = row / G;
-    const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
-    word = masked ? a.mask[bi] : ~0ull;
+  // ---- queries, as the second operand of K Q^T: row x of each tile, elements t W / 4 + ...
+  uint4 q[RT][NF];
+  uint64_t word[RT];                               // what its rows see of the block
+  floatx4 start[RT];                               // what the products begin from
+  // f16 logits are held 2^-21 of what they are
+  const float c = a.scale * kLog2e * (F16 ? 0x1p21f : 1.f);
+  float qz[RT];                                    // sum of q, as the logits are held
 #pragma unroll
-    for (int i = 0; i < NQF; ++i) {
-      const int e = t * (M == 16 ? W / 4 : W / 2) + 8 * i;
-      q[i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
+  for (int r = 0; r < RT; ++r) {
+    const int row = row0 + min(16 * r + x, rows - 1), bi = row / G;
+    const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
+    word[r] = masked ? a.mask[bi] : ~0ull;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int e = t * (W / 4) + 8 * i;
+      q[r][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        qsum += half_to_f32<F16>(part_of(q[i], w) & 0xFFFF) + half_to_f32<F16>(part_of(q[i], w) >> 16);
+        sum += half_to_f32<F16>(part_of(q[r][i], w) & 0xFFFF) + half_to_f32<F16>(part_of(q[r][i], w) >> 16);
     }
-    if constexpr (M == 16) qsum = swap16_sum(qsum);
-    qsum = swap32_sum(qsum);
+    sum = swap32_sum(swap16_sum(sum));
+    qz[r] = F16 ? sum * 0x1p-21f : sum;
+    start[r] = floatx4{} + (F16 ? 0.f : -16.f * sum);
   }
-  Acc start;                                       // what the products begin from
-#pragma unroll
-  for (int r = 0; r < R; ++r) start[r] = F16 ? 0.f : -16.f * qsum;
-  // f16 logits are held 2^-21 of what they are
-  const float c = a.scale * kLog2e * (F16 ? 0x1p21f : 1.f), qz = F16 ? qsum * 0x1p-21f : qsum;
 
-  // ---- loads
-  using Raw = Slots<W, M>;
+  // ---- loads.  Step i of this wavefront begins at slot key0 + 32 (KW i + wave); lane 2 i + k holds the page of
+  // its block k, for 32 steps, and those of the next 32 are on their way.
   const int last = max(key1 - 1, 0) & ~(kKv4Block - 1);
-  auto load = [&](int j0, Raw& s) {
-    const uint8_t* blk[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) blk[i] = kv4_block<W>(a.kv, b, hk, min(j0 + 16 * i, last));
-    if constexpr (M == 16) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if constexpr (W == 128) {
-          const uint4 kw = *reinterpret_cast<const uint4*>(blk[i] + lane * 16);
-          const uint4 vw = *reinterpret_cast<const uint4*>(blk[i] + 8 * W + lane * 16);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) s.k[i][w] = part_of(kw, w), s.v[i][w] = part_of(vw, w);
-        } else {
-          const uint2 kw = *reinterpret_cast<const uint2*>(blk[i] + lane * 8);
-          const uint2 vw = *reinterpret_cast<const uint2*>(blk[i] + 8 * W + lane * 8);
-          s.k[i][0] = kw.x, s.k[i][1] = kw.y, s.v[i][0] = vw.x, s.v[i][1] = vw.y;
-        }
-        s.kp[i] = *reinterpret_cast<const uint4*>(blk[i] + 16 * W + 16 * t);
-        s.vp[i] = *reinterpret_cast<const uint4*>(blk[i] + 16 * W + 64 + 16 * t);
-      }
-    } else {
-      const uint8_t* own = col < 16 ? blk[0] : blk[1];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {                // chunks 2 t + i of the lane's slot; chunks t + 2 u of both blocks' values
-        const uint8_t* kc = own + (16 * (2 * t + i) + x) * (W / 8);
-        if constexpr (W == 128) {
-          const uint4 kw = *reinterpret_cast<const uint4*>(kc);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) s.k[i][w] = part_of(kw, w);
-        } else {
-          const uint2 kw = *reinterpret_cast<const uint2*>(kc);
-          s.k[i][0] = kw.x, s.k[i][1] = kw.y;
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {              // W = 128: elements x + 64 (col / 16) + 16 d; W = 64: x + 32 (col / 16) + 16 d
-          const uint2 vw = *reinterpret_cast<const uint2*>(blk[i] + 8 * W + (16 * (t + 2 * u) + x) * (W / 8) + (W == 128 ? 8 * (col / 16) : 0));
-          const int down = W == 128 ? 0 : 8 * (col / 16);
-          s.v[i][2 * u] = vw.x >> down, s.v[i][2 * u + 1] = vw.y >> down;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        s.kp[i] = *reinterpret_cast<const uint4*>(blk[i / 2] + 16 * W + 16 * (2 * (i % 2) + t));
-        s.vp[i] = *reinterpret_cast<const uint4*>(blk[i / 2] + 16 * W + 64 + 16 * (2 * (i % 2) + t));
-      }
-    }
-    s.mark = *reinterpret_cast<const uint32_t*>((lane & 16 ? blk[1] : blk[0]) + 16 * W + 64 + 4 * x);
+  const int64_t table = static_cast<int64_t>(b) * a.kv.max_pages;
+  const int my0 = key0 + kStep * wave;
+  auto pages_of = [&](int step) {
+    return a.kv.table[table + (min(my0 + kStep * KW * (step + lane / 2) + kKv4Block * (lane & 1), last) >> a.kv.page_shift)];
+  };
+  const uint8_t* const head = a.kv.pages + hk * a.kv.head_stride;
+  auto block = [&](int held, int step, int k) {
+    const int page = clamp_id(__builtin_amdgcn_readlane(held, 2 * (step & 31) + k), a.kv.n_pages);
+    const int j = min(my0 + kStep * KW * step + kKv4Block * k, last);
+    return head + page * a.kv.page_stride + (j & ((1 << a.kv.page_shift) - 1)) / kKv4Block * kv4_block_bytes(W);
+  };
+  typedef uint32_t Codes __attribute__((ext_vector_type(W / 32)));
+  // chunk `lane` of a block's keys or values: a wavefront reads them in one piece
+  auto codes = [&](const uint8_t* blk) { return *reinterpret_cast<const Codes*>(blk + lane * static_cast<int>(sizeof(Codes))); };
+  // the pair of key lane % 32 in the lower lanes, of value lane % 32 in the upper ones
+  auto mark_of = [&](const uint8_t* b0, const uint8_t* b1) {
+    return *reinterpret_cast<const uint32_t*>((lane & 16 ? b1 : b0) + 16 * W + (lane & 32 ? 64 : 0) + 4 * x);
   };
 
-  Acc o[NO];
-#pragma unroll
-  for (int d = 0; d < NO; ++d) o[d] = Acc{};
+  floatx4 o[RT][NO];
   // m: the subtracted logit (unscaled); mc = c m - lift, lift = kTop - unit; l: this lane's part of the
   // sum of the weights; add: its part of what joins every element of the output
-  float m = -INFINITY, mc = 0.f, l = 0.f, add = 0.f;
+  float m[RT], mc[RT], l[RT], add[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    m[r] = -INFINITY;
+    mc[r] = l[r] = add[r] = 0.f;
+#pragma unroll
+    for (int d = 0; d < NO; ++d) o[r][d] = floatx4{};
+  }
   int unit = kLeastUnit<F16>;
   bool wide = false;                               // a row's mc is past kFine (the same in all lanes)
+  float2* const my_marks = marks + 64 * wave;
+  const float middle = lane & 32 ? 8.f : 0.f;
 
-  auto attend = [&](const Raw& s, int j0) {
-    // ---- S^T = K Q^T over the codes
-    float z[NS];
-    if constexpr (M == 16) {
+  const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
+  if (steps > 0) {
+    int held = pages_of(0), held_next = pages_of(32);
+    const uint8_t *b0 = block(held, 0, 0), *b1 = block(held, 0, 1);
+    Codes k[2] = {codes(b0), codes(b1)}, v[2] = {codes(b0 + 8 * W), codes(b1 + 8 * W)};
+    uint32_t mark = mark_of(b0, b1);
+    for (int step = 0; step < steps; ++step) {
+      const int j0 = my0 + kStep * KW * step;
+      // ---- S^T = K Q^T over the codes: register u of block i is slot 16 i + 4 t + u
+      floatx4 z[RT][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        floatx4 r = start;
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int f = 0; f < NF; ++f) r = mfma16<F16>(key_codes<F16>(s.k[i][f]), q[f], r);
+        for (int f = 0; f < NF; ++f) {
+          const uint4 kf = key_codes<F16>(k[i][f]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) z[4 * i + u] = r[u];
-      }
-    } else {
-      floatx16 r = start;
+          for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, q[r][f], f == 0 ? start[r] : z[r][i]);
+        }
+      // ---- steps and lowest values: one slot a lane, handed round through LDS
+      {
+        float s = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
+        float size = fmaxf(s, fabsf(y) * 0.0625f);
+        y = fmaf(middle, s, y);
+        if (j0 + kStep > key1) {                   // what lies past the run may be anything
+          const bool in = j0 + (lane & 31) < key1;
+          s = in ? s : 0.f;
+          y = in ? y : 0.f;
+          size = in ? size : 0.f;
+        }
+        my_marks[lane] = make_float2(s, y);
+        size = lane & 32 && size < INFINITY ? size : 0.f;
+        if (__any(size > __builtin_ldexpf(1.f, F16 ? unit : unit + 60))) {
+          const int grown = max(unit, __builtin_amdgcn_frexp_expf(wave_allmax(size)) - (F16 ? 0 : 60));
+          const float f = __builtin_ldexpf(1.f, unit - grown);
 #pragma unroll
-      for (int f = 0; f < 2 * NF; ++f) r = mfma32<F16>(key_codes<F16>(s.k[f / NF][f % NF]), q[f], r);
+          for (int r = 0; r < RT; ++r) {
+            l[r] *= f;
+            add[r] *= f;
 #pragma unroll
-      for (int u = 0; u < NS; ++u) z[u] = r[u];
-    }
-    float step[NS], low[NS];                       // of the values
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const uint32_t kp = part_of(s.kp[i / 4], i % 4), vp = part_of(s.vp[i / 4], i % 4);
-      z[i] = fmaf(kv4_step<F16>(kp), z[i], kv4_low<F16>(kp) * qz);
-      step[i] = kv4_step<F16>(vp);
-      low[i] = fmaf(8.f, step[i], kv4_low<F16>(vp));
-    }
-    const bool cut = j0 + kStep > key1 || (masked && j0 + kStep > base);
-    if (cut) {
-#pragma unroll
-      for (int i = 0; i < NS; i += 4) {
-        const int first = j0 + (M == 16 ? 4 * i : 2 * i) + 4 * t;
-        const uint32_t seen = seen4(masked ? word : ~0ull, masked ? first - base : 0, key1 - first);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const bool see = (seen >> u) & 1;
-          z[i + u] = see ? z[i + u] : -INFINITY;
-          step[i + u] = see ? step[i + u] : 0.f;   // what is not seen may hold anything
-          low[i + u] = see ? low[i + u] : 0.f;
+            for (int d = 0; d < NO; ++d) o[r][d] *= f;
+            mc[r] = m[r] == -INFINITY ? 0.f : m[r] * c - static_cast<float>(kTop<F16> - grown);
+          }
+          unit = grown;
         }
       }
-    }
-    // ---- softmax statistics
-    float top = z[0];
+      asm volatile("" ::: "memory");               // LDS works in order for a wavefront; so must the compiler
+      __builtin_amdgcn_wave_barrier();
+      // ---- the next step's keys
+      if (((step + 1) & 31) == 0) {
+        held = held_next;
+        held_next = pages_of(step + 33);
+      }
+      b0 = block(held, step + 1, 0);
+      b1 = block(held, step + 1, 1);
+      k[0] = codes(b0);
+      k[1] = codes(b1);
+      mark = mark_of(b0, b1);
+      __builtin_amdgcn_sched_barrier(0);
+
+      float4 pairs[2][2];
 #pragma unroll
-    for (int i = 1; i < NS; ++i) top = fmaxf(top, z[i]);
-    if constexpr (M == 16) top = swap16_max(top);
-    top = swap32_max(top);
-    float size = fmaxf(kv4_step<F16>(s.mark), fabsf(kv4_low<F16>(s.mark)) * 0.0625f);
-    size = j0 + (lane & 31) < key1 && size < INFINITY ? size : 0.f;
-    // The subtracted logit follows the maximum only once that is kLag ahead.
-    if (__any((top - m) * c > kLag<F16> || size > __builtin_ldexpf(1.f, F16 ? unit : unit + 60))) {
-      const float largest = wave_allmax(size);
-      const int need = largest > 0.f ? __builtin_amdgcn_frexp_expf(largest) - (F16 ? 0 : 60) : kLeastUnit<F16>;
-      const int grown = max(unit, need);
-      const float up = fmaxf(m, top);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(m - up, c, static_cast<float>(unit - grown)));
-      l *= f;
-      add *= f;
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int d = 0; d < NO; ++d) o[d] *= f;
-      m = up;
-      unit = grown;
-      mc = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
-      wide = __any(fabsf(mc) > kFine);
-    }
-    float sub = mc;
-    if (wide) {
-      const float from = m == -INFINITY ? 0.f : m;
-      sub = static_cast<float>(unit - kTop<F16>);
+        for (int u = 0; u < 2; ++u) pairs[i][u] = *reinterpret_cast<const float4*>(my_marks + 16 * i + 4 * t + 2 * u);
 #pragma unroll
-      for (int i = 0; i < NS; ++i) z[i] -= from;
-    }
-    // ---- weights.  p s is rounded to the cache's type, as the products take it; the sums of p and
-    // p y are of unrounded numbers.
-    uint32_t w[NS / 2];
-    float sum = 0.f, lows = 0.f;
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int i = 0; i < NS; i += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(z[i], c, -sub)), p1 = __builtin_amdgcn_exp2f(fmaf(z[i + 1], c, -sub));
-      sum += p0 + p1;
-      lows = fmaf(p0, low[i], fmaf(p1, low[i + 1], lows));
-      w[i / 2] = pack2<F16>(p0 * step[i], p1 * step[i + 1]);
-      lows = less_middle<F16>(w[i / 2], lows);
-    }
-    l += sum;
-    add += lows;
-    // ---- out^T += D^T W^T over the codes
-    each_index<NO>([&](auto index) {
-      constexpr int d = index, j = M == 16 ? d % 4 : d;
-      if constexpr (M == 16) {
-        constexpr int y = 2 * (d / 4);
-        const uint4 f = make_uint4(value_codes<F16, j>(s.v[0][y]), value_codes<F16, j>(s.v[0][y + 1]),
-                                   value_codes<F16, j>(s.v[1][y]), value_codes<F16, j>(s.v[1][y + 1]));
-        o[d] = mfma16<F16>(f, make_uint4(w[0], w[1], w[2], w[3]), o[d]);
-      } else {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const uint4 f = make_uint4(value_codes<F16, j>(s.v[g][0]), value_codes<F16, j>(s.v[g][1]),
-                                     value_codes<F16, j>(s.v[g][2]), value_codes<F16, j>(s.v[g][3]));
-          o[d] = mfma32<F16>(f, make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]), o[d]);
+          for (int u = 0; u < 2; ++u) {
+            z[r][i][2 * u] = fmaf(pairs[i][u].x, z[r][i][2 * u], pairs[i][u].y * qz[r]);
+            z[r][i][2 * u + 1] = fmaf(pairs[i][u].z, z[r][i][2 * u + 1], pairs[i][u].w * qz[r]);
+          }
+      const bool cut = j0 + kStep > key1 || (masked && j0 + kStep > base);
+      uint32_t seen[RT];                           // bit 4 i + u: slot 16 i + 4 t + u
+      if (cut) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          seen[r] = 0;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int first = j0 + 16 * i + 4 * t;
+            seen[r] |= seen4(masked ? word[r] : ~0ull, masked ? first - base : 0, key1 - first) << (4 * i);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) z[r][i][u] = (seen[r] >> (4 * i + u)) & 1 ? z[r][i][u] : -INFINITY;
+          }
         }
       }
-    });
-  };
-
-  int j0 = key0 + wave * kStep;
-  if (j0 < key1) {
-    Raw cur;
-    load(j0, cur);
-    for (; j0 < key1; j0 += kStep * KW) {
-      Raw next;
-      load(j0 + kStep * KW, next);
-      attend(cur, j0);
-      cur = next;
+      // ---- softmax statistics.  The subtracted logit follows the maximum only once that is kLag ahead.
+      float top[RT];
+      bool behind = false;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        top[r] = z[r][0][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], z[r][i / 4][i % 4]);
+        behind |= (top[r] - m[r]) * c > kLag<F16>;
+      }
+      if (__any(behind)) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const float up = fmaxf(m[r], swap32_max(swap16_max(top[r])));
+          const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
+          l[r] *= f;
+          add[r] *= f;
+#pragma unroll
+          for (int d = 0; d < NO; ++d) o[r][d] *= f;
+          m[r] = up;
+          mc[r] = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
+        }
+        bool far = false;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) far |= fabsf(mc[r]) > kFine;
+        wide = __any(far);
+      }
+      float sub[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) sub[r] = mc[r];
+      if (wide) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const float from = m[r] == -INFINITY ? 0.f : m[r];
+          sub[r] = static_cast<float>(unit - kTop<F16>);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[r][i / 4][i % 4] -= from;
+        }
+      }
+      // ---- weights.  p s is rounded to the cache's type, as the products take it; the sums of p and
+      // p y are of unrounded numbers.
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) pairs[i][u] = *reinterpret_cast<const float4*>(my_marks + 32 + 16 * i + 4 * t + 2 * u);
+      uint32_t w[RT][4];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        float sum = 0.f, lows = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float4 s = pairs[i / 2][i % 2];
+          if (cut) {                               // what a row does not see may hold anything
+            const bool see0 = (seen[r] >> (2 * i)) & 1, see1 = (seen[r] >> (2 * i + 1)) & 1;
+            s = make_float4(see0 ? s.x : 0.f, see0 ? s.y : 0.f, see1 ? s.z : 0.f, see1 ? s.w : 0.f);
+          }
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2)], c, -sub[r]));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2) + 1], c, -sub[r]));
+          sum += p0 + p1;
+          lows = fmaf(p0, s.y, fmaf(p1, s.w, lows));
+          w[r][i] = pack2<F16>(p0 * s.x, p1 * s.z);
+          lows = less_middle<F16>(w[r][i], lows);
+        }
+        l[r] += sum;
+        add[r] += lows;
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      // ---- out^T += D^T W^T over the codes
+      each_index<NO>([&](auto index) {
+        constexpr int d = index, y = 2 * (d / 4), j = d % 4;
+        const uint4 f = make_uint4(value_codes<F16, j>(v[0][y]), value_codes<F16, j>(v[0][y + 1]),
+                                   value_codes<F16, j>(v[1][y]), value_codes<F16, j>(v[1][y + 1]));
+#pragma unroll
+        for (int r = 0; r < RT; ++r) o[r][d] = mfma16<F16>(f, make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]), o[r][d]);
+      });
+      v[0] = codes(b0 + 8 * W);
+      v[1] = codes(b1 + 8 * W);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  if constexpr (M == 16) {
-    l = swap16_sum(l);
-    add = swap16_sum(add);
-  }
-  l = swap32_sum(l);
-  add = swap32_sum(add);
 
   // ---- join the wavefronts and write
-  {
-    float* const to = acc + (wave * M + col) * kOutRow;
-    each_index<NO>([&](auto index) {
-      constexpr int d = index, j = M == 16 ? d % 4 : d;
-      constexpr float f = !F16 ? 1.f : j % 2 ? 0x1p20f : 0x1p24f;
 #pragma unroll
-      for (int r = 0; r < R; r += 4) {
-        const int e = M == 16 ? 16 * d + 4 * t : 8 * (r / 4 % 2) + 4 * t + 16 * (W / 32 * (r / 8) + d);
-        *reinterpret_cast<float4*>(to + e) = make_float4(fmaf(o[d][r], f, add), fmaf(o[d][r + 1], f, add),
-                                                         fmaf(o[d][r + 2], f, add), fmaf(o[d][r + 3], f, add));
-      }
+  for (int r = 0; r < RT; ++r) {
+    const int at = wave * M + 16 * r + x;
+    const float total = swap32_sum(swap16_sum(l[r])), all = swap32_sum(swap16_sum(add[r]));
+    each_index<NO>([&](auto index) {
+      constexpr int d = index;
+      constexpr float f = !F16 ? 1.f : d % 2 ? 0x1p20f : 0x1p24f;
+      *reinterpret_cast<float4*>(acc + at * kOutRow + 16 * d + 4 * t) =
+          make_float4(fmaf(o[r][d][0], f, all), fmaf(o[r][d][1], f, all), fmaf(o[r][d][2], f, all), fmaf(o[r][d][3], f, all));
     });
     if (t == 0) {
-      stat[(wave * M + col) * 2] = l == 0.f ? -INFINITY : mc;
-      stat[(wave * M + col) * 2 + 1] = l;
+      stat[at * 2] = total == 0.f ? -INFINITY : mc[r];
+      stat[at * 2 + 1] = total;
     }
   }
   __syncthreads();
@@ -442,10 +444,11 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const Kv4Plan& p, hipStream_t s) {
   const dim3 grid((p.groups + 7) / 8 * 8 * p.tiles);
-  if (shape_for(static_cast<int64_t>(a.L) * (a.H / a.Hkv)).rows == 16)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 16, 4>), grid, dim3(256), 0, s, a, p);
-  else
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 32, 4>), grid, dim3(256), 0, s, a, p);
+  switch (shape_for(static_cast<int64_t>(a.L) * (a.H / a.Hkv)).rows) {
+    case 16: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, dim3(256), 0, s, a, p); break;
+    case 32: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, dim3(256), 0, s, a, p); break;
+    default: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 4, 4>), grid, dim3(256), 0, s, a, p); break;
+  }
 }
 
 }  // namespace
