@@ -103,20 +103,26 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, 
   const bool valid = tok >= 0 && tok < count;
   if (!__any(valid)) return;
   const int64_t src = b * a.seq_stride + tok * a.row_stride + h * a.head_stride;
-  uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(j0));
 
   uint4 kw[NK];
-  uint2 vw[NV];
+  uint2 vw[NV];                                    // elements 16 i + 4 q + 0 .. 3
 #pragma unroll
   for (int i = 0; i < NK; ++i) {
     const int e = 32 * i + 8 * q;
     kw[i] = valid && e < a.D ? *reinterpret_cast<const uint4*>(a.k + src + e) : make_uint4(0, 0, 0, 0);
   }
+  // Of the values lanes of even q load 8 elements of an even i, lanes of odd q of the next i, and
+  // each gives its neighbour half.
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = 16 * i + 4 * q;
-    vw[i] = valid && e < a.D ? *reinterpret_cast<const uint2*>(a.v + src + e) : make_uint2(0, 0);
+  for (int i = 0; i < NV; i += 2) {
+    const int e = 16 * (i + (q & 1)) + 8 * (q >> 1);
+    const uint4 v = valid && e < a.D ? *reinterpret_cast<const uint4*>(a.v + src + e) : make_uint4(0, 0, 0, 0);
+    const auto x = __builtin_amdgcn_permlane16_swap(v.x, v.z, false, false);
+    const auto y = __builtin_amdgcn_permlane16_swap(v.y, v.w, false, false);
+    vw[i] = make_uint2(x[0], y[0]);
+    vw[i + 1] = make_uint2(x[1], y[1]);
   }
+  uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(j0));
 
   {  // ---- the key: elements 32 i + 8 q + 0 .. 7
     float x[NK][8], lo = INFINITY, hi = -INFINITY, poison = 0.f;
@@ -201,6 +207,11 @@ __device__ __forceinline__ uint32_t value_of(uint32_t code, float step, float lo
   return f32_to_half<F16>(fmaf(step, static_cast<float>(code), low));
 }
 
+__device__ __forceinline__ void stream_out(uint16_t* p, uint4 v) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u4, v), reinterpret_cast<u4*>(p));
+}
+
 template <bool F16, int W>
 __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, int blocks, int64_t items) {
   constexpr int NK = W / 32, NV = W / 16;
@@ -213,8 +224,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, in
   const int64_t j0 = (first >= 0 ? first / kKv4Block : (first - (kKv4Block - 1)) / kKv4Block) * kKv4Block + 16 * static_cast<int64_t>(nth);
   const int64_t tok = j0 + key - first;
   if (!__any(tok >= 0 && tok < a.T)) return;
-  const bool wanted = tok >= 0 && tok < a.T, held = wanted && j0 + key >= 0 && j0 + key < n;
-  const int64_t dst = ((b * static_cast<int64_t>(a.T) + tok) * a.Hkv + h) * a.D;
+  const bool held = j0 + key >= 0 && j0 + key < n;
   // slots that nobody holds read the place of one that the table addresses, and are not used
   const uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(min(max(j0, int64_t{0}), (static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift) - 16)));
 
@@ -233,6 +243,26 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, in
   const uint32_t kp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 4 * key);
   const uint32_t vp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 64 + 4 * key);
 
+  // Heads go out through LDS, row after row, so that a store instruction covers whole lines; a row's
+  // 16-byte pieces are permuted by its number.
+  constexpr int kPieces = W / 8, kRowsOut = 64 / kPieces;
+  __shared__ uint4 rows[kWaves][16 * kPieces];
+  uint4* const mine = rows[threadIdx.x >> 6];
+  auto put = [&](int e, uint4 v) { mine[key * kPieces + ((e / 8) ^ (key % kPieces))] = v; };
+  auto out = [&](uint16_t* to) {
+    asm volatile("" ::: "memory");                 // LDS works in order for a wavefront; so must the compiler
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int g = 0; g < 16 / kRowsOut; ++g) {
+      const int row = g * kRowsOut + lane / kPieces, piece = lane % kPieces;
+      const int64_t at = j0 + row - first;
+      const uint4 v = mine[row * kPieces + (piece ^ (row % kPieces))];
+      if (at >= 0 && at < a.T && 8 * piece < a.D)
+        stream_out(to + ((b * static_cast<int64_t>(a.T) + at) * a.Hkv + h) * a.D + 8 * piece, v);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  };
   {
     const float s = kv4_step<F16>(kp), z = kv4_low<F16>(kp);
 #pragma unroll
@@ -242,9 +272,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, in
 #pragma unroll
       for (int p = 0; p < 4; ++p)
         o[p] = held ? value_of<F16>((w >> (4 * p)) & 15, s, z) | value_of<F16>((w >> (4 * p + 16)) & 15, s, z) << 16 : 0;
-      const int e = 32 * i + 8 * q;
-      if (wanted && e < a.D) *reinterpret_cast<uint4*>(a.k + dst + e) = make_uint4(o[0], o[1], o[2], o[3]);
+      put(32 * i + 8 * q, make_uint4(o[0], o[1], o[2], o[3]));
     }
+    out(a.k);
   }
   {
     // of x = 4 q + u, slots 4 t + 0 .. 3: to this lane's slot, x = 4 q + 0 .. 3
@@ -252,15 +282,21 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, in
                      (vc.y & 0xFFFF) | vc.w << 16, vc.y >> 16 | (vc.w & 0xFFFF0000u)};
     quad_transpose(w, lane);
     const float s = kv4_step<F16>(vp), z = kv4_low<F16>(vp);
+    // Elements 16 i + 4 q + 0 .. 3 of two i at a time: lanes of even q take the first i's of their own and
+    // of the next quarter's, lanes of odd q the second i's, so that a piece is of 16 bytes.
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      uint32_t o[2];
+    for (int i = 0; i < NV; i += 2) {
+      uint32_t o[2][2];
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-        o[p] = held ? value_of<F16>((w[2 * p] >> (4 * i)) & 15, s, z) | value_of<F16>((w[2 * p + 1] >> (4 * i)) & 15, s, z) << 16 : 0;
-      const int e = 16 * i + 4 * q;
-      if (wanted && e < a.D) *reinterpret_cast<uint2*>(a.v + dst + e) = make_uint2(o[0], o[1]);
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          o[n][p] = held ? value_of<F16>((w[2 * p] >> (4 * (i + n))) & 15, s, z) | value_of<F16>((w[2 * p + 1] >> (4 * (i + n))) & 15, s, z) << 16 : 0;
+      const auto x = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
+      const auto y = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
+      put(16 * (i + (q & 1)) + 8 * (q >> 1), make_uint4(x[0], y[0], x[1], y[1]));
     }
+    out(a.v);
   }
 }
 
