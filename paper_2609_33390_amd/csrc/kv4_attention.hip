@@ -105,10 +105,6 @@ __device__ __forceinline__ uint32_t seen4(uint64_t word, int at, int left) {
   return static_cast<uint32_t>(bits) & (left >= 4 ? 15u : left <= 0 ? 0u : (1u << left) - 1);
 }
 
-__device__ __forceinline__ float swap16_max(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 __device__ __forceinline__ uint32_t part_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // RT tiles of 16 rows a workgroup, KW wavefronts.

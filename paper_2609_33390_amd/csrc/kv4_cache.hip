@@ -36,11 +36,18 @@ __device__ __forceinline__ void quad_transpose(uint32_t (&w)[4], int lane) {
 }
 
 // Over the four lanes that share a slot.
-__device__ __forceinline__ float quarters_max(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+__device__ __forceinline__ float quarters_max(float v) { return swap32_max(swap16_max(v)); }
+
+// acc, or NaN where a number of the pair is not finite.
+template <bool F16>
+__device__ __forceinline__ float poisoned(uint32_t pair, float acc) {
+  if constexpr (F16) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, pair), h2{0, 0}, acc, false);
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, pair), __builtin_bit_cast(b2, 0u), acc, false);
+  }
 }
 
 // How a head is held.  The quotient t / s is taken as t (1 / s) with the reciprocal in two parts,
@@ -70,10 +77,12 @@ __device__ __forceinline__ Scheme scheme_of(float lowest, float highest, float p
   return h;
 }
 
-// The code as a float.  0 for every element of a head without a step (NaN compares false).
+// The code as a float (what a head without a step gives is not used).  A normal step is within 2^-8 of
+// a fifteenth of the range, so only a subnormal one, which f16 may have, can give more than 15.
+template <bool F16>
 __device__ __forceinline__ float code_of(float x, const Scheme& h) {
   const float t = x - h.low, y = fmaf(t, h.inv, t * h.inv_rest);
-  return __builtin_rintf(fminf(y, 15.f));
+  return __builtin_rintf(F16 ? fminf(y, 15.f) : y);
 }
 
 template <bool F16>
@@ -82,6 +91,9 @@ __device__ __forceinline__ void widen(uint32_t w, float& lo, float& hi) {
   hi = F16 ? half_to_f32<F16>(w >> 16) : __uint_as_float(w & 0xFFFF0000u);
 }
 
+// First slot of the block that slot j lies in, also below 0.
+__device__ __forceinline__ int64_t block_begin(int64_t j) { return j & ~static_cast<int64_t>(kKv4Block - 1); }
+
 // Place in a block of the word of a key's elements e .. e + 7.
 template <int W>
 __device__ __forceinline__ int key_word(int key, int e) {
@@ -89,63 +101,61 @@ __device__ __forceinline__ int key_word(int key, int e) {
 }
 
 template <bool F16, int W>
-__global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, int blocks, int64_t items) {
+__global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, int blocks, int items) {
   constexpr int NK = W / 32, NV = W / 16;
   const int lane = threadIdx.x & 63, q = lane >> 4, key = lane & 15;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= items) return;
   const int h = item % a.Hkv, b = item / a.Hkv / blocks, nth = item / a.Hkv % blocks;
   const int64_t first = a.first[b], count = a.count ? min(max(a.count[b], 0), a.T) : a.T;
   const int64_t cap = static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift;
-  const int64_t j0 = (first >= 0 ? first / kKv4Block : (first - (kKv4Block - 1)) / kKv4Block) * kKv4Block + 16 * static_cast<int64_t>(nth);
-  if (j0 < 0 || j0 >= cap || j0 >= first + count) return;
-  const int64_t tok = j0 + key - first;            // this lane's token
+  const int64_t j0 = block_begin(first) + 16 * static_cast<int64_t>(nth);
+  if (j0 < 0 || j0 >= cap || j0 >= first + count || j0 + 16 <= first) return;
+  // A lane whose slot gets no token, and one that holds no elements (D < W), works on others' and stores nothing.
+  const int64_t tok = j0 + key - first;
   const bool valid = tok >= 0 && tok < count;
-  if (!__any(valid)) return;
-  const int64_t src = b * a.seq_stride + tok * a.row_stride + h * a.head_stride;
+  const int64_t src = b * a.seq_stride + min(max(tok, int64_t{0}), count - 1) * a.row_stride + h * a.head_stride;
 
-  uint4 kw[NK];
-  uint2 vw[NV];                                    // elements 16 i + 4 q + 0 .. 3
+  uint4 kw[NK], vw[NV / 2];                        // elements 32 i + 8 q + 0 .. 7
 #pragma unroll
-  for (int i = 0; i < NK; ++i) {
-    const int e = 32 * i + 8 * q;
-    kw[i] = valid && e < a.D ? *reinterpret_cast<const uint4*>(a.k + src + e) : make_uint4(0, 0, 0, 0);
-  }
-  // Of the values lanes of even q load 8 elements of an even i, lanes of odd q of the next i, and
-  // each gives its neighbour half.
+  for (int i = 0; i < NK; ++i) kw[i] = *reinterpret_cast<const uint4*>(a.k + src + min(32 * i + 8 * q, a.D - 8));
+  // Of the values lanes of even q load 8 elements of an even 16, lanes of odd q of the next 16: each
+  // will give its neighbour half.
 #pragma unroll
-  for (int i = 0; i < NV; i += 2) {
-    const int e = 16 * (i + (q & 1)) + 8 * (q >> 1);
-    const uint4 v = valid && e < a.D ? *reinterpret_cast<const uint4*>(a.v + src + e) : make_uint4(0, 0, 0, 0);
-    const auto x = __builtin_amdgcn_permlane16_swap(v.x, v.z, false, false);
-    const auto y = __builtin_amdgcn_permlane16_swap(v.y, v.w, false, false);
-    vw[i] = make_uint2(x[0], y[0]);
-    vw[i + 1] = make_uint2(x[1], y[1]);
-  }
+  for (int i = 0; i < NV; i += 2)
+    vw[i / 2] = *reinterpret_cast<const uint4*>(a.v + src + min(16 * (i + (q & 1)) + 8 * (q >> 1), a.D - 8));
   uint8_t* const blk = kv4_block<W>(a.kv, b, h, static_cast<int>(j0));
 
-  {  // ---- the key: elements 32 i + 8 q + 0 .. 7
-    float x[NK][8], lo = INFINITY, hi = -INFINITY, poison = 0.f;
+  auto scheme = [&](auto& words) {
+    float lo = INFINITY, hi = -INFINITY, poison = 0.f;
+    for (const uint4& v : words) {
+      const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x0, x1;
+        widen<F16>(w4[i], x0, x1);
+        lo = fminf(fminf(x0, x1), lo);
+        hi = fmaxf(fmaxf(x0, x1), hi);
+        poison = poisoned<F16>(w4[i], poison);
+      }
+    }
+    return scheme_of<F16>(-quarters_max(-lo), quarters_max(hi), swap32_sum(swap16_sum(poison)));
+  };
+
+  {  // ---- the key
+    const Scheme s = scheme(kw);
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const uint32_t w4[4] = {kw[i].x, kw[i].y, kw[i].z, kw[i].w};
-      const bool in = 32 * i + 8 * q < a.D;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        widen<F16>(w4[e / 2], x[i][e], x[i][e + 1]);
-        lo = fminf(lo, in ? fminf(x[i][e], x[i][e + 1]) : INFINITY);
-        hi = fmaxf(hi, in ? fmaxf(x[i][e], x[i][e + 1]) : -INFINITY);
-        poison = fmaf(x[i][e], 0.f, fmaf(x[i][e + 1], 0.f, poison));
-      }
-    }
-    poison = swap32_sum(swap16_sum(poison));
-    const Scheme s = scheme_of<F16>(-quarters_max(-lo), quarters_max(hi), poison);
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
       // element e is nibble e / 2 of half e % 2
       float half[2] = {0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) half[e % 2] = fmaf(code_of(x[i][e], s), static_cast<float>(1 << (4 * (e / 2))), half[e % 2]);
+      for (int e = 0; e < 8; e += 2) {
+        float x0, x1;
+        widen<F16>(w4[e / 2], x0, x1);
+        half[0] = fmaf(code_of<F16>(x0, s), static_cast<float>(1 << (2 * e)), half[0]);
+        half[1] = fmaf(code_of<F16>(x1, s), static_cast<float>(1 << (2 * e)), half[1]);
+      }
       uint32_t w = static_cast<uint32_t>(half[0]) | static_cast<uint32_t>(half[1]) << 16;
       if (32 * i + 8 * q >= a.D || (s.pair & 0xFFFF) == 0) w = 0;
       if (valid) *reinterpret_cast<uint32_t*>(blk + key_word<W>(key, 32 * i + 8 * q)) = w << 3 | w >> 29;
@@ -154,32 +164,29 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, 
   }
 
   {  // ---- the value: elements x + 16 (4 y + j) for x = 4 q + 0 .. 3
-    float lo = INFINITY, hi = -INFINITY, poison = 0.f, x[NV][4];
+    const Scheme s = scheme(vw);
+    float half[4][2] = {};                         // for each x the codes of y = 0 and of y = 1
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const bool in = 16 * i + 4 * q < a.D;
-      widen<F16>(vw[i].x, x[i][0], x[i][1]);
-      widen<F16>(vw[i].y, x[i][2], x[i][3]);
+    for (int i = 0; i < NV; i += 2) {
+      const uint4 v = vw[i / 2];
+      const auto lo = __builtin_amdgcn_permlane16_swap(v.x, v.z, false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(v.y, v.w, false, false);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lo = fminf(lo, in ? x[i][e] : INFINITY);
-        hi = fmaxf(hi, in ? x[i][e] : -INFINITY);
-        poison = fmaf(x[i][e], 0.f, poison);
+      for (int n = 0; n < 2; ++n) {                // elements 16 (i + n) + 4 q + 0 .. 3
+        float x[4];
+        widen<F16>(lo[n], x[0], x[1]);
+        widen<F16>(hi[n], x[2], x[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          half[e][i / 4] = fmaf(code_of<F16>(x[e], s), static_cast<float>(1 << (4 * ((i + n) % 4))), half[e][i / 4]);
       }
     }
-    poison = swap32_sum(swap16_sum(poison));
-    const Scheme s = scheme_of<F16>(-quarters_max(-lo), quarters_max(hi), poison);
-    uint32_t w[4];                                 // for each x the 16 bits of y = 0 and, above them, of y = 1
+    // the 16 bits of y = 0 and, above them, of y = 1; elements past D are code 0
+    const int own = min(max((a.D - 4 * q + 15) / 16, 0), 8);
+    const uint32_t keep = (s.pair & 0xFFFF) == 0 ? 0u : own == 8 ? ~0u : (1u << (4 * own)) - 1;
+    uint32_t w[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float half[2] = {0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const float c = 16 * i + 4 * q < a.D ? code_of(x[i][e], s) : 0.f;
-        half[i / 4] = fmaf(c, static_cast<float>(1 << (4 * (i % 4))), half[i / 4]);
-      }
-      w[e] = (s.pair & 0xFFFF) == 0 ? 0 : static_cast<uint32_t>(half[0]) | static_cast<uint32_t>(half[1]) << 16;
-    }
+    for (int e = 0; e < 4; ++e) w[e] = (static_cast<uint32_t>(half[e][0]) | static_cast<uint32_t>(half[e][1]) << 16) & keep;
     uint8_t* const val = blk + 8 * W;
     const int t = key >> 2, u = key & 3;
     if (__all(valid)) {
@@ -213,15 +220,15 @@ __device__ __forceinline__ void stream_out(uint16_t* p, uint4 v) {
 }
 
 template <bool F16, int W>
-__global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, int blocks, int64_t items) {
+__global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, int blocks, int items) {
   constexpr int NK = W / 32, NV = W / 16;
   const int lane = threadIdx.x & 63, q = lane >> 4, key = lane & 15;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (item >= items) return;
   const int h = item % a.Hkv, b = item / a.Hkv / blocks, nth = item / a.Hkv % blocks;
   const int64_t first = a.first ? a.first[b] : 0;
   const int n = kv4_len(a.kv, b, static_cast<int>(static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift));
-  const int64_t j0 = (first >= 0 ? first / kKv4Block : (first - (kKv4Block - 1)) / kKv4Block) * kKv4Block + 16 * static_cast<int64_t>(nth);
+  const int64_t j0 = block_begin(first) + 16 * static_cast<int64_t>(nth);
   const int64_t tok = j0 + key - first;
   if (!__any(tok >= 0 && tok < a.T)) return;
   const bool held = j0 + key >= 0 && j0 + key < n;
@@ -310,8 +317,8 @@ bool kv4_launchable(int B, int Hkv, int T) { return static_cast<int64_t>(B) * Hk
 template <class Args, class Fn>
 static void launch_blocks(const Args& a, Fn kernel, hipStream_t s) {
   const int blocks = blocks_of(a.T);
-  const int64_t items = static_cast<int64_t>(a.B) * a.Hkv * blocks;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((items + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, s, a, blocks, items);
+  const int items = a.B * a.Hkv * blocks;          // kv4_launchable: below 2^25
+  hipLaunchKernelGGL(kernel, dim3((items + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, s, a, blocks, items);
 }
 
 void launch_kv4_write(const Kv4WriteArgs& a, bool f16, hipStream_t s) {
