@@ -831,11 +831,14 @@ class KVCache:
 
 def _steps(t: torch.Tensor) -> Tuple[int, ...]:
     """Strides, where a dimension of one element, whose stride nothing uses, has 0."""
-    return tuple(0 if n == 1 else s for n, s in zip(t.shape, t.stride()))
+    return tuple([0 if n == 1 else s for n, s in zip(t.shape, t.stride())])
 
 
 def _half_tensor(t: torch.Tensor, name: str, ndim: int, like: Optional[KVCache] = None) -> None:
     """A 2-byte tensor on a HIP device whose last dimension is contiguous."""
+    if (like is not None and type(t) is torch.Tensor and t.dtype is like.dtype and t.is_cuda and t.dim() == ndim
+            and t.device == like.device and t.stride(-1) == 1):
+        return                                     # nothing to object to: most calls end here
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype not in _HALF if like is None else t.dtype != like.dtype:
@@ -1138,7 +1141,7 @@ class KVCache4:
 
 
 def _cache4(cache) -> None:
-    if not isinstance(cache, KVCache4):
+    if type(cache) is not KVCache4 and not isinstance(cache, KVCache4):
         raise TypeError(f"cache must be a KVCache4, got {type(cache).__name__}")
 
 
@@ -1156,13 +1159,14 @@ def kv4_write(k: torch.Tensor, v: torch.Tensor, cache: KVCache4, first: torch.Te
     if B != cache.B or Hkv != cache.n_kv_heads or D != cache.d_head:
         raise ValueError(f"k is {tuple(k.shape)}, the cache holds {cache.B} sequences of {cache.n_kv_heads} heads of "
                          f"{cache.d_head}")
-    if v.shape != k.shape or _steps(v) != _steps(k):
+    if v.shape != k.shape or (v.stride() != k.stride() and _steps(v) != _steps(k)):
         raise ValueError("k and v must agree in shape and strides")
+    seq, row, head, _ = _steps(k) if B == 1 or T == 1 or Hkv == 1 else k.stride()
     dev = cache.device
     _dev_tensor(first, "first", torch.int32, shape=(B,), device=dev)
     if count is not None:
         _dev_tensor(count, "count", torch.int32, shape=(B,), device=dev)
-    st = lib().brisk_kv4_write(cache._ref, _ptr(k), _ptr(v), *_steps(k)[:3], B, T, _ptr(first), _ptr(count),
+    st = lib().brisk_kv4_write(cache._ref, k.data_ptr(), v.data_ptr(), seq, row, head, B, T, first.data_ptr(), _ptr(count),
                                _stream_ptr(dev, stream))
     _check(st, "brisk_kv4_write")
 
@@ -1173,19 +1177,20 @@ def kv4_read(cache: KVCache4, T: int, *, first: Optional[torch.Tensor] = None, k
     ``first[b]`` (0 without it) to ``first[b]`` + T - 1; zeros for slots that a
     sequence does not hold."""
     _cache4(cache)
-    dev, shape = cache.device, (cache.B, T, cache.n_kv_heads, cache.d_head)
+    dev, dtype, shape = cache.device, cache.dtype, (cache.B, T, cache.n_kv_heads, cache.d_head)
     if first is not None:
         _dev_tensor(first, "first", torch.int32, shape=(cache.B,), device=dev)
-    out = []
-    for t, n in ((k, "k"), (v, "v")):
-        if t is None:
-            t = torch.empty(shape, dtype=cache.dtype, device=dev)
-        else:
-            _dev_tensor(t, n, cache.dtype, shape=shape, device=dev)
-        out.append(t)
-    st = lib().brisk_kv4_read(cache._ref, cache.B, T, _ptr(first), _ptr(out[0]), _ptr(out[1]), _stream_ptr(dev, stream))
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        _dev_tensor(k, "k", dtype, shape=shape, device=dev)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        _dev_tensor(v, "v", dtype, shape=shape, device=dev)
+    st = lib().brisk_kv4_read(cache._ref, cache.B, T, _ptr(first), k.data_ptr(), v.data_ptr(), _stream_ptr(dev, stream))
     _check(st, "brisk_kv4_read")
-    return out[0], out[1]
+    return k, v
 
 
 def kv4_attention(q: torch.Tensor, cache: KVCache4, *, prefix: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,

@@ -16,6 +16,7 @@
 // steps in turn and join through LDS.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "attention_plan.h"
 #include "kernels.h"
@@ -99,6 +100,8 @@ __device__ __forceinline__ uint32_t value_codes(uint32_t w, const CodeBits& k) {
   return ((w >> (4 * J)) & k.value) | k.value_base;
 }
 
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
+
 // Which of four slots a row sees, the first one `at` slots past the block's begin and `left` before the end.
 __device__ __forceinline__ uint32_t seen4(uint64_t word, int at, int left) {
   const uint64_t bits = at >= 64 ? 0 : at >= 0 ? word >> at : at > -4 ? (word << -at) | ((1ull << -at) - 1) : ~0ull;
@@ -107,25 +110,15 @@ __device__ __forceinline__ uint32_t seen4(uint64_t word, int at, int left) {
 
 __device__ __forceinline__ uint32_t part_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// RT tiles of 16 rows a workgroup, KW wavefronts.
-template <bool F16, int W, int RT, int KW>
-__global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
-  constexpr int M = 16 * RT, NF = W / 32, NO = W / 16, kStep = 32;
-  constexpr int kAhead = 1;                        // steps on their way
-  constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides those ahead
-  constexpr int kOutRow = W + 4;
-  __shared__ __attribute__((aligned(16))) float acc[KW * M * kOutRow];
-  __shared__ float stat[KW * M * 2];
-  __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys and values
-
-  const int tid = threadIdx.x, lane = tid & 63, t = lane >> 4, x = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = a.H / a.Hkv;
-  const int bid = blockIdx.x, group = bid / 8 / p.tiles * 8 + bid % 8, tile = bid / 8 % p.tiles;
-  if (group >= p.groups) return;
-  // first runs of all sequences, then second ones, ...: later runs are fewer where lengths differ
-  const int hk = group % a.Hkv;
-  int b = group / a.Hkv % a.B, split = group / a.Hkv / a.B;
+// Which rows and slots a workgroup has: row tiles of a group follow each other on one XCD; first runs of
+// all sequences go first, then second ones, ...: later runs are fewer where lengths differ.
+struct Place {
+  int hk, b, split, tile;
+};
+__device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Plan& p, int lane, Place& w) {
+  const int bid = blockIdx.x, group = bid / 8 / p.tiles * 8 + bid % 8;
+  if (group >= p.groups) return false;
+  w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, bid / 8 % p.tiles};
   if (p.by_length) {                               // the b-th longest sequence, of at most 64
     const int len = lane < a.B ? kv4_len(a.kv, lane, a.max_seq_len) : -1;
     int before = 0;
@@ -133,82 +126,280 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : 2) void kv4_attend_kernel(Kv
       const int other = __builtin_amdgcn_readlane(len, i);
       before += other > len || (other == len && i < lane);
     }
-    b = __builtin_ctzll(__ballot(before == b));
+    w.b = __builtin_ctzll(__ballot(before == w.b));
   }
-  const int n = kv4_len(a.kv, b, a.max_seq_len);
-  const int key0 = split * p.run, key1 = min(n, key0 + p.run), base = n - a.L;
-  const int row0 = b * a.L * G + tile * M, rows = min(M, a.L * G - tile * M);
-  split += p.own_first;
-  if (key0 >= n && p.part) {                       // a run past the sequence: the join reads that it is empty
-    for (int r = tid; r < rows; r += 64 * KW) {
-      const int row = row0 + r;
-      p.part_lse[(static_cast<int64_t>(row / G) * a.H + hk * G + row % G) * p.splits + split] = -INFINITY;
-    }
-    return;
-  }
-  const bool masked = a.mask != nullptr;
+  return true;
+}
 
-  // ---- queries, as the second operand of K Q^T: row x of each tile, elements t W / 4 + ...
-  uint4 q[RT][NF];
-  // f16 logits are held 2^-21 of what they are
-  const float c = a.scale * kLog2e * (F16 ? 0x1p21f : 1.f);
+// A run past the sequence: the join reads that it is empty.
+__device__ __forceinline__ void leave_empty(const Kv4AttentionArgs& a, const Kv4Plan& p, const Place& w, int row0, int rows) {
+  const int G = a.H / a.Hkv;
+  for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+    const int row = row0 + r;
+    p.part_lse[(static_cast<int64_t>(row / G) * a.H + w.hk * G + row % G) * p.splits + p.own_first + w.split] = -INFINITY;
+  }
+}
+
+// A wavefront's 16 RT rows: row x = lane % 16 of each tile, of which quarter t = lane / 16 has the logits
+// and the elements 4 t .. 4 t + 3 of every 16.
+// `LEAN`: for wavefronts whose registers are few, values are read where they are used.
+template <bool F16, int W, int RT, bool LEAN>
+struct Rows {
+  static constexpr int NF = W / 32, NO = W / 16;
+  uint4 q[RT][NF];                                 // elements t W / 4 + ..., the second operand of K Q^T
   float qz[RT];                                    // sum of q, as the logits are held
-  // what a row sees of the block; one tile, short of registers, reads it where it is used
-  uint64_t word[RT];
+  uint64_t word[RT];                               // what a row sees of the block (one tile reads it where it is used)
+  floatx4 o[RT][NO];
+  // m: the subtracted logit (unscaled); mc = c m - lift, lift = kTop - unit; l: this lane's part of the
+  // sum of the weights; add: its part of what joins every element of the output
+  float m[RT], mc[RT], l[RT], add[RT];
+  int unit;
+  float limit;                                     // of a value's size within that unit
+  bool wide;                                       // a row's mc is past kFine (the same in all lanes)
+  float c;                                         // f16 logits are held 2^-21 of what they are
+  int key1, base, row0, rows;                      // end of the run, begin of the block, the wavefront's rows
+  const uint64_t* mask;
+
+  __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x, rows - 1)) / G]; }
+
+  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int n, int end, int lane) {
+    const int t = lane >> 4, x = lane & 15, G = a.H / a.Hkv;
+    row0 = first_row;
+    rows = n_rows;
+    key1 = end;
+    base = n - a.L;
+    mask = a.mask;
+    c = uniform(a.scale * kLog2e * (F16 ? 0x1p21f : 1.f));
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = row0 + min(16 * r + x, rows - 1), bi = row / G;
-    const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
-    word[r] = RT > 1 && masked ? a.mask[bi] : ~0ull;
-    float sum = 0.f;
+    for (int r = 0; r < RT; ++r) {
+      const int row = row0 + min(16 * r + x, rows - 1), bi = row / G;
+      const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
+      word[r] = !LEAN && mask ? mask[bi] : ~0ull;
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NF; ++i) {
-      const int e = t * (W / 4) + 8 * i;
-      q[r][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < NF; ++i) {
+        const int e = t * (W / 4) + 8 * i;
+        q[r][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        sum += half_to_f32<F16>(part_of(q[r][i], w) & 0xFFFF) + half_to_f32<F16>(part_of(q[r][i], w) >> 16);
+        for (int w = 0; w < 4; ++w)
+          sum += half_to_f32<F16>(part_of(q[r][i], w) & 0xFFFF) + half_to_f32<F16>(part_of(q[r][i], w) >> 16);
+      }
+      sum = swap32_sum(swap16_sum(sum));
+      qz[r] = F16 ? sum * 0x1p-21f : sum;
+      m[r] = -INFINITY;
+      mc[r] = l[r] = add[r] = 0.f;
+#pragma unroll
+      for (int d = 0; d < NO; ++d) o[r][d] = floatx4{};
     }
-    sum = swap32_sum(swap16_sum(sum));
-    qz[r] = F16 ? sum * 0x1p-21f : sum;
+    wide = false;
+    set_unit(kLeastUnit<F16>);
   }
 
-  // ---- loads.  Step i of this wavefront begins at slot key0 + 32 (KW i + wave).  Pages are looked up for kLooked
-  // steps and those ahead of them at once, block k of the i-th by lane 2 i + k, while the steps before are worked on.
-  const int last = max(key1 - 1, 0) & ~(kKv4Block - 1);
-  const int64_t table = static_cast<int64_t>(b) * a.kv.max_pages;
-  const int my0 = key0 + kStep * wave;
+  __device__ __forceinline__ void set_unit(int to) {
+    unit = to;
+    limit = __builtin_ldexpf(1.f, F16 ? unit : unit + 60);
+  }
+
+  // Grows the unit to what values of the upper lanes' sizes need.
+  __device__ __forceinline__ void fit(float size, int lane) {
+    if (static_cast<uint32_t>(__ballot(size > limit) >> 32) == 0) return;
+    const float finite = lane & 32 && size < INFINITY ? size : 0.f;
+    const int grown = max(unit, __builtin_amdgcn_frexp_expf(wave_allmax(finite)) - (F16 ? 0 : 60));
+    const float f = __builtin_ldexpf(1.f, unit - grown);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      l[r] *= f;
+      add[r] *= f;
+#pragma unroll
+      for (int d = 0; d < NO; ++d) o[r][d] *= f;
+      mc[r] = m[r] == -INFINITY ? 0.f : m[r] * c - static_cast<float>(kTop<F16> - grown);
+    }
+    set_unit(grown);
+  }
+
+  // Whether some row does not see some of the slots j0 .. j0 + 31 (the same in all lanes).
+  __device__ __forceinline__ bool cut(int j0) const { return j0 + 32 > key1 || (mask && j0 + 32 > base); }
+
+  // From products with the codes of the keys at slots j0 .. j0 + 31 (register u of block i is slot 16 i + 4 t + u)
+  // to weights, times the values' steps, as the second operand of D^T W^T.  `keys` and `values`: the slots'
+  // steps and lowest values, in LDS.  Where cut(j0), those of values that are not finite are 0 there, since a
+  // weight of 0 does not take them out, and `odd` says which: they count for the rows that see them.
+  __device__ __forceinline__ void weigh(floatx4 (&z)[RT][2], const float2* keys, const float2* values, uint32_t odd, int j0, int lane,
+                                        int G, uint32_t (&w)[RT][4]) {
+    const int t = lane >> 4, x = lane & 15;
+    // slots 16 i + 4 t + 2 u and the next one
+    auto pairs = [&](const float2* of, int i, int u) { return *reinterpret_cast<const float4*>(of + 16 * i + 4 * t + 2 * u); };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float4 p = pairs(keys, i, u);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          z[r][i][2 * u] = fmaf(p.x, z[r][i][2 * u], p.y * qz[r]);
+          z[r][i][2 * u + 1] = fmaf(p.z, z[r][i][2 * u + 1], p.w * qz[r]);
+        }
+      }
+    }
+    if (cut(j0)) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        if (LEAN && mask) word[r] = sees(r, x, G);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int first = j0 + 16 * i + 4 * t;
+          const uint32_t seen = seen4(word[r], mask ? first - base : 0, key1 - first);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) z[r][i][u] = (seen >> u) & 1 ? z[r][i][u] : -INFINITY;
+          if (seen & odd >> (16 * i + 4 * t)) add[r] = NAN;
+        }
+      }
+    }
+    // The subtracted logit follows the maximum only once that is kLag ahead.
+    float top[RT];
+    bool behind = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      top[r] = z[r][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], z[r][i / 4][i % 4]);
+      behind |= (top[r] - m[r]) * c > kLag<F16>;
+    }
+    if (__any(behind)) {
+      bool far = false;
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float up = fmaxf(m[r], swap32_max(swap16_max(top[r])));
+        const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
+        l[r] *= f;
+        add[r] *= f;
+#pragma unroll
+        for (int d = 0; d < NO; ++d) o[r][d] *= f;
+        m[r] = up;
+        mc[r] = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
+        far |= fabsf(mc[r]) > kFine;
+      }
+      wide = __any(far);
+    }
+    float sub[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sub[r] = mc[r];
+    // c z - mc is off by the rounding of mc, by the same for all of a row, which cancels in the quotient;
+    // but past kFine that may be more than the exponent range.
+    if (wide) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float from = m[r] == -INFINITY ? 0.f : m[r];
+        sub[r] = static_cast<float>(unit - kTop<F16>);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[r][i / 4][i % 4] -= from;
+      }
+    }
+    // p s is rounded to the cache's type, as the products take it: relative to sum p s |d - 8|, as large an
+    // error as that of rounding the output.  The sums of p and p y are of unrounded numbers.
+    float sum[RT], lows[RT];                       // a step's, so that many small ones beside a large one count together
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 y = pairs(values, i / 2, i % 2);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2)], c, -sub[r]));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2) + 1], c, -sub[r]));
+        sum[r] = i == 0 ? p0 + p1 : sum[r] + (p0 + p1);
+        lows[r] = fmaf(p0, y.y, i == 0 ? p1 * y.w : fmaf(p1, y.w, lows[r]));
+        w[r][i] = pack2<F16>(p0 * y.x, p1 * y.z);
+        lows[r] = less_middle<F16>(w[r][i], lows[r]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      l[r] += sum[r];
+      add[r] += lows[r];
+    }
+  }
+
+  // Sums of the rows over the wavefront; then element 16 d + 4 t + u of the (unnormalised) output is element(r, d, u).
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      l[r] = swap32_sum(swap16_sum(l[r]));
+      add[r] = swap32_sum(swap16_sum(add[r]));
+    }
+  }
+  template <int d>
+  __device__ __forceinline__ float4 elements(int r) const {
+    constexpr float f = !F16 ? 1.f : d % 2 ? 0x1p20f : 0x1p24f;
+    return make_float4(fmaf(o[r][d][0], f, add[r]), fmaf(o[r][d][1], f, add[r]), fmaf(o[r][d][2], f, add[r]), fmaf(o[r][d][3], f, add[r]));
+  }
+};
+
+// Elements e .. e + 3 of a row's normalised sum, and its log-sum-exp, to where the plan has them.
+template <bool F16>
+__device__ __forceinline__ void put(const Kv4AttentionArgs& a, const Kv4Plan& p, int64_t out, int split, int e, float4 v) {
+  if (p.part)
+    *reinterpret_cast<float4*>(p.part + (out * p.splits + split) * a.D + e) = v;
+  else
+    *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
+}
+__device__ __forceinline__ void put_lse(const Kv4AttentionArgs& a, const Kv4Plan& p, int64_t out, int split, float mc, float total) {
+  const float lse = total == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(total)) * kLn2;
+  if (p.part)
+    p.part_lse[out * p.splits + split] = lse;
+  else if (a.lse)
+    a.lse[out] = lse;
+}
+
+// Few rows: RT tiles of 16 a workgroup, KW wavefronts that take steps of 32 slots in turn, each from
+// registers that its loads filled in operand order.
+template <bool F16, int W, int RT, int KW>
+__global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
+  using R = Rows<F16, W, RT, RT == 1>;
+  constexpr int M = 16 * RT, NF = R::NF, NO = R::NO, kStep = 32;
+  constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides the one ahead
+  constexpr int kOutRow = W + 4;
+  __shared__ __attribute__((aligned(16))) float acc[KW * M * kOutRow];
+  __shared__ float stat[KW * M * 2];
+  __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys, then values
+
+  const int tid = threadIdx.x, lane = tid & 63, t = lane >> 4, x = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.H / a.Hkv;
+  Place w;
+  if (!place_of(a, p, lane, w)) return;
+  // ---- pages.  Step i of this wavefront begins at slot key0 + 32 (KW i + wave).  Pages are looked up for kLooked
+  // steps and the one ahead at once, block k of the i-th by lane 2 i + k, the first ones while the length is
+  // (entries past it are not used).
+  const int key0 = w.split * p.run, my0 = key0 + kStep * wave, most = max(a.max_seq_len - 1, 0);
+  const int64_t table = static_cast<int64_t>(w.b) * a.kv.max_pages;
   auto pages_of = [&](int step) {
-    return a.kv.table[table + (min(my0 + kStep * KW * (step + lane / 2) + kKv4Block * (lane & 1), last) >> a.kv.page_shift)];
+    return a.kv.table[table + (min(my0 + kStep * KW * (step + lane / 2) + kKv4Block * (lane & 1), most) >> a.kv.page_shift)];
   };
-  const uint8_t* const head = a.kv.pages + hk * a.kv.head_stride;
-  auto block = [&](int held, int nth, int step, int k) {
+  int held = pages_of(0);
+  const int n = kv4_len(a.kv, w.b, a.max_seq_len), key1 = min(n, key0 + p.run);
+  const int row0 = w.b * a.L * G + w.tile * M, rows = min(M, a.L * G - w.tile * M);
+  if (key0 >= n && p.part) return leave_empty(a, p, w, row0, rows);
+
+  R rs;
+  rs.begin(a, w.hk, row0, rows, n, key1, lane);
+  const int last = max(key1 - 1, 0) & ~(kKv4Block - 1);
+  const uint8_t* const head = a.kv.pages + w.hk * a.kv.head_stride;
+  auto block = [&](int nth, int step, int k) {
     const int page = clamp_id(__builtin_amdgcn_readlane(held, 2 * nth + k), a.kv.n_pages);
     const int j = min(my0 + kStep * KW * step + kKv4Block * k, last);
     return head + page * a.kv.page_stride + (j & ((1 << a.kv.page_shift) - 1)) / kKv4Block * kv4_block_bytes(W);
   };
   typedef uint32_t Codes __attribute__((ext_vector_type(W / 32)));
-  // chunk `lane` of a block's keys or values: a wavefront reads them in one piece
-  auto codes = [&](const uint8_t* blk) { return *reinterpret_cast<const Codes*>(blk + lane * static_cast<uint32_t>(sizeof(Codes))); };
+  // Chunk `lane` of a block's keys or values: a wavefront reads them in one piece, and one tile's rows are the only
+  // ones to read them (64 caches of 500 to 8000 keys: 73 us as ordinary loads, 64 so).
+  auto codes = [&](const uint8_t* blk) {
+    const auto* at = reinterpret_cast<const Codes*>(blk + lane * static_cast<uint32_t>(sizeof(Codes)));
+    if constexpr (RT == 1) return __builtin_nontemporal_load(at);
+    return *at;
+  };
   // the pair of key lane % 32 in the lower lanes, of value lane % 32 in the upper ones
   auto mark_of = [&](const uint8_t* b0, const uint8_t* b1) {
     return *reinterpret_cast<const uint32_t*>((lane & 16 ? b1 : b0) + static_cast<uint32_t>(16 * W + (lane & 32 ? 64 : 0) + 4 * x));
   };
-
-  floatx4 o[RT][NO];
-  // m: the subtracted logit (unscaled); mc = c m - lift, lift = kTop - unit; l: this lane's part of the
-  // sum of the weights; add: its part of what joins every element of the output
-  float m[RT], mc[RT], l[RT], add[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    m[r] = -INFINITY;
-    mc[r] = l[r] = add[r] = 0.f;
-#pragma unroll
-    for (int d = 0; d < NO; ++d) o[r][d] = floatx4{};
-  }
-  int unit = kLeastUnit<F16>;
-  float limit = lane & 32 ? __builtin_ldexpf(1.f, F16 ? unit : unit + 60) : INFINITY;  // of a value's size within that unit
-  bool wide = false;                               // a row's mc is past kFine (the same in all lanes)
   float2* const my_marks = marks + 64 * wave;
   // what joins a slot's lowest value, in steps: of a value the middle of its codes, of a key less what bf16 codes
   // stand on
@@ -217,209 +408,80 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : 2) void kv4_attend_kernel(Kv
 
   const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
   if (steps > 0) {
-    int held = pages_of(0);
-    const uint8_t *blk[kAhead][2];
-    Codes k[kAhead][2], v[kAhead][2];
-    uint32_t mark[kAhead];
-    each_index<kAhead>([&](auto index) {
-      constexpr int s = index;
-      blk[s][0] = block(held, s, s, 0);
-      blk[s][1] = block(held, s, s, 1);
-      k[s][0] = codes(blk[s][0]);
-      k[s][1] = codes(blk[s][1]);
-      mark[s] = mark_of(blk[s][0], blk[s][1]);
-      __builtin_amdgcn_sched_barrier(0);           // in the order in which the loop has them on their way
-      v[s][0] = codes(blk[s][0] + 8 * W);
-      v[s][1] = codes(blk[s][1] + 8 * W);
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    // One step, from register set s, which then gets the step kAhead later.
-    auto attend = [&](auto set, int step, int nth) {
-      constexpr int s = set;
-      const int j0 = my0 + kStep * KW * step;
-      // ---- S^T = K Q^T over the codes: register u of block i is slot 16 i + 4 t + u
-      floatx4 z[RT][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          const uint4 kf = key_codes<F16>(k[s][i][f], bits);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, q[r][f], f == 0 ? floatx4{} : z[r][i]);
-        }
-      // ---- steps and lowest values: one slot a lane, handed round through LDS
-      {
-        float st = kv4_step<F16>(mark[s]), y = kv4_low<F16>(mark[s]);
-        if (j0 + kStep > key1 && j0 + (lane & 31) >= key1) st = y = 0.f;   // what lies past the run may be anything
-        const float size = fmaxf(st, fabsf(y) * 0.0625f);
-        my_marks[lane] = make_float2(st, fmaf(middle, st, y));
-        if (__any(size > limit)) {
-          const float finite = lane & 32 && size < INFINITY ? size : 0.f;
-          const int grown = max(unit, __builtin_amdgcn_frexp_expf(wave_allmax(finite)) - (F16 ? 0 : 60));
-          const float f = __builtin_ldexpf(1.f, unit - grown);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            l[r] *= f;
-            add[r] *= f;
-#pragma unroll
-            for (int d = 0; d < NO; ++d) o[r][d] *= f;
-            mc[r] = m[r] == -INFINITY ? 0.f : m[r] * c - static_cast<float>(kTop<F16> - grown);
-          }
-          unit = grown;
-          limit = lane & 32 ? __builtin_ldexpf(1.f, F16 ? unit : unit + 60) : INFINITY;
-        }
-      }
-      asm volatile("" ::: "memory");               // LDS works in order for a wavefront; so must the compiler
-      __builtin_amdgcn_wave_barrier();
-      // ---- the keys of a later step
-      blk[s][0] = block(held, nth + kAhead, step + kAhead, 0);
-      blk[s][1] = block(held, nth + kAhead, step + kAhead, 1);
-      k[s][0] = codes(blk[s][0]);
-      k[s][1] = codes(blk[s][1]);
-      mark[s] = mark_of(blk[s][0], blk[s][1]);
-      __builtin_amdgcn_sched_barrier(0);
-
-      // slots 16 i + 4 t + 2 u and the next one; a block's at a time, for want of registers
-      auto pairs = [&](int of, int i, int u) { return *reinterpret_cast<const float4*>(my_marks + of + 16 * i + 4 * t + 2 * u); };
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const float4 p = pairs(0, i, u);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            z[r][i][2 * u] = fmaf(p.x, z[r][i][2 * u], p.y * qz[r]);
-            z[r][i][2 * u + 1] = fmaf(p.z, z[r][i][2 * u + 1], p.w * qz[r]);
-          }
-        }
-        if (RT == 1) __builtin_amdgcn_sched_barrier(0);
-      }
-      const bool cut = j0 + kStep > key1 || (masked && j0 + kStep > base);
-      uint32_t seen[RT];                           // bit 4 i + u: slot 16 i + 4 t + u
-      if (cut) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          seen[r] = 0;
-          if (RT == 1 && masked) word[0] = a.mask[(row0 + min(x, rows - 1)) / G];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int first = j0 + 16 * i + 4 * t;
-            seen[r] |= seen4(word[r], masked ? first - base : 0, key1 - first) << (4 * i);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) z[r][i][u] = (seen[r] >> (4 * i + u)) & 1 ? z[r][i][u] : -INFINITY;
-          }
-        }
-      }
-      // ---- softmax statistics.  The subtracted logit follows the maximum only once that is kLag ahead.
-      float top[RT];
-      bool behind = false;
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        top[r] = z[r][0][0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], z[r][i / 4][i % 4]);
-        behind |= (top[r] - m[r]) * c > kLag<F16>;
-      }
-      if (__any(behind)) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const float up = fmaxf(m[r], swap32_max(swap16_max(top[r])));
-          const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
-          l[r] *= f;
-          add[r] *= f;
-#pragma unroll
-          for (int d = 0; d < NO; ++d) o[r][d] *= f;
-          m[r] = up;
-          mc[r] = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
-        }
-        bool far = false;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) far |= fabsf(mc[r]) > kFine;
-        wide = __any(far);
-      }
-      float sub[RT];
-#pragma unroll
-      for (int r = 0; r < RT; ++r) sub[r] = mc[r];
-      if (wide) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const float from = m[r] == -INFINITY ? 0.f : m[r];
-          sub[r] = static_cast<float>(unit - kTop<F16>);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z[r][i / 4][i % 4] -= from;
-        }
-      }
-      // ---- weights.  p s is rounded to the cache's type, as the products take it; the sums of p and
-      // p y are of unrounded numbers.
-      uint32_t w[RT][4];
-      float sum[RT], lows[RT];
-#pragma unroll
-      for (int r = 0; r < RT; ++r) sum[r] = lows[r] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 both = pairs(32, i / 2, i % 2);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          float4 y = both;
-          if (cut) {                               // what a row does not see may hold anything
-            const bool see0 = (seen[r] >> (2 * i)) & 1, see1 = (seen[r] >> (2 * i + 1)) & 1;
-            y = make_float4(see0 ? y.x : 0.f, see0 ? y.y : 0.f, see1 ? y.z : 0.f, see1 ? y.w : 0.f);
-          }
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2)], c, -sub[r]));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2) + 1], c, -sub[r]));
-          sum[r] += p0 + p1;
-          lows[r] = fmaf(p0, y.y, fmaf(p1, y.w, lows[r]));
-          w[r][i] = pack2<F16>(p0 * y.x, p1 * y.z);
-          lows[r] = less_middle<F16>(w[r][i], lows[r]);
-        }
-        if (RT == 1 && i == 1) __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        l[r] += sum[r];
-        add[r] += lows[r];
-      }
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_wave_barrier();
-      // ---- out^T += D^T W^T over the codes
-      each_index<NO>([&](auto index) {
-        constexpr int d = index, y = 2 * (d / 4), j = d % 4;
-        const uint4 f = make_uint4(value_codes<F16, j>(v[s][0][y], bits), value_codes<F16, j>(v[s][0][y + 1], bits),
-                                   value_codes<F16, j>(v[s][1][y], bits), value_codes<F16, j>(v[s][1][y + 1], bits));
-#pragma unroll
-        for (int r = 0; r < RT; ++r) o[r][d] = mfma16<F16>(f, make_uint4(w[r][0], w[r][1], w[r][2], w[r][3]), o[r][d]);
-      });
-      v[s][0] = codes(blk[s][0] + 8 * W);
-      v[s][1] = codes(blk[s][1] + 8 * W);
-      __builtin_amdgcn_sched_barrier(0);
-    };
+    const uint8_t *b0 = block(0, 0, 0), *b1 = block(0, 0, 1);
+    Codes k[2], v[2];
+    k[0] = codes(b0);
+    k[1] = codes(b1);
+    uint32_t mark = mark_of(b0, b1);
+    __builtin_amdgcn_sched_barrier(0);             // in the order in which the loop has them on their way
+    v[0] = codes(b0 + 8 * W);
+    v[1] = codes(b1 + 8 * W);
     for (int step0 = 0; step0 < steps; step0 += kLooked) {
-      const int held_next = pages_of(step0 + kLooked), end = min(steps - step0, kLooked);
+      const int end = min(steps - step0, kLooked);
       for (int nth = 0; nth < end; ++nth) {
-        attend(std::integral_constant<int, 0>{}, step0 + nth, nth);
-        if constexpr (kAhead == 2) {
-          if (++nth >= end) break;
-          attend(std::integral_constant<int, 1>{}, step0 + nth, nth);
+        const int step = step0 + nth, j0 = my0 + kStep * KW * step;
+        // ---- S^T = K Q^T over the codes
+        floatx4 z[RT][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int f = 0; f < NF; ++f) {
+            const uint4 kf = key_codes<F16>(k[i][f], bits);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, rs.q[r][f], f == 0 ? floatx4{} : z[r][i]);
+          }
+        // ---- steps and lowest values: one slot a lane, handed round through LDS
+        float st = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
+        uint32_t odd = 0;
+        if (rs.cut(j0)) {
+          const bool past = j0 + (lane & 31) >= key1;                     // what lies past the run may be anything
+          const bool finite = fabsf(st) < INFINITY && fabsf(y) < INFINITY;
+          odd = static_cast<uint32_t>(__ballot(!past && !finite) >> 32);
+          if (past || (lane & 32 && !finite)) st = y = 0.f;
         }
+        my_marks[lane] = make_float2(st, fmaf(middle, st, y));
+        rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
+        asm volatile("" ::: "memory");             // LDS works in order for a wavefront; so must the compiler
+        __builtin_amdgcn_wave_barrier();
+        // ---- the next step's keys
+        b0 = block(nth + 1, step + 1, 0);
+        b1 = block(nth + 1, step + 1, 1);
+        k[0] = codes(b0);
+        k[1] = codes(b1);
+        mark = mark_of(b0, b1);
+        __builtin_amdgcn_sched_barrier(0);
+        uint32_t wt[RT][4];
+        rs.weigh(z, my_marks, my_marks + 32, odd, j0, lane, G, wt);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        // ---- out^T += D^T W^T over the codes
+        each_index<NO>([&](auto index) {
+          constexpr int d = index, u = 2 * (d / 4), j = d % 4;
+          const uint4 f = make_uint4(value_codes<F16, j>(v[0][u], bits), value_codes<F16, j>(v[0][u + 1], bits),
+                                     value_codes<F16, j>(v[1][u], bits), value_codes<F16, j>(v[1][u + 1], bits));
+#pragma unroll
+          for (int r = 0; r < RT; ++r) rs.o[r][d] = mfma16<F16>(f, make_uint4(wt[r][0], wt[r][1], wt[r][2], wt[r][3]), rs.o[r][d]);
+        });
+        v[0] = codes(b0 + 8 * W);
+        v[1] = codes(b1 + 8 * W);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      held = held_next;
+      if (step0 + kLooked < steps) held = pages_of(step0 + kLooked);
     }
   }
 
   // ---- join the wavefronts and write
+  rs.finish();
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int at = wave * M + 16 * r + x;
-    const float total = swap32_sum(swap16_sum(l[r])), all = swap32_sum(swap16_sum(add[r]));
     each_index<NO>([&](auto index) {
       constexpr int d = index;
-      constexpr float f = !F16 ? 1.f : d % 2 ? 0x1p20f : 0x1p24f;
-      *reinterpret_cast<float4*>(acc + at * kOutRow + 16 * d + 4 * t) =
-          make_float4(fmaf(o[r][d][0], f, all), fmaf(o[r][d][1], f, all), fmaf(o[r][d][2], f, all), fmaf(o[r][d][3], f, all));
+      *reinterpret_cast<float4*>(acc + at * kOutRow + 16 * d + 4 * t) = rs.template elements<d>(r);
     });
     if (t == 0) {
-      stat[at * 2] = total == 0.f ? -INFINITY : mc[r];
-      stat[at * 2 + 1] = total;
+      stat[at * 2] = rs.l[r] == 0.f ? -INFINITY : rs.mc[r];
+      stat[at * 2 + 1] = rs.l[r];
     }
   }
   __syncthreads();
@@ -427,15 +489,15 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : 2) void kv4_attend_kernel(Kv
     const int r = i / (W / 4), e = i % (W / 4) * 4;
     float top = -INFINITY, total = 0.f;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) top = fmaxf(top, stat[(w * M + r) * 2]);
+    for (int v = 0; v < KW; ++v) top = fmaxf(top, stat[(v * M + r) * 2]);
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
-      const float mw = stat[(w * M + r) * 2];
+    for (int v = 0; v < KW; ++v) {
+      const float mw = stat[(v * M + r) * 2];
       if (mw == -INFINITY) continue;               // no key seen
       const float f = __builtin_amdgcn_exp2f(mw - top);
-      total += f * stat[(w * M + r) * 2 + 1];
-      const float4 y = *reinterpret_cast<const float4*>(acc + (w * M + r) * kOutRow + e);
+      total += f * stat[(v * M + r) * 2 + 1];
+      const float4 y = *reinterpret_cast<const float4*>(acc + (v * M + r) * kOutRow + e);
       sum.x += f * y.x;
       sum.y += f * y.y;
       sum.z += f * y.z;
@@ -443,40 +505,28 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 4 : 2) void kv4_attend_kernel(Kv
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const int row = row0 + r;
-    const int64_t out = static_cast<int64_t>(row / G) * a.H + hk * G + row % G;
-    if (e < a.D) {
-      if (p.part)
-        *reinterpret_cast<float4*>(p.part + (out * p.splits + split) * a.D + e) =
-            make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-      else
-        *reinterpret_cast<uint2*>(a.out + out * a.D + e) =
-            make_uint2(pack2<F16>(sum.x * inv, sum.y * inv), pack2<F16>(sum.z * inv, sum.w * inv));
-    }
-    if (e == 0) {
-      const float lse = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
-      if (p.part)
-        p.part_lse[out * p.splits + split] = lse;
-      else if (a.lse)
-        a.lse[out] = lse;
-    }
+    const int64_t out = static_cast<int64_t>(row / G) * a.H + w.hk * G + row % G;
+    if (e < a.D) put<F16>(a, p, out, p.own_first + w.split, e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+    if (e == 0) put_lse(a, p, out, p.own_first + w.split, top, total);
   }
 }
 
-// A launch's rows a tile, and the workgroups that the GPU holds at once.
-struct Shape { int rows, waves, slots; };
-Shape shape_for(int64_t rows) { return rows <= 16 ? Shape{16, 4, 4 * kCUs} : Shape{32, 4, 2 * kCUs}; }
+// A launch's rows a tile, slots of a step of the whole workgroup, and the workgroups that the GPU holds at once.
+struct Shape { int rows, keys, slots; };
+Shape shape_for(int64_t rows) {
+  return rows <= 16 ? Shape{16, 128, 3 * kCUs} : Shape{32, 128, 2 * kCUs};
+}
 
 // Runs of the own keys.  A workgroup's start, its join and the partial sums of its rows, written and read
 // again, count as `start` keys.  One sequence's runs are of one length, and take rounds of workgroups.
 // Sequences differ in lengths that are not known here: the last workgroup to end then has at most a run
 // more than its share of all.
 Runs kv4_runs(int keys, int B, int64_t whole, Shape shape, int rows) {
-  const int step = 32 * shape.waves;
   const double start = 500. + 24. * rows;
   Runs best{};
   double least = 1e300;
   for (int s = 1; s <= 64; ++s) {
-    const int run = ceil_div(ceil_div(keys, s), step) * step, count = ceil_div(keys, run);
+    const int run = ceil_div(ceil_div(keys, s), shape.keys) * shape.keys, count = ceil_div(keys, run);
     if (s > 1 && whole * count > kMostRuns) break;
     const double rounds = static_cast<double>(whole * count) / shape.slots;
     const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start) : run + start * std::max(1., rounds));
