@@ -42,7 +42,7 @@ struct Kv4Plan {
   float* part_lse;       // [rows][splits]
   int groups, tiles, run;  // (sequence, head, split) triples, row tiles, slots of a run
   int splits, own_first;
-  int by_length;         // whether long sequences go first
+  int by_length;         // whether long runs go first
 };
 
 // What the sum of the rounded weights is times, in `add`: weights are of codes about 8, so that their
@@ -110,23 +110,49 @@ __device__ __forceinline__ uint32_t seen4(uint64_t word, int at, int left) {
 
 __device__ __forceinline__ uint32_t part_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Which rows and slots a workgroup has: row tiles of a group follow each other on one XCD; first runs of
-// all sequences go first, then second ones, ...: later runs are fewer where lengths differ.
+// Sum of v over the lanes before this one.
+__device__ __forceinline__ int sum_before(int v, int lane) {
+  int sum = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int other = __shfl_up(sum, d, kWave);
+    sum += lane >= d ? other : 0;
+  }
+  return sum - v;
+}
+
+// Which rows and slots a workgroup has: row tiles of a group follow each other on one XCD.
 struct Place {
   int hk, b, split, tile;
 };
 __device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Plan& p, int lane, Place& w) {
   const int bid = blockIdx.x, group = bid / 8 / p.tiles * 8 + bid % 8;
   if (group >= p.groups) return false;
+  // first runs of all sequences go first, then second ones, ...: later runs are fewer where lengths differ
   w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, bid / 8 % p.tiles};
-  if (p.by_length) {                               // the b-th longest sequence, of at most 64
-    const int len = lane < a.B ? kv4_len(a.kv, lane, a.max_seq_len) : -1;
-    int before = 0;
-    for (int i = 0; i < a.B; ++i) {
-      const int other = __builtin_amdgcn_readlane(len, i);
-      before += other > len || (other == len && i < lane);
+  if (p.by_length) {
+    // Long runs first (64 caches of 500 to 8000 slots, 4 runs each: 54 us in the order above, 45 so): the whole ones,
+    // then the last ones of all sequences (at most 64, one a lane) by length, then what lies past them.
+    const int runs = p.splits - p.own_first, nth = group / a.Hkv;
+    const int len = lane < a.B ? kv4_len(a.kv, lane, a.max_seq_len) : 0;
+    const int whole = lane < a.B ? min(len / p.run, runs - 1) : 0, rest = len - whole * p.run;
+    const int first = sum_before(whole, lane), wholes = __builtin_amdgcn_readlane(first + whole, 63);
+    if (nth < wholes) {
+      w.b = __builtin_ctzll(__ballot(nth >= first && nth < first + whole));
+      w.split = nth - __builtin_amdgcn_readlane(first, w.b);
+    } else if (nth < wholes + a.B) {
+      int before = 0;
+      for (int i = 0; i < a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(rest, i);
+        before += other > rest || (other == rest && i < lane);
+      }
+      w.b = __builtin_ctzll(__ballot(lane < a.B && before == nth - wholes));
+      w.split = __builtin_amdgcn_readlane(whole, w.b);
+    } else {
+      const int left = lane < a.B ? runs - 1 - whole : 0, from = wholes + a.B + sum_before(left, lane);
+      w.b = __builtin_ctzll(__ballot(nth >= from && nth < from + left));
+      w.split = __builtin_amdgcn_readlane(whole, w.b) + 1 + nth - __builtin_amdgcn_readlane(from, w.b);
     }
-    w.b = __builtin_ctzll(__ballot(before == w.b));
   }
   return true;
 }
@@ -517,19 +543,24 @@ Shape shape_for(int64_t rows) {
   return rows <= 16 ? Shape{16, 128, 3 * kCUs} : Shape{32, 128, 2 * kCUs};
 }
 
+// Whether a launch's workgroups go by length: those of more than a round, and lengths that a wavefront has at hand.
+bool by_length(int B, double rounds) { return B > 1 && B <= 64 && rounds > 1; }
+
 // Runs of the own keys.  A workgroup's start, its join and the partial sums of its rows, written and read
 // again, count as `start` keys.  One sequence's runs are of one length, and take rounds of workgroups.
 // Sequences differ in lengths that are not known here: the last workgroup to end then has at most a run
-// more than its share of all.
+// more than its share of all, and about a third of one where long runs go first.  (64 caches of 500 to
+// 8000 slots: 1 run 74 us, 2 runs 58, 3 runs 62, 8 runs 65; 32 of 40 to 4000 with 32 heads: 53, 57, 61, 76.)
 Runs kv4_runs(int keys, int B, int64_t whole, Shape shape, int rows) {
-  const double start = 500. + 24. * rows;
+  const double start = 650. + 24. * rows;
   Runs best{};
   double least = 1e300;
   for (int s = 1; s <= 64; ++s) {
     const int run = ceil_div(ceil_div(keys, s), shape.keys) * shape.keys, count = ceil_div(keys, run);
     if (s > 1 && whole * count > kMostRuns) break;
     const double rounds = static_cast<double>(whole * count) / shape.slots;
-    const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start) : run + start * std::max(1., rounds));
+    const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start)
+                                                          : run * (by_length(B, rounds) ? 0.35 : 1.) + start * std::max(1., rounds));
     if (cost < least) {
       least = cost;
       best = {count, run};
@@ -554,7 +585,7 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len
     c.p.run = r.keys;
     c.p.groups = B * Hkv * r.count;
     c.p.splits = r.count;
-    c.p.by_length = r.count == 1 && B > 1 && B <= 64 && B * Hkv * c.p.tiles > s.slots;
+    c.p.by_length = by_length(B, static_cast<double>(c.p.groups) * c.p.tiles / s.slots);
   }
   c.p.own_first = c.pre_splits;
   c.p.splits += c.pre_splits;
