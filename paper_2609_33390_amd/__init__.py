@@ -910,11 +910,13 @@ def _attend(entry, where, workspace_size, tag, q, cache, prefix, block_mask, sca
         _dev_tensor(lse, "lse", torch.float32, shape=(B, L, H), device=dev)
     most = cache.max_seq_len if max_seq_len is None else max_seq_len
     need = workspace_size(B, L, H, cache.n_kv_heads, D, P, most)
-    if workspace is None:
-        workspace = _workspace(dev, need, tag, stream)
-    st = entry(cache._ref, None if pre is None else ctypes.byref(pre), _ptr(q), row, head, _ptr(block_mask), B, L, H,
-               most, D ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(workspace),
-               _ws_bytes(workspace, dev, need), _stream_ptr(dev, stream))
+    if workspace is not None:
+        ws, nbytes = workspace.data_ptr(), _ws_bytes(workspace, dev, need)
+    else:
+        ws, nbytes = (_workspace(dev, need, tag, stream).data_ptr(), need) if need else (None, 0)
+    st = entry(cache._ref, None if pre is None else ctypes.byref(pre), q.data_ptr(), row, head, _ptr(block_mask), B, L, H,
+               most, D ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(), ws, nbytes,
+               _stream_ptr(dev, stream))
     _check(st, where)
     return out, lse
 

@@ -819,9 +819,6 @@ int brisk_kv4_attention(const brisk_kv4_cache* cache, const brisk_kv_prefix* pre
     pre.pre_slot_stride = prefix->slot_stride;
     pre.pre_head_stride = prefix->head_stride;
   }
-  const size_t need = brisk::kv4_attention_workspace_bytes(B, L, n_heads, cache->n_kv_heads, cache->d_head,
-                                                           prefix_len, max_seq_len);
-  if (ws_bytes < need || (need > 0 && !ws)) return BRISK_ERR_WORKSPACE;
   if (!aligned16(ws)) return BRISK_ERR_UNSUPPORTED;
   a.q = pre.q = q;
   a.q_row_stride = pre.q_row_stride = q_row_stride;
@@ -837,7 +834,8 @@ int brisk_kv4_attention(const brisk_kv4_cache* cache, const brisk_kv_prefix* pre
   a.max_seq_len = max_seq_len;
   pre.prefix_len = prefix_len;
   a.scale = pre.scale = scale;
-  brisk::launch_kv4_attention(a, pre, cache->dtype == BRISK_F16, ws, static_cast<hipStream_t>(stream));
+  if (!brisk::launch_kv4_attention(a, pre, cache->dtype == BRISK_F16, ws, ws_bytes, static_cast<hipStream_t>(stream)))
+    return BRISK_ERR_WORKSPACE;
   return launch_status();
 }
 

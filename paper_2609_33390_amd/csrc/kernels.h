@@ -137,8 +137,9 @@ struct Kv4AttentionArgs {
   float scale;
 };
 size_t kv4_attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len);
-// `pre` holds the same call as the attention over a 2-byte prefix sees it (no cache).
-void launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, hipStream_t s);
+// `pre` holds the same call as the attention over a 2-byte prefix sees it (no cache).  False, with nothing launched,
+// where the workspace is too small.
+bool launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, size_t ws_bytes, hipStream_t s);
 
 // ---- received attention weight, eviction ---------------------------------------
 struct ScoreArgs {

@@ -359,22 +359,6 @@ struct Rows {
   }
 };
 
-// Elements e .. e + 3 of a row's normalised sum, and its log-sum-exp, to where the plan has them.
-template <bool F16>
-__device__ __forceinline__ void put(const Kv4AttentionArgs& a, const Kv4Plan& p, int64_t out, int split, int e, float4 v) {
-  if (p.part)
-    *reinterpret_cast<float4*>(p.part + (out * p.splits + split) * a.D + e) = v;
-  else
-    *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(v.x, v.y), pack2<F16>(v.z, v.w));
-}
-__device__ __forceinline__ void put_lse(const Kv4AttentionArgs& a, const Kv4Plan& p, int64_t out, int split, float mc, float total) {
-  const float lse = total == 0.f ? -INFINITY : (mc + __builtin_amdgcn_logf(total)) * kLn2;
-  if (p.part)
-    p.part_lse[out * p.splits + split] = lse;
-  else if (a.lse)
-    a.lse[out] = lse;
-}
-
 // Few rows: RT tiles of 16 a workgroup, KW wavefronts that take steps of 32 slots in turn, each from
 // registers that its loads filled in operand order.
 template <bool F16, int W, int RT, int KW>
@@ -531,9 +515,21 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const int row = row0 + r;
-    const int64_t out = static_cast<int64_t>(row / G) * a.H + w.hk * G + row % G;
-    if (e < a.D) put<F16>(a, p, out, p.own_first + w.split, e, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
-    if (e == 0) put_lse(a, p, out, p.own_first + w.split, top, total);
+    const int64_t out = static_cast<int64_t>(row / G) * a.H + w.hk * G + row % G, at = out * p.splits + p.own_first + w.split;
+    sum = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+    if (e < a.D) {
+      if (p.part)
+        *reinterpret_cast<float4*>(p.part + at * a.D + e) = sum;
+      else
+        *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(sum.x, sum.y), pack2<F16>(sum.z, sum.w));
+    }
+    if (e == 0) {
+      const float lse = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+      if (p.part)
+        p.part_lse[at] = lse;
+      else if (a.lse)
+        a.lse[out] = lse;
+    }
   }
 }
 
@@ -556,7 +552,7 @@ Runs kv4_runs(int keys, int B, int64_t whole, Shape shape, int rows) {
   Runs best{};
   double least = 1e300;
   for (int s = 1; s <= 64; ++s) {
-    const int run = ceil_div(ceil_div(keys, s), shape.keys) * shape.keys, count = ceil_div(keys, run);
+    const int run = (keys + s * shape.keys - 1) / (s * shape.keys) * shape.keys, count = (keys + run - 1) / run;
     if (s > 1 && whole * count > kMostRuns) break;
     const double rounds = static_cast<double>(whole * count) / shape.slots;
     const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start)
@@ -565,6 +561,7 @@ Runs kv4_runs(int keys, int B, int64_t whole, Shape shape, int rows) {
       least = cost;
       best = {count, run};
     }
+    if (run == shape.keys) break;                  // no shorter ones
   }
   return best;
 }
@@ -592,6 +589,12 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len
   return c;
 }
 
+size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
+  if (c.p.splits <= 1) return 0;
+  const size_t runs = static_cast<size_t>(rows) * c.p.splits;
+  return (runs + 3) / 4 * 16 + runs * D * sizeof(float);
+}
+
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const Kv4Plan& p, hipStream_t s) {
   const dim3 grid((p.groups + 7) / 8 * 8 * p.tiles);
@@ -605,18 +608,17 @@ void launch_own(const Kv4AttentionArgs& a, const Kv4Plan& p, hipStream_t s) {
 
 // Workspace: where rows have several runs, a log-sum-exp and D sums of each.
 size_t kv4_attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len) {
-  const CallPlan c = make_plan(B, L, H, Hkv, prefix_len, max_seq_len);
-  if (c.p.splits <= 1) return 0;
-  const size_t runs = static_cast<size_t>(B) * L * H * c.p.splits;
-  return (runs + 3) / 4 * 16 + runs * D * sizeof(float);
+  return bytes_of(make_plan(B, L, H, Hkv, prefix_len, max_seq_len), static_cast<int64_t>(B) * L * H, D);
 }
 
-void launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, hipStream_t s) {
+bool launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, size_t ws_bytes, hipStream_t s) {
   CallPlan c = make_plan(a.B, a.L, a.H, a.Hkv, pre.prefix_len, a.max_seq_len);
-  if (c.p.splits > 1) {
-    const size_t runs = static_cast<size_t>(a.B) * a.L * a.H * c.p.splits;
+  const int64_t rows = static_cast<int64_t>(a.B) * a.L * a.H;
+  const size_t need = bytes_of(c, rows, a.D);
+  if (ws_bytes < need || (need > 0 && !ws)) return false;
+  if (need > 0) {
     c.p.part_lse = static_cast<float*>(ws);
-    c.p.part = c.p.part_lse + (runs + 3) / 4 * 4;
+    c.p.part = c.p.part_lse + (static_cast<size_t>(rows) * c.p.splits + 3) / 4 * 4;
   }
   if (c.pre_splits) launch_attention_prefix(pre, f16, c.p.part, c.p.part_lse, c.p.splits, s);
   if (c.p.groups) {
@@ -627,6 +629,7 @@ void launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, b
       wide ? launch_own<false, 128>(a, c.p, s) : launch_own<false, 64>(a, c.p, s);
   }
   if (c.p.part) launch_attention_join(pre, f16, c.p.part, c.p.part_lse, c.p.splits, s);
+  return true;
 }
 
 }  // namespace brisk
