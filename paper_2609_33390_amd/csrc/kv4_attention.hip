@@ -430,16 +430,6 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
       const int end = min(steps - step0, kLooked);
       for (int nth = 0; nth < end; ++nth) {
         const int step = step0 + nth, j0 = my0 + kStep * KW * step;
-        // ---- S^T = K Q^T over the codes
-        floatx4 z[RT][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int f = 0; f < NF; ++f) {
-            const uint4 kf = key_codes<F16>(k[i][f], bits);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, rs.q[r][f], f == 0 ? floatx4{} : z[r][i]);
-          }
         // ---- steps and lowest values: one slot a lane, handed round through LDS
         float st = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
         uint32_t odd = 0;
@@ -450,9 +440,19 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
           if (past || (lane & 32 && !finite)) st = y = 0.f;
         }
         my_marks[lane] = make_float2(st, fmaf(middle, st, y));
-        rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
         asm volatile("" ::: "memory");             // LDS works in order for a wavefront; so must the compiler
         __builtin_amdgcn_wave_barrier();
+        // ---- S^T = K Q^T over the codes
+        floatx4 z[RT][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int f = 0; f < NF; ++f) {
+            const uint4 kf = key_codes<F16>(k[i][f], bits);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, rs.q[r][f], f == 0 ? floatx4{} : z[r][i]);
+          }
+        rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
         // ---- the next step's keys
         b0 = block(nth + 1, step + 1, 0);
         b1 = block(nth + 1, step + 1, 1);
@@ -533,10 +533,14 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
   }
 }
 
-// A launch's rows a tile, slots of a step of the whole workgroup, and the workgroups that the GPU holds at once.
-struct Shape { int rows, keys, slots; };
-Shape shape_for(int64_t rows) {
-  return rows <= 16 ? Shape{16, 128, 3 * kCUs} : Shape{32, 128, 2 * kCUs};
+// A launch's rows a tile, wavefronts, slots of a step of the whole workgroup, and the workgroups that the GPU
+// holds at once.  Few rows over short caches take two wavefronts instead of four: they start and join
+// sooner, and more of them are at hand (lengths up to 512: 256 caches of 4 heads 15.6 us against 17.3, of 32 heads 68
+// against 87; up to 1024: 29 against 25, 61 against 66; up to 2048: 41 against 38).
+struct Shape { int rows, waves, keys, slots; };
+Shape shape_for(int64_t rows, int max_seq_len) {
+  if (rows > 16) return {32, 4, 128, 2 * kCUs};
+  return max_seq_len > 768 ? Shape{16, 4, 128, 3 * kCUs} : Shape{16, 2, 64, 6 * kCUs};
 }
 
 // Whether a launch's workgroups go by length: those of more than a round, and lengths that a wavefront has at hand.
@@ -576,7 +580,7 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len
   c.pre_splits = prefix_len > 0 ? attention_prefix_splits(B, L, H, Hkv, prefix_len) : 0;
   if (max_seq_len > 0 || prefix_len == 0) {
     const int rows = L * (H / Hkv);
-    const Shape s = shape_for(rows);
+    const Shape s = shape_for(rows, max_seq_len);
     c.p.tiles = ceil_div(rows, s.rows);
     const Runs r = kv4_runs(max_seq_len > 0 ? max_seq_len : 1, B, static_cast<int64_t>(B) * Hkv * c.p.tiles, s, std::min(rows, s.rows));
     c.p.run = r.keys;
@@ -598,10 +602,13 @@ size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const Kv4Plan& p, hipStream_t s) {
   const dim3 grid((p.groups + 7) / 8 * 8 * p.tiles);
-  switch (shape_for(static_cast<int64_t>(a.L) * (a.H / a.Hkv)).rows) {
-    case 16: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, dim3(256), 0, s, a, p); break;
-    default: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, dim3(256), 0, s, a, p); break;
-  }
+  const Shape shape = shape_for(static_cast<int64_t>(a.L) * (a.H / a.Hkv), a.max_seq_len);
+  if (shape.rows > 16)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, dim3(256), 0, s, a, p);
+  else if (shape.waves > 2)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, dim3(256), 0, s, a, p);
+  else
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 2>), grid, dim3(128), 0, s, a, p);
 }
 
 }  // namespace
