@@ -703,7 +703,8 @@ int brisk_kv4_write(const brisk_kv4_cache* cache, const uint16_t* k, const uint1
 /*
  * Reads T slots of every sequence back, from slot first[b] on (0 where first is
  * NULL): k and v [B, T, n_kv_heads, d_head] get type(fl(z + s c)), and 0 for slots
- * outside [0, seq_len[b]).  Limits as brisk_kv4_write.
+ * outside [0, seq_len[b]).  Limits as brisk_kv4_write; the outputs must overlap
+ * neither the inputs nor one another (BRISK_ERR_UNSUPPORTED).
  */
 int brisk_kv4_read(const brisk_kv4_cache* cache, int32_t B, int32_t T, const int32_t* first,
                    uint16_t* k, uint16_t* v, void* stream);
@@ -719,9 +720,12 @@ int brisk_kv4_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, in
  * type.  The prefix is in 2 bytes, as there (the batch holds it once).  Arguments,
  * masks, empty rows, hidden slots and the roundings of the results are those of
  * brisk_block_attention (weights are rounded to the cache's type where they meet
- * the codes).
+ * the codes; a weight counts by how far a value lies from the middle of its head's
+ * range).
  *
- * Limits as there, with B * L * n_heads <= 2^22.  Deterministic.
+ * Limits as there, with B * L * n_heads <= 2^22.  A logit is made of s times
+ * products with codes and of z times the query's sum: (31 s + |z|) sum_d |q_d| must
+ * be finite in fp32, or the row is not a number.  Deterministic.
  */
 int brisk_kv4_attention(const brisk_kv4_cache* cache, const brisk_kv_prefix* prefix, const uint16_t* q,
                         int64_t q_row_stride, int64_t q_head_stride, const uint64_t* block_mask,

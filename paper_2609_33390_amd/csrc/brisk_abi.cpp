@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <iterator>
+#include <utility>
 
 #include "brisk.h"
 #include "kernels.h"
@@ -24,6 +25,16 @@ bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0
 
 constexpr int32_t kMaxProfileM = 1024;
 constexpr int32_t kMaxProfileBlocks = 1 << 30;
+
+// A device buffer of a call, for the question whether two of them share memory.
+struct Span {
+  const void* p;
+  uint64_t bytes;
+};
+bool overlap(Span a, Span b) {
+  const uint64_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
 
 constexpr int32_t kMaxAttnRows = 1 << 24;
 constexpr int32_t kMaxSlots = 1 << 30;
@@ -72,6 +83,23 @@ int64_t kv4_part_bytes(int32_t page_size, int32_t d_head) {
   return static_cast<int64_t>(page_size) * brisk::kv4_slot_bytes(brisk::kv4_width(d_head));
 }
 
+// What the pages of the 4-bit cache span, and whether no two parts of them are the same memory.
+struct Kv4Reach {
+  Span span;
+  bool apart;
+};
+Kv4Reach kv4_reach(const brisk_kv4_cache* c) {
+  const int64_t part = kv4_part_bytes(c->page_size, c->d_head);
+  int64_t inner = c->head_stride, outer = c->page_stride, inner_n = c->n_kv_heads, outer_n = c->n_pages;
+  if (outer < inner) {
+    std::swap(inner, outer);
+    std::swap(inner_n, outer_n);
+  }
+  const __int128 row = static_cast<__int128>(inner_n - 1) * inner + part;
+  const bool apart = (inner_n == 1 || inner >= part) && (outer_n == 1 || outer >= row);
+  return {{c->pages, static_cast<uint64_t>(row + static_cast<__int128>(outer_n - 1) * outer)}, apart};
+}
+
 // Rows of a block's queries: [B * L, n_heads] with head groups of the cache.
 int block_rows_check(int32_t B, int32_t L, int32_t n_heads, int32_t n_kv_heads) {
   if (B < 1 || L < 1 || L > 64 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 ||
@@ -104,16 +132,6 @@ bool places_apart(const brisk_kv_cache* c) {
     span += static_cast<__int128>(x.size - 1) * x.stride;
   }
   return true;
-}
-
-// A device buffer of a call, for the question whether two of them share memory.
-struct Span {
-  const void* p;
-  uint64_t bytes;
-};
-bool overlap(Span a, Span b) {
-  const uint64_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 
 // Tokens of a call on the 4-bit cache, and what its launch holds.
@@ -720,20 +738,12 @@ int brisk_kv4_write(const brisk_kv4_cache* cache, const uint16_t* k, const uint1
       !aligned4(first) || !aligned4(count))
     return BRISK_ERR_UNSUPPORTED;
   // Wavefronts write some slots while others read their tokens, lengths and pages.
-  const int64_t part = kv4_part_bytes(cache->page_size, cache->d_head);
-  const bool pages_outside = cache->page_stride >= cache->head_stride;
-  const int64_t inner = pages_outside ? cache->head_stride : cache->page_stride;
-  const int64_t outer = pages_outside ? cache->page_stride : cache->head_stride;
-  const int64_t inner_n = pages_outside ? cache->n_kv_heads : cache->n_pages;
-  const int64_t outer_n = pages_outside ? cache->n_pages : cache->n_kv_heads;
-  if ((inner_n > 1 && inner < part) ||
-      (outer_n > 1 && outer < static_cast<__int128>(inner_n > 1 ? (inner_n - 1) * static_cast<__int128>(inner) : 0) + part))
-    return BRISK_ERR_UNSUPPORTED;
+  const Kv4Reach pages = kv4_reach(cache);
+  if (!pages.apart) return BRISK_ERR_UNSUPPORTED;
   const uint64_t seqs = static_cast<uint64_t>(B) * 4;
-  const uint64_t reach = static_cast<uint64_t>(inner_n - 1) * inner + static_cast<uint64_t>(outer_n - 1) * outer + part;
   const uint64_t span = 2 * (static_cast<uint64_t>(B - 1) * seq_stride + static_cast<uint64_t>(T - 1) * row_stride +
                              static_cast<uint64_t>(cache->n_kv_heads - 1) * head_stride + cache->d_head);
-  const Span out{cache->pages, reach};
+  const Span out = pages.span;
   if (overlap(out, {k, span}) || overlap(out, {v, span}) || overlap(out, {first, seqs}) ||
       (count && overlap(out, {count, seqs})) || overlap(out, {cache->seq_len, seqs}) ||
       overlap(out, {cache->block_table, seqs * cache->max_pages}))
@@ -764,9 +774,9 @@ int brisk_kv4_read(const brisk_kv4_cache* cache, int32_t B, int32_t T, const int
   if (!aligned16(k) || !aligned16(v) || !aligned4(first)) return BRISK_ERR_UNSUPPORTED;
   const uint64_t seqs = static_cast<uint64_t>(B) * 4;
   const uint64_t bytes = 2 * static_cast<uint64_t>(B) * T * cache->n_kv_heads * cache->d_head;
-  const Span outs[] = {{k, bytes}, {v, bytes}};
+  const Span outs[] = {{k, bytes}, {v, bytes}}, pages = kv4_reach(cache).span;
   for (const Span& out : outs)
-    if ((first && overlap(out, {first, seqs})) || overlap(out, {cache->seq_len, seqs}) ||
+    if (overlap(out, pages) || (first && overlap(out, {first, seqs})) || overlap(out, {cache->seq_len, seqs}) ||
         overlap(out, {cache->block_table, seqs * cache->max_pages}))
       return BRISK_ERR_UNSUPPORTED;
   if (overlap(outs[0], outs[1])) return BRISK_ERR_UNSUPPORTED;

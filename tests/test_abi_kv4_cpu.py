@@ -87,7 +87,8 @@ def test_write_refuses_pages_that_share_memory(kw):
 @pytest.mark.parametrize("kw,want", [
     (dict(k=None), ENULL), (dict(v=None), ENULL), (dict(B=0), ESHAPE), (dict(T=0), ESHAPE), (dict(T=-3), ESHAPE),
     (dict(T=1 << 29), ESHAPE), (dict(k=ODD), EUNSUP), (dict(v=ODD), EUNSUP), (dict(first=ODD), EUNSUP),
-    (dict(k=FAKE), EUNSUP), (dict(v=FAKE), EUNSUP), (dict(v=0x20000000), EUNSUP), (dict(v=0x20000000 + 4 * 16 * 8 * 256 - 16), EUNSUP),
+    (dict(k=FAKE), EUNSUP), (dict(v=FAKE), EUNSUP), (dict(v=0x20000000), EUNSUP), (dict(k=PAGES), EUNSUP),
+    (dict(v=PAGES + 100 * 8 * PART - 16), EUNSUP), (dict(k=PAGES - 4 * 16 * 8 * 256 + 16), EUNSUP), (dict(v=0x20000000 + 4 * 16 * 8 * 256 - 16), EUNSUP),
 ])
 def test_read_validation(kw, want):
     assert _read(**kw) == want

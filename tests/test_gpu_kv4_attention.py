@@ -65,6 +65,39 @@ def test_attention_matches_oracle(kw):
     c.check(*_run(c))
 
 
+@pytest.mark.parametrize("kw", [
+    # more runs than workgroups at once, of sequences that a wavefront orders by length (up to 64 of them) or not
+    dict(B=64, L=1, H=16, Hkv=16, lens=[(977 * b) % 1500 for b in range(64)], page=64),
+    dict(B=40, L=1, H=16, Hkv=16, lens=[0, 128, 256, 2048, 2050, 4100] + [(1301 * b) % 4000 for b in range(34)], dtype="f16"),
+    dict(B=33, L=2, H=32, Hkv=32, lens=[2000] * 33, mask="causal"),
+    dict(B=64, L=17, H=16, Hkv=16, lens=[17 + (61 * b) % 200 for b in range(64)], mask="causal", dtype="f16"),
+    dict(B=70, L=1, H=8, Hkv=8, lens=[(733 * b) % 2600 for b in range(70)], page=128),
+    dict(B=65, L=1, H=16, Hkv=16, lens=[(389 * b) % 800 for b in range(65)]),
+    dict(B=2, L=1, H=64, Hkv=64, lens=[769, 20000], page=1024),
+])
+def test_batches_of_many_runs(kw):
+    c = Case4(brisk, D=64, prefix=None, seed=kw["B"], **kw)
+    c.check(*_run(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L", [2, 20])
+def test_queries_that_are_not_finite(L, dtype):
+    """A row's query of NaN or infinities stays out of the other rows (which may be rescaled at another step than
+    beside a finite one, so they are within their tolerances, not the same bits)."""
+    c = Case4(brisk, 2, L, 4, 2, 64, 40, [L, 90], mask="causal", dtype=dtype, seed=9)
+    o, z, tol, ltol = c.expect()
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        q = c.q.clone()
+        q[1, 1, 3, 7] = bad
+        out, lse = brisk.kv4_attention(q.cuda(), c.cache, prefix=c.gpu_prefix(), block_mask=c.gpu_mask(), scale=c.scale)
+        keep = np.ones((2, L, 4), dtype=bool)
+        keep[1, 1, 3] = False
+        assert (np.abs(out.double().cpu().numpy() - o) <= tol)[keep].all()
+        assert (np.abs(lse.double().cpu().numpy() - z) <= ltol)[keep].all()
+        assert not torch.isfinite(out[1, 1, 3]).any()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("D", [64, 96, 128])
 def test_as_the_attention_over_what_is_read_back(D, dtype):
