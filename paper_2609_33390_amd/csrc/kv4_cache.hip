@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_write_kernel(Kv4WriteArgs a, 
   const int64_t first = a.first[b], count = a.count ? min(max(a.count[b], 0), a.T) : a.T;
   const int64_t cap = static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift;
   const int64_t j0 = block_begin(first) + 16 * static_cast<int64_t>(nth);
-  if (j0 < 0 || j0 >= cap || j0 >= first + count || j0 + 16 <= first) return;
+  if (count < 1 || j0 < 0 || j0 >= cap || j0 >= first + count || j0 + 16 <= first) return;
   // A lane whose slot gets no token, and one that holds no elements (D < W), works on others' and stores nothing.
   const int64_t tok = j0 + key - first;
   const bool valid = tok >= 0 && tok < count;

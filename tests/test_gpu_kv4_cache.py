@@ -136,6 +136,15 @@ def test_tokens_go_where_they_are_told_and_nothing_else_changes():
     assert (cache.pages[spare] == 0xFF).all()     # a page of nobody
 
 
+def test_sequences_without_tokens_read_none():
+    """A count of 0 inside a block: there is no token to read, not the one before the first either."""
+    cache = _cache(2, 2, 64, 16, 2)
+    before = cache.pages.clone()
+    k, v = _tokens(2, 5, 2, 64)
+    brisk.kv4_write(k.cuda(), v.cuda(), cache, _i32([5, 21]), count=_i32([0, -3]))
+    assert torch.equal(cache.pages, before)
+
+
 @pytest.mark.parametrize("W", [64, 128])
 def test_a_token_writes_its_own_bytes_only(W):
     """Every byte of a block belongs to one slot: 16 single tokens leave what one call leaves, and each changes
