@@ -51,15 +51,17 @@ struct Kv4Plan {
 // codes stand on 128 besides.
 template <bool F16> constexpr float kMiddle = F16 ? 8.f : 136.f;
 
-// acc - kMiddle times the sum of a pair.
+// acc + f times the sum of a pair; f is a number of the type.
 template <bool F16>
-__device__ __forceinline__ float less_middle(uint32_t pair, float acc) {
+__device__ __forceinline__ float plus_pair(uint32_t pair, float f, float acc) {
   if constexpr (F16) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, pair), h2{-8, -8}, acc, false);
+    const auto g = static_cast<_Float16>(f);
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, pair), h2{g, g}, acc, false);
   } else {
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, pair), __builtin_bit_cast(b2, 0xC308C308u), acc, false);
+    const auto g = static_cast<__bf16>(f);
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, pair), b2{g, g}, acc, false);
   }
 }
 
@@ -141,12 +143,17 @@ __device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Pla
       w.b = __builtin_ctzll(__ballot(nth >= first && nth < first + whole));
       w.split = nth - __builtin_amdgcn_readlane(first, w.b);
     } else if (nth < wholes + a.B) {
-      int before = 0;
-      for (int i = 0; i < a.B; ++i) {
-        const int other = __builtin_amdgcn_readlane(rest, i);
-        before += other > rest || (other == rest && i < lane);
+      // the sequence that so many come before, from the highest bit of the lengths down
+      uint64_t those = __ballot(lane < a.B);
+      int before = nth - wholes;
+      for (int bit = 31 - __builtin_clz(p.run); bit >= 0; --bit) {
+        const uint64_t ones = those & __ballot((rest >> bit) & 1);
+        const int n = __builtin_popcountll(ones);
+        those = before < n ? ones : those & ~ones;
+        before -= before < n ? 0 : n;
       }
-      w.b = __builtin_ctzll(__ballot(lane < a.B && before == nth - wholes));
+      for (; before > 0; --before) those &= those - 1;
+      w.b = __builtin_ctzll(those);
       w.split = __builtin_amdgcn_readlane(whole, w.b);
     } else {
       const int left = lane < a.B ? runs - 1 - whole : 0, from = wholes + a.B + sum_before(left, lane);
@@ -207,8 +214,7 @@ struct Rows {
         const int e = t * (W / 4) + 8 * i;
         q[r][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          sum += half_to_f32<F16>(part_of(q[r][i], w) & 0xFFFF) + half_to_f32<F16>(part_of(q[r][i], w) >> 16);
+        for (int w = 0; w < 4; ++w) sum = plus_pair<F16>(part_of(q[r][i], w), 1.f, sum);
       }
       sum = swap32_sum(swap16_sum(sum));
       qz[r] = F16 ? sum * 0x1p-21f : sum;
@@ -292,15 +298,20 @@ struct Rows {
       behind |= (top[r] - m[r]) * c > kLag<F16>;
     }
     if (__any(behind)) {
-      bool far = false;
+      bool far = false, held = false;              // whether a row holds anything yet
+#pragma unroll
+      for (int r = 0; r < RT; ++r) held |= m[r] != -INFINITY;
+      held = __any(held);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const float up = fmaxf(m[r], swap32_max(swap16_max(top[r])));
         const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
-        l[r] *= f;
-        add[r] *= f;
+        if (held) {
+          l[r] *= f;
+          add[r] *= f;
 #pragma unroll
-        for (int d = 0; d < NO; ++d) o[r][d] *= f;
+          for (int d = 0; d < NO; ++d) o[r][d] *= f;
+        }
         m[r] = up;
         mc[r] = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
         far |= fabsf(mc[r]) > kFine;
@@ -334,7 +345,7 @@ struct Rows {
         sum[r] = i == 0 ? p0 + p1 : sum[r] + (p0 + p1);
         lows[r] = fmaf(p0, y.y, i == 0 ? p1 * y.w : fmaf(p1, y.w, lows[r]));
         w[r][i] = pack2<F16>(p0 * y.x, p1 * y.z);
-        lows[r] = less_middle<F16>(w[r][i], lows[r]);
+        lows[r] = plus_pair<F16>(w[r][i], -kMiddle<F16>, lows[r]);
       }
     }
 #pragma unroll
@@ -368,7 +379,8 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
   constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides the one ahead
   constexpr int kOutRow = W + 4;
   __shared__ __attribute__((aligned(16))) float acc[KW * M * kOutRow];
-  __shared__ float stat[KW * M * 2];
+  __shared__ float stat[KW * M * 2], factor[KW * M];
+  __shared__ int place[M];
   __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys, then values
 
   const int tid = threadIdx.x, lane = tid & 63, t = lane >> 4, x = lane & 15;
@@ -495,40 +507,47 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
     }
   }
   __syncthreads();
+  if (tid < rows) {                                // what the wavefronts' sums of a row are times
+    float top = -INFINITY, total = 0.f, f[KW];
+#pragma unroll
+    for (int v = 0; v < KW; ++v) top = fmaxf(top, stat[(v * M + tid) * 2]);
+#pragma unroll
+    for (int v = 0; v < KW; ++v) {
+      const float mw = stat[(v * M + tid) * 2];
+      f[v] = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);   // no key seen
+      total += f[v] * stat[(v * M + tid) * 2 + 1];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int v = 0; v < KW; ++v) factor[tid * KW + v] = f[v] * inv;
+    const int row = row0 + tid;
+    const int out = row / G * a.H + w.hk * G + row % G, at = out * p.splits + p.own_first + w.split;   // below 2^22, 2^29
+    place[tid] = p.part ? at : out;
+    const float lse = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    if (p.part)
+      p.part_lse[at] = lse;
+    else if (a.lse)
+      a.lse[out] = lse;
+  }
+  __syncthreads();
   for (int i = tid; i < rows * (W / 4); i += 64 * KW) {
     const int r = i / (W / 4), e = i % (W / 4) * 4;
-    float top = -INFINITY, total = 0.f;
-#pragma unroll
-    for (int v = 0; v < KW; ++v) top = fmaxf(top, stat[(v * M + r) * 2]);
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int v = 0; v < KW; ++v) {
-      const float mw = stat[(v * M + r) * 2];
-      if (mw == -INFINITY) continue;               // no key seen
-      const float f = __builtin_amdgcn_exp2f(mw - top);
-      total += f * stat[(v * M + r) * 2 + 1];
+      const float f = factor[r * KW + v];
       const float4 y = *reinterpret_cast<const float4*>(acc + (v * M + r) * kOutRow + e);
       sum.x += f * y.x;
       sum.y += f * y.y;
       sum.z += f * y.z;
       sum.w += f * y.w;
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const int row = row0 + r;
-    const int64_t out = static_cast<int64_t>(row / G) * a.H + w.hk * G + row % G, at = out * p.splits + p.own_first + w.split;
-    sum = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
     if (e < a.D) {
+      const int64_t to = static_cast<int64_t>(place[r]) * a.D + e;
       if (p.part)
-        *reinterpret_cast<float4*>(p.part + at * a.D + e) = sum;
+        *reinterpret_cast<float4*>(p.part + to) = sum;
       else
-        *reinterpret_cast<uint2*>(a.out + out * a.D + e) = make_uint2(pack2<F16>(sum.x, sum.y), pack2<F16>(sum.z, sum.w));
-    }
-    if (e == 0) {
-      const float lse = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
-      if (p.part)
-        p.part_lse[at] = lse;
-      else if (a.lse)
-        a.lse[out] = lse;
+        *reinterpret_cast<uint2*>(a.out + to) = make_uint2(pack2<F16>(sum.x, sum.y), pack2<F16>(sum.z, sum.w));
     }
   }
 }
