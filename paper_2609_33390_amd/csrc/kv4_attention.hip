@@ -488,7 +488,10 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
         v[1] = codes(b1 + 8 * W);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (step0 + kLooked < steps) held = pages_of(step0 + kLooked);
+      if (step0 + kLooked < steps) {
+        held = pages_of(step0 + kLooked);
+        asm volatile("" : "+v"(held));             // waited for here: in the loop each step's codes would be waited for with it
+      }
     }
   }
 
