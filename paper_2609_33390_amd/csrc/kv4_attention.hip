@@ -370,10 +370,10 @@ struct Rows {
   }
 };
 
-// Few rows: RT tiles of 16 a workgroup, KW wavefronts that take steps of 32 slots in turn, each from
+// RT tiles of 16 rows a workgroup, KW wavefronts that take steps of 32 slots in turn, each from
 // registers that its loads filled in operand order.
 template <bool F16, int W, int RT, int KW>
-__global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
+__global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
   using R = Rows<F16, W, RT, RT == 1>;
   constexpr int M = 16 * RT, NF = R::NF, NO = R::NO, kStep = 32;
   constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides the one ahead
@@ -555,60 +555,97 @@ __global__ __launch_bounds__(64 * KW, RT == 1 ? 3 : 2) void kv4_attend_kernel(Kv
   }
 }
 
-// A launch's rows a tile, wavefronts, slots of a step of the whole workgroup, and the workgroups that the GPU
-// holds at once.  Few rows over short caches take two wavefronts instead of four: they start and join
-// sooner, and more of them are at hand (lengths up to 512: 256 caches of 4 heads 15.6 us against 17.3, of 32 heads 68
-// against 87; up to 1024: 29 against 25, 61 against 66; up to 2048: 41 against 38).
-struct Shape { int rows, waves, keys, slots; };
-Shape shape_for(int64_t rows, int max_seq_len) {
-  if (rows > 16) return {32, 4, 128, 2 * kCUs};
-  return max_seq_len > 768 ? Shape{16, 4, 128, 3 * kCUs} : Shape{16, 2, 64, 6 * kCUs};
-}
+// A launch's workgroups: rows of a tile, wavefronts, and the runs of the own keys.
+struct Shape {
+  int rows, waves;
+  Runs runs;
+};
+constexpr int kHeld = 2 * 4 * kCUs;                // wavefronts that the GPU works on without a wait for a place
 
 // Whether a launch's workgroups go by length: those of more than a round, and lengths that a wavefront has at hand.
 bool by_length(int B, double rounds) { return B > 1 && B <= 64 && rounds > 1; }
 
-// Runs of the own keys.  A workgroup's start, its join and the partial sums of its rows, written and read
+// More than 16 rows.  A workgroup's start, its join and the partial sums of its rows, written and read
 // again, count as `start` keys.  One sequence's runs are of one length, and take rounds of workgroups.
 // Sequences differ in lengths that are not known here: the last workgroup to end then has at most a run
-// more than its share of all, and about a third of one where long runs go first.  (64 caches of 500 to
-// 8000 slots: 1 run 74 us, 2 runs 58, 3 runs 62, 8 runs 65; 32 of 40 to 4000 with 32 heads: 53, 57, 61, 76.)
-Runs kv4_runs(int keys, int B, int64_t whole, Shape shape, int rows) {
+// more than its share of all, and about a third of one where long runs go first.
+Shape many_rows(int keys, int B, int64_t whole, int rows) {
+  constexpr int kKeys = 128;
   const double start = 650. + 24. * rows;
-  Runs best{};
+  Shape best{32, 4, {}};
   double least = 1e300;
   for (int s = 1; s <= 64; ++s) {
-    const int run = (keys + s * shape.keys - 1) / (s * shape.keys) * shape.keys, count = (keys + run - 1) / run;
+    const int run = (keys + s * kKeys - 1) / (s * kKeys) * kKeys, count = (keys + run - 1) / run;
     if (s > 1 && whole * count > kMostRuns) break;
-    const double rounds = static_cast<double>(whole * count) / shape.slots;
+    const double rounds = static_cast<double>(whole * count) * 4 / kHeld;
     const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start)
                                                           : run * (by_length(B, rounds) ? 0.35 : 1.) + start * std::max(1., rounds));
     if (cost < least) {
       least = cost;
-      best = {count, run};
+      best.runs = {count, run};
     }
-    if (run == shape.keys) break;                  // no shorter ones
+    if (run == kKeys) break;                       // no shorter ones
+  }
+  return best;
+}
+
+// Up to 16 rows: 2, 4 or 8 wavefronts a workgroup, by what a plan would take in us.  A round of wavefronts takes
+// kStart and kStep for each of its steps; lengths may be all the same or anything up to the bound, and the
+// plan is for the mean of both.  Runs cost a second launch, the scratch (together at least kTwo a call, where one
+// launch takes kOne) and the partial sums.  So a batch is split when it does not fill the GPU,
+// and otherwise takes the wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52.6
+// us with 8 (71.6 with 4 and 134.9 with 2, in one round; 57.5 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 51.0
+// with 4 (60.9, 73.3), 128 of 600 18.2 with 2 (22.0 with 4, 25.6 with 8), 16 of 6000 22.1 in 2 runs with 8 (30.3 whole),
+// one of 1500 11.5 whole with 8 (12.5 in 6 runs or 12).
+Shape few_rows(int keys, int B, int64_t whole, int64_t rows, bool prefix) {
+  constexpr double kStart = 3., kStep = 1.1, kOne = 9., kTwo = 12.5, kRow = 2 * 512 / 5e6;
+  Shape best{16, 8, {}};
+  double least = 1e300;
+  for (int waves : {2, 4, 8}) {
+    const int step = 32 * waves;
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      const int run = (keys + s * step - 1) / (s * step) * step, count = (keys + run - 1) / run;
+      if (s > 1 && whole * count > kMostRuns) break;
+      const double steps = run / step * kStep, rounds = static_cast<double>(whole * count) * waves / kHeld;
+      // with 2 and 4 wavefronts the GPU holds half as many again, which then take as much longer; a last round that
+      // does not fill it shows where nothing is ordered
+      const double thirds = B > 64 && waves < 8 && rounds > 1 ? std::ceil(rounds / 1.5) * 1.5 : rounds;
+      const double same = std::max(1., B > 1 && rounds > 2 ? thirds : std::ceil(thirds)) * (steps + kStart);
+      const double total = rounds * (steps / 2 + kStart), longest = steps + kStart;
+      const double other = by_length(B, rounds) || rounds <= 1 ? std::max(longest, total) : total + steps / 2;
+      const bool two = count > 1 || prefix;
+      const double cost = std::max((B > 1 ? (same + other) / 2 : same) + (two ? 4.5 + kRow * rows * count : 0.), two ? kTwo : kOne);
+      if (cost < least) {
+        least = cost;
+        best.waves = waves;
+        best.runs = {count, run};
+      }
+      if (run == step) break;                      // no shorter ones
+    }
   }
   return best;
 }
 
 struct CallPlan {
   Kv4Plan p;
-  int pre_splits;
+  int pre_splits, rows, waves;
 };
 
 CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len) {
   CallPlan c{};
   c.pre_splits = prefix_len > 0 ? attention_prefix_splits(B, L, H, Hkv, prefix_len) : 0;
   if (max_seq_len > 0 || prefix_len == 0) {
-    const int rows = L * (H / Hkv);
-    const Shape s = shape_for(rows, max_seq_len);
-    c.p.tiles = ceil_div(rows, s.rows);
-    const Runs r = kv4_runs(max_seq_len > 0 ? max_seq_len : 1, B, static_cast<int64_t>(B) * Hkv * c.p.tiles, s, std::min(rows, s.rows));
-    c.p.run = r.keys;
-    c.p.groups = B * Hkv * r.count;
-    c.p.splits = r.count;
-    c.p.by_length = by_length(B, static_cast<double>(c.p.groups) * c.p.tiles / s.slots);
+    const int rows = L * (H / Hkv), keys = std::max(max_seq_len, 1);
+    const int64_t whole = static_cast<int64_t>(B) * Hkv;
+    c.p.tiles = rows > 16 ? ceil_div(rows, 32) : 1;
+    const Shape s = rows > 16 ? many_rows(keys, B, whole * c.p.tiles, std::min(rows, 32))
+                              : few_rows(keys, B, whole, static_cast<int64_t>(B) * L * H, prefix_len > 0);
+    c.rows = s.rows;
+    c.waves = s.waves;
+    c.p.run = s.runs.keys;
+    c.p.groups = B * Hkv * s.runs.count;
+    c.p.splits = s.runs.count;
+    c.p.by_length = by_length(B, static_cast<double>(c.p.groups) * c.p.tiles * s.waves / kHeld);
   }
   c.p.own_first = c.pre_splits;
   c.p.splits += c.pre_splits;
@@ -622,15 +659,16 @@ size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
 }
 
 template <bool F16, int W>
-void launch_own(const Kv4AttentionArgs& a, const Kv4Plan& p, hipStream_t s) {
-  const dim3 grid((p.groups + 7) / 8 * 8 * p.tiles);
-  const Shape shape = shape_for(static_cast<int64_t>(a.L) * (a.H / a.Hkv), a.max_seq_len);
-  if (shape.rows > 16)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, dim3(256), 0, s, a, p);
-  else if (shape.waves > 2)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, dim3(256), 0, s, a, p);
+void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
+  const dim3 grid((c.p.groups + 7) / 8 * 8 * c.p.tiles), threads(64 * c.waves);
+  if (c.rows > 16)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, threads, 0, s, a, c.p);
+  else if (c.waves == 8)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 8>), grid, threads, 0, s, a, c.p);
+  else if (c.waves == 4)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, threads, 0, s, a, c.p);
   else
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 2>), grid, dim3(128), 0, s, a, p);
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 2>), grid, threads, 0, s, a, c.p);
 }
 
 }  // namespace
@@ -653,9 +691,9 @@ bool launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, b
   if (c.p.groups) {
     const bool wide = kv4_width(a.D) == 128;
     if (f16)
-      wide ? launch_own<true, 128>(a, c.p, s) : launch_own<true, 64>(a, c.p, s);
+      wide ? launch_own<true, 128>(a, c, s) : launch_own<true, 64>(a, c, s);
     else
-      wide ? launch_own<false, 128>(a, c.p, s) : launch_own<false, 64>(a, c.p, s);
+      wide ? launch_own<false, 128>(a, c, s) : launch_own<false, 64>(a, c, s);
   }
   if (c.p.part) launch_attention_join(pre, f16, c.p.part, c.p.part_lse, c.p.splits, s);
   return true;

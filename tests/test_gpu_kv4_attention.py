@@ -80,6 +80,23 @@ def test_batches_of_many_runs(kw):
     c.check(*_run(c))
 
 
+@pytest.mark.parametrize("kw", [
+    dict(B=128, H=8, Hkv=8, D=8, lens=[600] * 127 + [3]),                      # two wavefronts, whole caches
+    dict(B=1, H=4, Hkv=2, D=64, lens=[4001]),                                  # and short runs
+    dict(B=64, H=8, Hkv=8, D=16, lens=[1024] + [40, 0] * 31 + [1]),            # four, whole
+    dict(B=65, H=8, Hkv=8, D=8, lens=[1999] * 3 + [0, 500] * 31, dtype="f16"),
+    dict(B=8, H=16, Hkv=8, D=72, lens=[6000, 5999, 1, 0, 4097, 1536, 1537, 3000]),  # eight, runs
+    dict(B=40, H=8, Hkv=8, D=8, lens=[3000] * 2 + [70, 900] * 19, dtype="f16"),  # eight, whole, by length
+    dict(B=3, H=32, Hkv=2, D=128, lens=[257, 256, 255], dtype="f16"),          # eight, all 16 rows
+    dict(B=3, H=8, Hkv=8, D=40, lens=[1500, 9, 0], prefix=77),
+], ids=str)
+def test_single_tokens_of_every_plan(kw):
+    kw = dict(kw)
+    B, H, Hkv, D, lens, prefix = (kw.pop(n, None) for n in ("B", "H", "Hkv", "D", "lens", "prefix"))
+    c = Case4(brisk, B, 1, H, Hkv, D, prefix, lens, seed=B, **kw)
+    c.check(*_run(c))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("L", [2, 20])
 def test_queries_that_are_not_finite(L, dtype):
