@@ -5,11 +5,14 @@
 //   out = (sum_j (p_j r_j) (d_j - 8) + sum_j p_j (y_j + 8 r_j)) / sum_j p_j
 // The matrix instructions work on the codes alone, whole numbers that their types
 // hold exactly; steps and lowest values meet the logits and the probabilities in
-// fp32.  A bf16 code is made with one instruction for two of them, by putting its
-// bits under an exponent (16 + c, 128 + d), and the 16 and 128 are taken out again:
+// fp32.  Two codes are made with one instruction, by putting their bits under an exponent
+// (bf16 16 + c and 128 + d, f16 64 + d), and the 16, 128 and 64 are taken out again:
 // from the logits through the lowest value, from the sums (with the 8) through the sum
-// of the rounded weights.  An f16 code is its own bits, a subnormal number (8 c and d or
-// 16 d times 2^-24), whose power of two the scale and the last step take out.
+// of the rounded weights.  An f16 key's code is its own bits, a subnormal number (8 c times
+// 2^-24), whose power of two the scale takes out.  Sums over such numbers are truncated
+// early, at about 2^-17 of the largest factor: logits have room for that, but outputs over long
+// caches had not (45000 slots of which 50 count: 4.9e-4 off, all to one side, where 2.6e-4 is
+// what the roundings of weights and outputs cost).
 //
 // Codes come from memory to registers in operand order, 32 slots of a head a step
 // of a wavefront, the next ones' on the way; the wavefronts of a workgroup take
@@ -48,8 +51,8 @@ struct Kv4Plan {
 // What the sum of the rounded weights is times, in `add`: weights are of codes about 8, so that their
 // rounding counts by how far a value lies from the middle of its head's range, not from the lowest one
 // (64 caches of 500 to 8000 keys: outputs off by 0.0046 from that, by 0.0022 from this); bf16
-// codes stand on 128 besides.
-template <bool F16> constexpr float kMiddle = F16 ? 8.f : 136.f;
+// codes stand on 128 besides, f16 ones on 64.
+template <bool F16> constexpr float kMiddle = F16 ? 72.f : 136.f;
 
 // acc + f times the sum of a pair; f is a number of the type.
 template <bool F16>
@@ -77,8 +80,10 @@ __device__ __forceinline__ floatx4 mfma16(uint4 a, uint4 b, floatx4 c) {
 
 // The masks of the codes in vector registers and what they stand on in scalar ones: an and-or takes
 // no literals, and one scalar operand.
+template <bool F16>
 struct CodeBits {
-  uint32_t key = 0x00780078, value = 0x000F000F, key_base = 0x41804180, value_base = 0x43004300;
+  uint32_t key = 0x00780078, value = F16 ? 0x00F000F0 : 0x000F000F;
+  uint32_t key_base = 0x41804180, value_base = F16 ? 0x54005400 : 0x43004300;
   __device__ __forceinline__ CodeBits() {
     asm("" : "+v"(key));
     asm("" : "+v"(value));
@@ -89,17 +94,17 @@ struct CodeBits {
 
 // Eight codes of a key: 16 + c in bf16, 8 c 2^-24 in f16.
 template <bool F16>
-__device__ __forceinline__ uint4 key_codes(uint32_t w, const CodeBits& k) {
+__device__ __forceinline__ uint4 key_codes(uint32_t w, const CodeBits<F16>& k) {
   const uint32_t w1 = w >> 4, w2 = w >> 8, w3 = __builtin_amdgcn_alignbit(w, w, 12);
   if constexpr (F16) return make_uint4(w & k.key, w1 & k.key, w2 & k.key, w3 & k.key);
   return make_uint4((w & k.key) | k.key_base, (w1 & k.key) | k.key_base, (w2 & k.key) | k.key_base, (w3 & k.key) | k.key_base);
 }
 
-// Nibble j of both halves of a word of values: 128 + d in bf16, d 2^-24 or (odd j) 16 d 2^-24 in f16.
+// Nibble j of both halves of a word of values: 128 + d in bf16, 64 + d in f16.
 template <bool F16, int J>
-__device__ __forceinline__ uint32_t value_codes(uint32_t w, const CodeBits& k) {
-  if constexpr (F16) return (w >> (J / 2 * 8)) & (J % 2 ? k.value << 4 : k.value);
-  return ((w >> (4 * J)) & k.value) | k.value_base;
+__device__ __forceinline__ uint32_t value_codes(uint32_t w, const CodeBits<F16>& k) {
+  constexpr int right = 4 * (F16 ? J - 1 : J);
+  return ((right < 0 ? w << 4 : w >> (right < 0 ? 0 : right)) & k.value) | k.value_base;
 }
 
 __device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
@@ -355,7 +360,7 @@ struct Rows {
     }
   }
 
-  // Sums of the rows over the wavefront; then element 16 d + 4 t + u of the (unnormalised) output is element(r, d, u).
+  // Sums of the rows over the wavefront; then elements 16 d + 4 t .. + 3 of the (unnormalised) output are elements<d>(r).
   __device__ __forceinline__ void finish() {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -365,8 +370,7 @@ struct Rows {
   }
   template <int d>
   __device__ __forceinline__ float4 elements(int r) const {
-    constexpr float f = !F16 ? 1.f : d % 2 ? 0x1p20f : 0x1p24f;
-    return make_float4(fmaf(o[r][d][0], f, add[r]), fmaf(o[r][d][1], f, add[r]), fmaf(o[r][d][2], f, add[r]), fmaf(o[r][d][3], f, add[r]));
+    return make_float4(o[r][d][0] + add[r], o[r][d][1] + add[r], o[r][d][2] + add[r], o[r][d][3] + add[r]);
   }
 };
 
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   // what joins a slot's lowest value, in steps: of a value the middle of its codes, of a key less what bf16 codes
   // stand on
   const float middle = lane & 32 ? 8.f : F16 ? 0.f : -16.f;
-  const CodeBits bits;
+  const CodeBits<F16> bits;
 
   const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
   if (steps > 0) {

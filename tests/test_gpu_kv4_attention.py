@@ -236,6 +236,28 @@ def test_weak_keys_in_long_runs_count():
         assert abs(lse.item() - (c.scale * 15 + np.log(total))) <= 2.0 ** -18 * 14
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_sums_over_long_caches_are_not_biased(dtype):
+    """45000 slots and logits of a wide spread.  The result's error is that of the roundings of the output and of the
+    weights: each is off by at most half a step, evenly spread, so by u / sqrt(3) of itself at most in the mean square, and
+    independent of the others.  With 8192 outputs and some hundred weights a row, that sum is known to 5 percent."""
+    u, n, H, D = torch.finfo(TYPES[dtype]).eps / 2, 45000, 8, 64
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn(1, n, 1, D, generator=g).to(TYPES[dtype]) for _ in range(2))
+    c = Case4(brisk, 1, 16, H, 1, D, None, [n], dtype=dtype, seed=5, q_std=2.0, k=k, v=v)
+    out = _run(c)[0].double().cpu().numpy().reshape(-1, D)
+    from kv4_cases import hold
+    (z, s, a), (y, r, d) = ([np.broadcast_to(x, k.shape)[0, :, 0] for x in hold(t, dtype)] for t in (k, v))
+    p = c.q.double().numpy().reshape(-1, D) @ (z + s * a).T * c.scale
+    p = np.exp(p - p.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    want = p @ (y + r * d)
+    square = (want ** 2).sum() + ((p ** 2) @ ((r * (d - 8)) ** 2)).sum()
+    assert ((out - want) ** 2).sum() <= 1.1 * u * u / 3 * square
+    off = np.abs((out - want).sum(1))                # to one side: no more than so many independent ones add up to
+    assert (off ** 2).sum() <= 1.3 * u * u / 3 * ((want ** 2).sum() + ((p ** 2) @ ((r * (d - 8)).sum(1) ** 2)).sum())
+
+
 def test_length_bound_and_table_are_clamped():
     c = Case4(brisk, 3, 2, 8, 2, 128, None, [90, 40, 7], mask="causal", seed=4)
     want = c.expect()
