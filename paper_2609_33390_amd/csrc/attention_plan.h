@@ -12,8 +12,8 @@ inline int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) 
 // Runs of `keys` keys that `whole` workgroups would cover: the fewest rounds of
 // workgroups, each counted as its keys and 512 for its start.  What that constant is
 // hardly matters (64 to 1500 plan the timing cases alike): the rule fills a round,
-// and weighs neither rows nor the bytes of the partial sums.  (64 caches of up to 2048 keys, 512 workgroups: whole caches 110 us,
-// runs of 512 keys 119, of 256 147.)
+// and weighs neither rows nor the bytes of the partial sums.  (64 caches of up to 2048
+// keys, 512 workgroups: whole caches 110 us, runs of 512 keys 119, of 256 147.)
 struct Runs { int count, keys; };
 constexpr int64_t kMostRuns = 1 << 20;
 inline Runs runs_of(int keys, int64_t whole, int step, int slots) {

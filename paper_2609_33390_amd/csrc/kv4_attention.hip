@@ -17,6 +17,16 @@
 // Codes come from memory to registers in operand order, 32 slots of a head a step
 // of a wavefront, the next ones' on the way; the wavefronts of a workgroup take
 // steps in turn and join through LDS.
+//
+// What bounds it.  Single tokens of a batch: the read of the cache (64 caches of 500 to 8000
+// slots of 8 heads, 300 MB in 54 us, 5.5 TB/s).  32 rows: vector and matrix instructions, which take
+// turns on a SIMD whatever its wavefronts are: a step's 290 vector ones (56 make the keys' codes,
+// 56 the values', 32 take steps and lowest values to the logits, 104 make the weights and their sums)
+// keep it for 1215 cycles, its 32 products for 512, and a step takes 1725.
+// (One block of 32 over 65536 slots: 61 us, 0.57 PFLOP/s.)  So more wavefronts a SIMD
+// (3 with the queries in LDS) or codes two steps ahead change nothing, 64 rows a
+// wavefront make half as many codes but leave half as many tiles to share a batch's ends.
+// A wavefront's 800 instructions before and after its steps count as two or three of them.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -138,7 +148,8 @@ __device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Pla
   // first runs of all sequences go first, then second ones, ...: later runs are fewer where lengths differ
   w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, bid / 8 % p.tiles};
   if (p.by_length) {
-    // Long runs first (64 caches of 500 to 8000 slots, 4 runs each: 54 us in the order above, 45 so): the whole ones,
+    // Long runs first (single tokens of 64 caches of 500 to 8000 slots: 68 us in the order above, 54 so; blocks of 16 over
+    // 16 to 4096: 80, 67; for more caches than that the search costs what the order gains): the whole ones,
     // then the last ones of all sequences (at most 64, one a lane) by length, then what lies past them.
     const int runs = p.splits - p.own_first, nth = group / a.Hkv;
     const int len = lane < a.B ? kv4_len(a.kv, lane, a.max_seq_len) : 0;
@@ -416,7 +427,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   };
   typedef uint32_t Codes __attribute__((ext_vector_type(W / 32)));
   // Chunk `lane` of a block's keys or values: a wavefront reads them in one piece, and one tile's rows are the only
-  // ones to read them (64 caches of 500 to 8000 keys: 73 us as ordinary loads, 64 so).
+  // ones to read them (64 caches of 500 to 8000 keys: 60 us as ordinary loads, 54 so; 32 of 40 to 4000 with 32 heads: 56, 51).
   auto codes = [&](const uint8_t* blk) {
     const auto* at = reinterpret_cast<const Codes*>(blk + lane * static_cast<uint32_t>(sizeof(Codes)));
     if constexpr (RT == 1) return __builtin_nontemporal_load(at);
@@ -572,7 +583,9 @@ bool by_length(int B, double rounds) { return B > 1 && B <= 64 && rounds > 1; }
 // More than 16 rows.  A workgroup's start, its join and the partial sums of its rows, written and read
 // again, count as `start` keys.  One sequence's runs are of one length, and take rounds of workgroups.
 // Sequences differ in lengths that are not known here: the last workgroup to end then has at most a run
-// more than its share of all, and about a third of one where long runs go first.
+// more than its share of all, and about a third of one where long runs go first.  (64 blocks of 16 over 16 to 4096
+// slots: 1 run 65 us, 2 runs 78; one of 32 over 65536: 12 runs 75, 16 61, 24 64; 13 of 21 over 5 to 1777: 46, 39, 42 in
+// 1, 2 and 3 runs.)
 Shape many_rows(int keys, int B, int64_t whole, int rows) {
   constexpr int kKeys = 128;
   const double start = 650. + 24. * rows;

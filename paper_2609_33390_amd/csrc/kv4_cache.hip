@@ -4,7 +4,13 @@
 //
 // A wavefront takes 16 slots of a head, aligned to the cache's blocks.  Lane
 // (q, key) = (lane / 16, lane % 16) holds a quarter of the key and a quarter of the
-// value, in the pieces that the block's layout keeps together.
+// value, in the pieces that the block's layout keeps together, so that codes leave it as
+// whole words and a block is written by one wavefront alone: tokens next to each other, which
+// a decoding step and a prompt give alike, share no bytes across wavefronts.
+//
+// Both passes are bound by memory.  Writing 8 x 4096 tokens of 8 heads of 128 (134 MB in, 36 MB out) takes
+// 19 us; reading 16 x 8190 slots back (97 MB in, 537 MB out) takes 90 us, 7.0 TB/s.  64
+// single tokens take 5 us to write and 4.8 to read, of which the launch is 3.
 #include "kernels.h"
 #include "kv4_common.h"
 
@@ -250,8 +256,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_read_kernel(Kv4ReadArgs a, in
   const uint32_t kp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 4 * key);
   const uint32_t vp = *reinterpret_cast<const uint32_t*>(blk + 16 * W + 64 + 4 * key);
 
-  // Heads go out through LDS, row after row, so that a store instruction covers whole lines; a row's
-  // 16-byte pieces are permuted by its number.
+  // Heads go out through LDS, row after row, so that a store instruction covers whole lines, and past the
+  // caches, which the outputs do not fit (16 x 8190 slots: 206 us from the registers, 148 through LDS, 90 so); a
+  // row's 16-byte pieces are permuted by its number.
   constexpr int kPieces = W / 8, kRowsOut = 64 / kPieces;
   __shared__ uint4 rows[kWaves][16 * kPieces];
   uint4* const mine = rows[threadIdx.x >> 6];
