@@ -258,6 +258,33 @@ def test_sums_over_long_caches_are_not_biased(dtype):
     assert (off ** 2).sum() <= 1.3 * u * u / 3 * ((want ** 2).sum() + ((p ** 2) @ ((r * (d - 8)).sum(1) ** 2)).sum())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B,L", [(256, 1), (64, 16)])
+def test_sums_in_one_long_run(B, L, dtype):
+    """A batch that fills the GPU without splitting caches of 131072 slots (all the same one): the bound of the test above,
+    for 1024 outputs, whose sum of squares is known to 5 percent in the standard deviation."""
+    dt, n, Hkv, G, D, page = TYPES[dtype], 131072, 4, 4, 64, 256
+    u = torch.finfo(dt).eps / 2
+    g = torch.Generator().manual_seed(B)
+    k, v = (torch.randn(1, n, Hkv, D, generator=g).to(dt) for _ in range(2))
+    q = (0.3 * torch.randn(B, L, G * Hkv, D, generator=g)).to(dt)
+    pages = torch.zeros(n // page, Hkv, brisk.kv4_page_bytes(page, D), dtype=torch.uint8, device="cuda")
+    table = torch.randperm(n // page, generator=g).to(torch.int32).cuda().view(1, -1)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    brisk.kv4_write(k.cuda(), v.cuda(), brisk.KVCache4(pages, table, lens[:1], D, dt), lens[:1] - n)
+    cache = brisk.KVCache4(pages, table.expand(B, -1).contiguous(), lens, D, dt)
+    out = brisk.kv4_attention(q.cuda(), cache)[0]
+    rows = 16 // L // G or 1                         # sequences that are looked at, key head 0
+    out = out[:rows, :, :G].double().cpu().numpy().reshape(-1, D)[:16]
+    from kv4_cases import hold
+    (z, s, a), (y, r, d) = ([np.broadcast_to(x, k.shape)[0, :, 0] for x in hold(t, dtype)] for t in (k, v))
+    p = q[:rows, :, :G].double().numpy().reshape(-1, D)[:16] @ (z + s * a).T * D ** -0.5
+    p = np.exp(p - p.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    want = p @ (y + r * d)
+    assert ((out - want) ** 2).sum() <= 1.2 * u * u / 3 * ((want ** 2).sum() + ((p ** 2) @ ((r * (d - 8)) ** 2)).sum())
+
+
 def test_length_bound_and_table_are_clamped():
     c = Case4(brisk, 3, 2, 8, 2, 128, None, [90, 40, 7], mask="causal", seed=4)
     want = c.expect()
