@@ -211,24 +211,33 @@ struct Rows {
 
   __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x, rows - 1)) / G]; }
 
-  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int n, int end, int lane) {
+  // The queries, which wait for nothing that the kernel reads first.
+  __device__ __forceinline__ void load(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int lane) {
     const int t = lane >> 4, x = lane & 15, G = a.H / a.Hkv;
     row0 = first_row;
     rows = n_rows;
-    key1 = end;
-    base = n - a.L;
     mask = a.mask;
-    c = uniform(a.scale * kLog2e * (F16 ? 0x1p21f : 1.f));
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int row = row0 + min(16 * r + x, rows - 1), bi = row / G;
       const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
       word[r] = !LEAN && mask ? mask[bi] : ~0ull;
+#pragma unroll
+      for (int i = 0; i < NF; ++i) q[r][i] = *reinterpret_cast<const uint4*>(src + min(t * (W / 4) + 8 * i, a.D - 8));
+    }
+  }
+
+  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane) {
+    const int t = lane >> 4;
+    key1 = end;
+    base = n - a.L;
+    c = uniform(a.scale * kLog2e * (F16 ? 0x1p21f : 1.f));
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NF; ++i) {
-        const int e = t * (W / 4) + 8 * i;
-        q[r][i] = e < a.D ? *reinterpret_cast<const uint4*>(src + e) : make_uint4(0, 0, 0, 0);
+        if (t * (W / 4) + 8 * i >= a.D) q[r][i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int w = 0; w < 4; ++w) sum = plus_pair<F16>(part_of(q[r][i], w), 1.f, sum);
       }
@@ -425,12 +434,12 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
     return a.kv.table[table + (min(my0 + kStep * KW * (step + lane / 2) + kKv4Block * (lane & 1), most) >> a.kv.page_shift)];
   };
   int held = pages_of(0);
-  const int n = kv4_len(a.kv, w.b, a.max_seq_len), key1 = min(n, key0 + p.run);
   const int row0 = w.b * a.L * G + w.tile * M, rows = min(M, a.L * G - w.tile * M);
+  R rs;
+  rs.load(a, w.hk, row0, rows, lane);
+  const int n = kv4_len(a.kv, w.b, a.max_seq_len), key1 = min(n, key0 + p.run);
   if (key0 >= n && p.part) return leave_empty(a, p, w, row0, rows);
 
-  R rs;
-  rs.begin(a, w.hk, row0, rows, n, key1, lane);
   const int last = max(key1 - 1, 0) & ~(kKv4Block - 1);
   const uint8_t* const head = a.kv.pages + w.hk * a.kv.head_stride;
   auto block = [&](int nth, int step, int k) {
@@ -457,6 +466,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   const CodeBits<F16> bits;
 
   const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
+  if (steps == 0) rs.begin(a, n, key1, lane);
   if (steps > 0) {
     const uint8_t *b0 = block(0, 0, 0), *b1 = block(0, 0, 1);
     Codes k[2], v[2];
@@ -466,6 +476,8 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
     __builtin_amdgcn_sched_barrier(0);             // in the order in which the loop has them on their way
     v[0] = codes(b0 + 8 * W);
     v[1] = codes(b1 + 8 * W);
+    __builtin_amdgcn_sched_barrier(0);
+    rs.begin(a, n, key1, lane);
     for (int step0 = 0; step0 < steps; step0 += kLooked) {
       const int end = min(steps - step0, kLooked);
       for (int nth = 0; nth < end; ++nth) {
