@@ -127,6 +127,34 @@ __device__ __forceinline__ uint32_t seen4(uint64_t word, int at, int left) {
 
 __device__ __forceinline__ uint32_t part_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// v where the banks (four lanes each of a row of 16) of `BANKS` have it, old elsewhere.
+template <int BANKS>
+__device__ __forceinline__ float in_banks(float old, float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), 0xE4, 0xF, BANKS, false));
+}
+// v of the lane N further in the row of 16 (SHIFT 0x100: the last ones get 0; 0x120: round the row).
+template <int SHIFT, int N>
+__device__ __forceinline__ uint32_t along_row(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), SHIFT + N, 0xF, 0xF, true));
+}
+template <int N> __device__ __forceinline__ float round_row(float v) { return __uint_as_float(along_row<0x120, N>(__float_as_uint(v))); }
+
+// Over the lanes that share a row: the four quarters and, of a row on SP lanes of each, those.
+template <int SP>
+__device__ __forceinline__ float row_sum(float v) {
+  v = swap32_sum(swap16_sum(v));
+  if constexpr (SP > 1) v += round_row<8>(v);
+  if constexpr (SP > 2) v += round_row<4>(v);
+  return v;
+}
+template <int SP>
+__device__ __forceinline__ float row_max(float v) {
+  v = swap32_max(swap16_max(v));
+  if constexpr (SP > 1) v = fmaxf(v, round_row<8>(v));
+  if constexpr (SP > 2) v = fmaxf(v, round_row<4>(v));
+  return v;
+}
+
 // Sum of v over the lanes before this one.
 __device__ __forceinline__ int sum_before(int v, int lane) {
   int sum = v;
@@ -191,10 +219,13 @@ __device__ __forceinline__ void leave_empty(const Kv4AttentionArgs& a, const Kv4
 
 // A wavefront's 16 RT rows: row x = lane % 16 of each tile, of which quarter t = lane / 16 has the logits
 // and the elements 4 t .. 4 t + 3 of every 16.
+// Up to 16 / SP rows stand SP times among the 16, and each of a row's lanes takes the weights of some of its logits only
+// (of 8 a lane 8 / SP): a cache of 1500 slots 10.4 us with SP = 4, 11.1 with 1.
 // `LEAN`: for wavefronts whose registers are few, values are read where they are used.
-template <bool F16, int W, int RT, bool LEAN>
+template <bool F16, int W, int RT, bool LEAN, int SP>
 struct Rows {
-  static constexpr int NF = W / 32, NO = W / 16;
+  static constexpr int NF = W / 32, NO = W / 16, NZ = 8 / SP, kRows = 16 / SP;
+  static_assert(SP == 1 || RT == 1);
   uint4 q[RT][NF];                                 // elements t W / 4 + ..., the second operand of K Q^T
   float qz[RT];                                    // sum of q, as the logits are held
   uint64_t word[RT];                               // what a row sees of the block (one tile reads it where it is used)
@@ -208,8 +239,9 @@ struct Rows {
   float c;                                         // f16 logits are held 2^-21 of what they are
   int key1, base, row0, rows;                      // end of the run, begin of the block, the wavefront's rows
   const uint64_t* mask;
+  int slot0;                                       // first of a step's slots whose weights this lane takes
 
-  __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x, rows - 1)) / G]; }
+  __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G]; }
 
   // The queries, which wait for nothing that the kernel reads first.
   __device__ __forceinline__ void load(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int lane) {
@@ -219,7 +251,7 @@ struct Rows {
     mask = a.mask;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const int row = row0 + min(16 * r + x, rows - 1), bi = row / G;
+      const int row = row0 + min(16 * r + x % kRows, rows - 1), bi = row / G;
       const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
       word[r] = !LEAN && mask ? mask[bi] : ~0ull;
 #pragma unroll
@@ -228,7 +260,8 @@ struct Rows {
   }
 
   __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane) {
-    const int t = lane >> 4;
+    const int t = lane >> 4, skip = (lane & 15) / kRows * NZ;
+    slot0 = 16 * (skip / 4) + 4 * t + skip % 4;
     key1 = end;
     base = n - a.L;
     c = uniform(a.scale * kLog2e * (F16 ? 0x1p21f : 1.f));
@@ -241,7 +274,7 @@ struct Rows {
 #pragma unroll
         for (int w = 0; w < 4; ++w) sum = plus_pair<F16>(part_of(q[r][i], w), 1.f, sum);
       }
-      sum = swap32_sum(swap16_sum(sum));
+      sum = swap32_sum(swap16_sum(sum));           // (columns of one row agree)
       qz[r] = F16 ? sum * 0x1p-21f : sum;
       m[r] = -INFINITY;
       mc[r] = l[r] = add[r] = 0.f;
@@ -281,21 +314,31 @@ struct Rows {
   // to weights, times the values' steps, as the second operand of D^T W^T.  `keys` and `values`: the slots'
   // steps and lowest values, in LDS.  Where cut(j0), those of values that are not finite are 0 there, since a
   // weight of 0 does not take them out, and `odd` says which: they count for the rows that see them.
-  __device__ __forceinline__ void weigh(floatx4 (&z)[RT][2], const float2* keys, const float2* values, uint32_t odd, int j0, int lane,
+  __device__ __forceinline__ void weigh(const floatx4 (&dots)[RT][2], const float2* keys, const float2* values, uint32_t odd, int j0, int lane,
                                         int G, uint32_t (&w)[RT][4]) {
-    const int t = lane >> 4, x = lane & 15;
-    // slots 16 i + 4 t + 2 u and the next one
-    auto pairs = [&](const float2* of, int i, int u) { return *reinterpret_cast<const float4*>(of + 16 * i + 4 * t + 2 * u); };
+    const int x = lane & 15;
+    // a lane's logit i is of slot slot0 + i, or on from 16 after four
+    auto pairs = [&](const float2* of, int i) { return *reinterpret_cast<const float4*>(of + slot0 + i / 4 * 16 + i % 4); };
+    float z[RT][NZ];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const float4 p = pairs(keys, i, u);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          z[r][i][2 * u] = fmaf(p.x, z[r][i][2 * u], p.y * qz[r]);
-          z[r][i][2 * u + 1] = fmaf(p.z, z[r][i][2 * u + 1], p.w * qz[r]);
+      for (int i = 0; i < NZ; ++i) {
+        z[r][i] = dots[r][i / 4][i % 4];
+        if constexpr (SP == 2) z[r][i] = in_banks<0xC>(z[r][i], dots[r][1][i]);
+        if constexpr (SP == 4) {
+          z[r][i] = in_banks<2>(z[r][i], dots[r][0][2 + i]);
+          z[r][i] = in_banks<4>(z[r][i], dots[r][1][i]);
+          z[r][i] = in_banks<8>(z[r][i], dots[r][1][2 + i]);
         }
+      }
+#pragma unroll
+    for (int i = 0; i < NZ; i += 2) {
+      const float4 p = pairs(keys, i);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        z[r][i] = fmaf(p.x, z[r][i], p.y * qz[r]);
+        z[r][i + 1] = fmaf(p.z, z[r][i + 1], p.w * qz[r]);
       }
     }
     if (cut(j0)) {
@@ -303,12 +346,12 @@ struct Rows {
       for (int r = 0; r < RT; ++r) {
         if (LEAN && mask) word[r] = sees(r, x, G);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int first = j0 + 16 * i + 4 * t;
-          const uint32_t seen = seen4(word[r], mask ? first - base : 0, key1 - first);
+        for (int i = 0; i < NZ; i += 4) {
+          const int at = slot0 + i / 4 * 16, first = j0 + at;
+          const uint32_t seen = seen4(word[r], mask ? first - base : 0, key1 - first) & ((1 << min(NZ, 4)) - 1);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) z[r][i][u] = (seen >> u) & 1 ? z[r][i][u] : -INFINITY;
-          if (seen & odd >> (16 * i + 4 * t)) add[r] = NAN;
+          for (int u = 0; u < min(NZ, 4); ++u) z[r][i + u] = (seen >> u) & 1 ? z[r][i + u] : -INFINITY;
+          if (seen & odd >> at) add[r] = NAN;
         }
       }
     }
@@ -317,9 +360,9 @@ struct Rows {
     bool behind = false;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      top[r] = z[r][0][0];
+      top[r] = z[r][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top[r] = fmaxf(top[r], z[r][i / 4][i % 4]);
+      for (int i = 1; i < NZ; ++i) top[r] = fmaxf(top[r], z[r][i]);
       behind |= (top[r] - m[r]) * c > kLag<F16>;
     }
     if (__any(behind)) {
@@ -329,7 +372,7 @@ struct Rows {
       held = __any(held);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float up = fmaxf(m[r], swap32_max(swap16_max(top[r])));
+        const float up = fmaxf(m[r], row_max<SP>(top[r]));
         const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
         if (held) {
           l[r] *= f;
@@ -354,23 +397,39 @@ struct Rows {
         const float from = m[r] == -INFINITY ? 0.f : m[r];
         sub[r] = static_cast<float>(unit - kTop<F16>);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[r][i / 4][i % 4] -= from;
+        for (int i = 0; i < NZ; ++i) z[r][i] -= from;
       }
     }
     // p s is rounded to the cache's type, as the products take it: relative to sum p s |d - 8|, as large an
     // error as that of rounding the output.  The sums of p and p y are of unrounded numbers.
     float sum[RT], lows[RT];                       // a step's, so that many small ones beside a large one count together
+    uint32_t own[RT][NZ / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 y = pairs(values, i / 2, i % 2);
+    for (int i = 0; i < NZ / 2; ++i) {
+      const float4 y = pairs(values, 2 * i);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2)], c, -sub[r]));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(z[r][i / 2][2 * (i % 2) + 1], c, -sub[r]));
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(z[r][2 * i], c, -sub[r]));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(z[r][2 * i + 1], c, -sub[r]));
         sum[r] = i == 0 ? p0 + p1 : sum[r] + (p0 + p1);
         lows[r] = fmaf(p0, y.y, i == 0 ? p1 * y.w : fmaf(p1, y.w, lows[r]));
-        w[r][i] = pack2<F16>(p0 * y.x, p1 * y.z);
-        lows[r] = plus_pair<F16>(w[r][i], -kMiddle<F16>, lows[r]);
+        own[r][i] = pack2<F16>(p0 * y.x, p1 * y.z);
+        lows[r] = plus_pair<F16>(own[r][i], -kMiddle<F16>, lows[r]);
+      }
+    }
+    // the products take a row's weights from its first lane
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+      for (int i = 0; i < NZ / 2; ++i) w[r][i] = own[r][i];
+      if constexpr (SP == 2) {
+        w[r][2] = along_row<0x100, 8>(own[r][0]);
+        w[r][3] = along_row<0x100, 8>(own[r][1]);
+      }
+      if constexpr (SP == 4) {
+        w[r][1] = along_row<0x100, 4>(own[r][0]);
+        w[r][2] = along_row<0x100, 8>(own[r][0]);
+        w[r][3] = along_row<0x100, 12>(own[r][0]);
       }
     }
 #pragma unroll
@@ -386,7 +445,7 @@ struct Rows {
   __device__ __forceinline__ void center() {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const float all = swap32_sum(swap16_sum(add[r]));
+      const float all = row_sum<SP>(add[r]);
 #pragma unroll
       for (int d = 0; d < NO; ++d) o[r][d] += all;
       add[r] = 0.f;
@@ -397,8 +456,8 @@ struct Rows {
   __device__ __forceinline__ void finish() {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      l[r] = swap32_sum(swap16_sum(l[r]));
-      add[r] = swap32_sum(swap16_sum(add[r]));
+      l[r] = row_sum<SP>(l[r]);
+      add[r] = row_sum<SP>(add[r]);
     }
   }
   template <int d>
@@ -409,13 +468,17 @@ struct Rows {
 
 // RT tiles of 16 rows a workgroup, KW wavefronts that take steps of 32 slots in turn, each from
 // registers that its loads filled in operand order.
-template <bool F16, int W, int RT, int KW>
+template <bool F16, int W, int RT, int KW, int SP>
 __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
-  using R = Rows<F16, W, RT, RT == 1>;
-  constexpr int M = 16 * RT, NF = R::NF, NO = R::NO, kStep = 32;
+  using R = Rows<F16, W, RT, RT == 1, SP>;
+  constexpr int M = RT * R::kRows, NF = R::NF, NO = R::NO, kStep = 32;
   constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides the one ahead
   constexpr int kOutRow = W + 4;
-  __shared__ __attribute__((aligned(16))) float acc[KW * M * kOutRow];
+  // Few rows: as much LDS as leaves a CU 1, 3 or 6 workgroups of 8, 4 or 2 wavefronts.  More of them at once only let short
+  // caches slow down long ones (64 caches of 16 to 8000 slots 51.4 us without this, 48.6 so; 128 of up to 4000 68.5, 63.6;
+  // 256 of up to 2000 56.8, 54.0), fewer of 2 leave gaps (256 of 512: 4 34.3, 6 29.5).
+  constexpr int kLeast = RT > 1 ? 0 : (KW == 8 ? 82 : KW == 4 ? 42 : 25) * 256, kSums = KW * M * kOutRow;
+  __shared__ __attribute__((aligned(16))) float acc[kSums > kLeast ? kSums : kLeast];
   __shared__ float stat[KW * M * 2], factor[KW * M];
   __shared__ int place[M];
   __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys, then values
@@ -541,6 +604,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int at = wave * M + 16 * r + x;
+    if (x >= R::kRows) continue;
     each_index<NO>([&](auto index) {
       constexpr int d = index;
       *reinterpret_cast<float4*>(acc + at * kOutRow + 16 * d + 4 * t) = rs.template elements<d>(r);
@@ -704,14 +768,24 @@ size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
   const dim3 grid((c.p.groups + 7) / 8 * 8 * c.p.tiles), threads(64 * c.waves);
+  const int rows = a.L * (a.H / a.Hkv);
+  auto few = [&](auto waves) {
+    constexpr int KW = waves;
+    if (rows <= 4)
+      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 4>), grid, threads, 0, s, a, c.p);
+    else if (rows <= 8)
+      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 2>), grid, threads, 0, s, a, c.p);
+    else
+      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 1>), grid, threads, 0, s, a, c.p);
+  };
   if (c.rows > 16)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4>), grid, threads, 0, s, a, c.p);
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4, 1>), grid, threads, 0, s, a, c.p);
   else if (c.waves == 8)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 8>), grid, threads, 0, s, a, c.p);
+    few(std::integral_constant<int, 8>{});
   else if (c.waves == 4)
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 4>), grid, threads, 0, s, a, c.p);
+    few(std::integral_constant<int, 4>{});
   else
-    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, 2>), grid, threads, 0, s, a, c.p);
+    few(std::integral_constant<int, 2>{});
 }
 
 }  // namespace

@@ -98,6 +98,16 @@ def test_single_tokens_of_every_plan(kw):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("mask", ["causal", "random", "hidden"])
+@pytest.mark.parametrize("L,G", [(1, 3), (4, 1), (2, 2), (5, 1), (8, 1), (3, 3), (16, 1), (17, 1)])
+def test_rows_of_every_tile(L, G, mask, dtype):
+    """Up to 4 rows, 8, 16 and more; blocks that end inside the 4 slots of a lane, and lengths shorter than the block."""
+    lens = [L, max(L - 1, 1), 33 + L, 64, 130]
+    c = Case4(brisk, 5, L, 2 * G, 2, 64, None, lens, mask=mask, dtype=dtype, seed=L)
+    c.check(*_run(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("L", [2, 20])
 def test_queries_that_are_not_finite(L, dtype):
     """A row's query of NaN or infinities stays out of the other rows (which may be rescaled at another step than
