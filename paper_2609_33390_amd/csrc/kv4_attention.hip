@@ -19,11 +19,11 @@
 // steps in turn and join through LDS.
 //
 // What bounds it.  Single tokens of a batch: the read of the cache (64 caches of 500 to 8000
-// slots of 8 heads, 300 MB in 54 us, 5.5 TB/s).  32 rows: vector and matrix instructions, which take
+// slots of 8 heads, 296 MB in 52 us, 5.7 TB/s).  32 rows: vector and matrix instructions, which take
 // turns on a SIMD whatever its wavefronts are: a step's 290 vector ones (56 make the keys' codes,
 // 56 the values', 32 take steps and lowest values to the logits, 104 make the weights and their sums)
 // keep it for 1215 cycles, its 32 products for 512, and a step takes 1725.
-// (One block of 32 over 65536 slots: 61 us, 0.57 PFLOP/s.)  So more wavefronts a SIMD
+// (One block of 32 over 65536 slots: 59 us, 0.58 PFLOP/s.)  So more wavefronts a SIMD
 // (3 with the queries in LDS) or codes two steps ahead change nothing, 64 rows a
 // wavefront make half as many codes but leave half as many tiles to share a batch's ends.
 // A wavefront's 800 instructions before and after its steps count as two or three of them.
@@ -176,8 +176,8 @@ __device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Pla
   // first runs of all sequences go first, then second ones, ...: later runs are fewer where lengths differ
   w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, bid / 8 % p.tiles};
   if (p.by_length) {
-    // Long runs first (single tokens of 64 caches of 500 to 8000 slots: 68 us in the order above, 54 so; blocks of 16 over
-    // 16 to 4096: 80, 67; for more caches than that the search costs what the order gains): the whole ones,
+    // Long runs first (single tokens of 64 caches of 500 to 8000 slots: 64 us in the order above, 53 so; blocks of 16 over
+    // 16 to 4096: 76, 67; for more caches than that the search costs what the order gains): the whole ones,
     // then the last ones of all sequences (at most 64, one a lane) by length, then what lies past them.
     const int runs = p.splits - p.own_first, nth = group / a.Hkv;
     const int len = lane < a.B ? kv4_len(a.kv, lane, a.max_seq_len) : 0;
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   };
   typedef uint32_t Codes __attribute__((ext_vector_type(W / 32)));
   // Chunk `lane` of a block's keys or values: a wavefront reads them in one piece, and one tile's rows are the only
-  // ones to read them (64 caches of 500 to 8000 keys: 60 us as ordinary loads, 54 so; 32 of 40 to 4000 with 32 heads: 56, 51).
+  // ones to read them (64 caches of 500 to 8000 keys: 58 us as ordinary loads, 53 so; 32 of 40 to 4000 with 32 heads: 56, 51).
   auto codes = [&](const uint8_t* blk) {
     const auto* at = reinterpret_cast<const Codes*>(blk + lane * static_cast<uint32_t>(sizeof(Codes)));
     if constexpr (RT == 1) return __builtin_nontemporal_load(at);
@@ -700,10 +700,10 @@ Shape many_rows(int keys, int B, int64_t whole, int rows) {
 // kStart and kStep for each of its steps; lengths may be all the same or anything up to the bound, and the
 // plan is for the mean of both.  Runs cost a second launch, the scratch (together at least kTwo a call, where one
 // launch takes kOne) and the partial sums.  So a batch is split when it does not fill the GPU,
-// and otherwise takes the wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52.6
-// us with 8 (71.6 with 4 and 134.9 with 2, in one round; 57.5 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 51.0
-// with 4 (60.9, 73.3), 128 of 600 18.2 with 2 (22.0 with 4, 25.6 with 8), 16 of 6000 22.1 in 2 runs with 8 (30.3 whole),
-// one of 1500 11.5 whole with 8 (12.5 in 6 runs or 12).
+// and otherwise takes the wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52 us
+// with 8 (68 with 4 and 123 with 2, in one round; 56 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 51 with 4 (60
+// with 8, 67 with 2), 128 of 600 17 with 2 (20 with 4, 25 with 8), 16 of 6000 22 in 2 runs with 8 (28 whole), one of 1500
+// 10.8 whole with 8 (12.2 to 13.9 in runs).
 Shape few_rows(int keys, int B, int64_t whole, int64_t rows, bool prefix) {
   constexpr double kStart = 3., kStep = 1.1, kOne = 9., kTwo = 12.5, kRow = 2 * 512 / 5e6;
   Shape best{16, 8, {}};
