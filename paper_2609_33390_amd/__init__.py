@@ -1187,7 +1187,7 @@ def kv4_read(cache: KVCache4, T: int, *, first: Optional[torch.Tensor] = None, k
     else:
         _dev_tensor(k, "k", dtype, shape=shape, device=dev)
     if v is None:
-        v = torch.empty(shape, dtype=dtype, device=dev)
+        v = torch.empty_like(k)
     else:
         _dev_tensor(v, "v", dtype, shape=shape, device=dev)
     st = lib().brisk_kv4_read(cache._ref, cache.B, T, _ptr(first), k.data_ptr(), v.data_ptr(), _stream_ptr(dev, stream))
