@@ -226,7 +226,9 @@ template <bool F16, int W, int RT, bool LEAN, int SP>
 struct Rows {
   static constexpr int NF = W / 32, NO = W / 16, NZ = 8 / SP, kRows = 16 / SP;
   static_assert(SP == 1 || RT == 1);
-  uint4 q[RT][NF];                                 // elements t W / 4 + ..., the second operand of K Q^T
+  static constexpr bool kHeld = RT < 4;            // queries in registers; else each wavefront brings a tile to LDS
+  uint4 q[kHeld ? RT : 1][NF];                     // elements t W / 4 + ..., the second operand of K Q^T
+  uint4* far;                                      // [RT][NF][64] in LDS
   float qz[RT];                                    // sum of q, as the logits are held
   uint64_t word[RT];                               // what a row sees of the block (one tile reads it where it is used)
   floatx4 o[RT][NO];
@@ -244,29 +246,33 @@ struct Rows {
   __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G]; }
 
   // The queries, which wait for nothing that the kernel reads first.
-  __device__ __forceinline__ void load(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int lane) {
+  __device__ __forceinline__ void load(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int lane, int wave, uint4* lds) {
     const int t = lane >> 4, x = lane & 15, G = a.H / a.Hkv;
     row0 = first_row;
     rows = n_rows;
     mask = a.mask;
+    far = lds;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int row = row0 + min(16 * r + x % kRows, rows - 1), bi = row / G;
+    for (int r = 0; r < RT; ++r) word[r] = !LEAN && mask ? mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G] : ~0ull;
+#pragma unroll
+    for (int r = 0; r < (kHeld ? RT : 1); ++r) {
+      const int row = row0 + min(16 * (kHeld ? r : wave) + x % kRows, rows - 1), bi = row / G;
       const uint16_t* src = a.q + bi * a.q_row_stride + (hk * G + row % G) * a.q_head_stride;
-      word[r] = !LEAN && mask ? mask[bi] : ~0ull;
 #pragma unroll
       for (int i = 0; i < NF; ++i) q[r][i] = *reinterpret_cast<const uint4*>(src + min(t * (W / 4) + 8 * i, a.D - 8));
     }
   }
 
-  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane) {
+  // (the same in all wavefronts of a workgroup where queries are in LDS)
+  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane, int wave) {
     const int t = lane >> 4, skip = (lane & 15) / kRows * NZ;
     slot0 = 16 * (skip / 4) + 4 * t + skip % 4;
     key1 = end;
     base = n - a.L;
     c = uniform(a.scale * kLog2e * (F16 ? 0x1p21f : 1.f));
+    float sums[kHeld ? RT : 1];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
+    for (int r = 0; r < (kHeld ? RT : 1); ++r) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NF; ++i) {
@@ -274,8 +280,21 @@ struct Rows {
 #pragma unroll
         for (int w = 0; w < 4; ++w) sum = plus_pair<F16>(part_of(q[r][i], w), 1.f, sum);
       }
-      sum = swap32_sum(swap16_sum(sum));           // (columns of one row agree)
-      qz[r] = F16 ? sum * 0x1p-21f : sum;
+      sum = swap32_sum(swap16_sum(sum));
+      sums[r] = F16 ? sum * 0x1p-21f : sum;
+    }
+    if constexpr (!kHeld) {
+      float* const all = reinterpret_cast<float*>(far + RT * NF * 64);
+#pragma unroll
+      for (int i = 0; i < NF; ++i) far[(wave * NF + i) * 64 + lane] = q[0][i];
+      if (t == 0) all[16 * wave + lane] = sums[0];
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < RT; ++r) qz[r] = all[16 * r + (lane & 15)];
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if constexpr (kHeld) qz[r] = sums[r];
       m[r] = -INFINITY;
       mc[r] = l[r] = add[r] = 0.f;
 #pragma unroll
@@ -470,15 +489,16 @@ struct Rows {
 // registers that its loads filled in operand order.
 template <bool F16, int W, int RT, int KW, int SP>
 __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend_kernel(Kv4AttentionArgs a, Kv4Plan p) {
-  using R = Rows<F16, W, RT, RT == 1, SP>;
+  using R = Rows<F16, W, RT, RT != 2, SP>;
   constexpr int M = RT * R::kRows, NF = R::NF, NO = R::NO, kStep = 32;
   constexpr int kLooked = 31;                      // steps whose pages are looked up at once, besides the one ahead
-  constexpr int kOutRow = W + 4;
+  constexpr int kPart = RT < 4 ? W : W / 4, kOutRow = kPart + 4;     // elements joined at once
   // Few rows: as much LDS as leaves a CU 1, 3 or 6 workgroups of 8, 4 or 2 wavefronts.  More of them at once only let short
   // caches slow down long ones (64 caches of 16 to 8000 slots 51.4 us without this, 48.6 so; 128 of up to 4000 68.5, 63.6;
   // 256 of up to 2000 56.8, 54.0), fewer of 2 leave gaps (256 of 512: 4 34.3, 6 29.5).
   constexpr int kLeast = RT > 1 ? 0 : (KW == 8 ? 82 : KW == 4 ? 42 : 25) * 256, kSums = KW * M * kOutRow;
   __shared__ __attribute__((aligned(16))) float acc[kSums > kLeast ? kSums : kLeast];
+  __shared__ __attribute__((aligned(16))) uint4 queries[R::kHeld ? 1 : RT * NF * 64 + RT * 4];
   __shared__ float stat[KW * M * 2], factor[KW * M];
   __shared__ int place[M];
   __shared__ __attribute__((aligned(16))) float2 marks[KW * 64];     // (step, lowest) of a step's keys, then values
@@ -499,7 +519,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   int held = pages_of(0);
   const int row0 = w.b * a.L * G + w.tile * M, rows = min(M, a.L * G - w.tile * M);
   R rs;
-  rs.load(a, w.hk, row0, rows, lane);
+  rs.load(a, w.hk, row0, rows, lane, wave, queries);
   const int n = kv4_len(a.kv, w.b, a.max_seq_len), key1 = min(n, key0 + p.run);
   if (key0 >= n && p.part) return leave_empty(a, p, w, row0, rows);
 
@@ -529,36 +549,36 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   const CodeBits<F16> bits;
 
   const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
-  if (steps == 0) rs.begin(a, n, key1, lane);
-  if (steps > 0) {
-    const uint8_t *b0 = block(0, 0, 0), *b1 = block(0, 0, 1);
-    Codes k[2], v[2];
-    k[0] = codes(b0);
-    k[1] = codes(b1);
-    uint32_t mark = mark_of(b0, b1);
-    __builtin_amdgcn_sched_barrier(0);             // in the order in which the loop has them on their way
-    v[0] = codes(b0 + 8 * W);
-    v[1] = codes(b1 + 8 * W);
-    __builtin_amdgcn_sched_barrier(0);
-    rs.begin(a, n, key1, lane);
-    for (int step0 = 0; step0 < steps; step0 += kLooked) {
-      const int end = min(steps - step0, kLooked);
-      for (int nth = 0; nth < end; ++nth) {
-        const int step = step0 + nth, j0 = my0 + kStep * KW * step;
-        // ---- steps and lowest values: one slot a lane, handed round through LDS
-        float st = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
-        uint32_t odd = 0;
-        if (rs.cut(j0)) {
-          const bool past = j0 + (lane & 31) >= key1;                     // what lies past the run may be anything
-          const bool finite = fabsf(st) < INFINITY && fabsf(y) < INFINITY;
-          odd = static_cast<uint32_t>(__ballot(!past && !finite) >> 32);
-          if (past || (lane & 32 && !finite)) st = y = 0.f;
-        }
-        my_marks[lane] = make_float2(st, fmaf(middle, st, y));
-        asm volatile("" ::: "memory");             // LDS works in order for a wavefront; so must the compiler
-        __builtin_amdgcn_wave_barrier();
-        // ---- S^T = K Q^T over the codes
-        floatx4 z[RT][2];
+  // (of a wavefront without steps: of slots that are there to be read, and not used)
+  const uint8_t *b0 = block(0, 0, 0), *b1 = block(0, 0, 1);
+  Codes k[2], v[2];
+  k[0] = codes(b0);
+  k[1] = codes(b1);
+  uint32_t mark = mark_of(b0, b1);
+  __builtin_amdgcn_sched_barrier(0);             // in the order in which the loop has them on their way
+  v[0] = codes(b0 + 8 * W);
+  v[1] = codes(b1 + 8 * W);
+  __builtin_amdgcn_sched_barrier(0);
+  rs.begin(a, n, key1, lane, wave);
+  for (int step0 = 0; step0 < steps; step0 += kLooked) {
+    const int end = min(steps - step0, kLooked);
+    for (int nth = 0; nth < end; ++nth) {
+      const int step = step0 + nth, j0 = my0 + kStep * KW * step;
+      // ---- steps and lowest values: one slot a lane, handed round through LDS
+      float st = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
+      uint32_t odd = 0;
+      if (rs.cut(j0)) {
+        const bool past = j0 + (lane & 31) >= key1;                     // what lies past the run may be anything
+        const bool finite = fabsf(st) < INFINITY && fabsf(y) < INFINITY;
+        odd = static_cast<uint32_t>(__ballot(!past && !finite) >> 32);
+        if (past || (lane & 32 && !finite)) st = y = 0.f;
+      }
+      my_marks[lane] = make_float2(st, fmaf(middle, st, y));
+      asm volatile("" ::: "memory");             // LDS works in order for a wavefront; so must the compiler
+      __builtin_amdgcn_wave_barrier();
+      // ---- S^T = K Q^T over the codes
+      floatx4 z[RT][2];
+      if constexpr (R::kHeld) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -567,53 +587,78 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
 #pragma unroll
             for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, rs.q[r][f], f == 0 ? floatx4{} : z[r][i]);
           }
-        rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
-        // ---- the next step's keys
-        b0 = block(nth + 1, step + 1, 0);
-        b1 = block(nth + 1, step + 1, 1);
-        k[0] = codes(b0);
-        k[1] = codes(b1);
-        mark = mark_of(b0, b1);
-        __builtin_amdgcn_sched_barrier(0);
-        uint32_t wt[RT][4];
-        rs.weigh(z, my_marks, my_marks + 32, odd, j0, lane, G, wt);
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        // ---- out^T += D^T W^T over the codes
-        each_index<NO>([&](auto index) {
-          constexpr int d = index, u = 2 * (d / 4), j = d % 4;
-          const uint4 f = make_uint4(value_codes<F16, j>(v[0][u], bits), value_codes<F16, j>(v[0][u + 1], bits),
-                                     value_codes<F16, j>(v[1][u], bits), value_codes<F16, j>(v[1][u + 1], bits));
+      } else {
 #pragma unroll
-          for (int r = 0; r < RT; ++r) rs.o[r][d] = mfma16<F16>(f, make_uint4(wt[r][0], wt[r][1], wt[r][2], wt[r][3]), rs.o[r][d]);
-        });
-        v[0] = codes(b0 + 8 * W);
-        v[1] = codes(b1 + 8 * W);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int f = 0; f < NF; ++f) {
+          asm volatile("" ::: "memory");         // queries from LDS no sooner than they are needed
+          uint4 qf[RT];
+#pragma unroll
+          for (int r = 0; r < RT; ++r) qf[r] = queries[(r * NF + f) * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 kf = key_codes<F16>(k[i][f], bits);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) z[r][i] = mfma16<F16>(kf, qf[r], f == 0 ? floatx4{} : z[r][i]);
+          }
+        }
       }
-      if (step0 + kLooked < steps) {
-        held = pages_of(step0 + kLooked);
-        rs.center();
-        asm volatile("" : "+v"(held));             // waited for here: in the loop each step's codes would be waited for with it
-      }
+      rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
+      // ---- the next step's keys
+      b0 = block(nth + 1, step + 1, 0);
+      b1 = block(nth + 1, step + 1, 1);
+      k[0] = codes(b0);
+      k[1] = codes(b1);
+      mark = mark_of(b0, b1);
+      __builtin_amdgcn_sched_barrier(0);
+      uint32_t wt[RT][4];
+      rs.weigh(z, my_marks, my_marks + 32, odd, j0, lane, G, wt);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+      // ---- out^T += D^T W^T over the codes
+      each_index<NO>([&](auto index) {
+        constexpr int d = index, u = 2 * (d / 4), j = d % 4;
+        const uint4 f = make_uint4(value_codes<F16, j>(v[0][u], bits), value_codes<F16, j>(v[0][u + 1], bits),
+                                   value_codes<F16, j>(v[1][u], bits), value_codes<F16, j>(v[1][u + 1], bits));
+#pragma unroll
+        for (int r = 0; r < RT; ++r) rs.o[r][d] = mfma16<F16>(f, make_uint4(wt[r][0], wt[r][1], wt[r][2], wt[r][3]), rs.o[r][d]);
+      });
+      v[0] = codes(b0 + 8 * W);
+      v[1] = codes(b1 + 8 * W);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (step0 + kLooked < steps) {
+      held = pages_of(step0 + kLooked);
+      rs.center();
+      asm volatile("" : "+v"(held));             // waited for here: in the loop each step's codes would be waited for with it
     }
   }
 
   // ---- join the wavefronts and write
+  if constexpr (!R::kHeld) {                       // or what is joined would be made in the loop, and kept
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int d = 0; d < NO; ++d) asm volatile("" : "+v"(rs.o[r][d]));
+  }
   rs.finish();
+  auto put = [&](auto from) {                      // elements from .. + kPart
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+      if (x < R::kRows)
+        each_index<kPart / 16>([&](auto index) {
+          constexpr int d = from / 16 + index;
+          *reinterpret_cast<float4*>(acc + (wave * M + 16 * r + x) * kOutRow + 16 * index + 4 * t) = rs.template elements<d>(r);
+        });
+  };
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int at = wave * M + 16 * r + x;
-    if (x >= R::kRows) continue;
-    each_index<NO>([&](auto index) {
-      constexpr int d = index;
-      *reinterpret_cast<float4*>(acc + at * kOutRow + 16 * d + 4 * t) = rs.template elements<d>(r);
-    });
-    if (t == 0) {
+    if (x < R::kRows && t == 0) {
       stat[at * 2] = rs.l[r] == 0.f ? -INFINITY : rs.mc[r];
       stat[at * 2 + 1] = rs.l[r];
     }
   }
+  put(std::integral_constant<int, 0>{});
   __syncthreads();
   if (tid < rows) {                                // what the wavefronts' sums of a row are times
     float top = -INFINITY, total = 0.f, f[KW];
@@ -638,26 +683,36 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
       a.lse[out] = lse;
   }
   __syncthreads();
-  for (int i = tid; i < rows * (W / 4); i += 64 * KW) {
-    const int r = i / (W / 4), e = i % (W / 4) * 4;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int v = 0; v < KW; ++v) {
-      const float f = factor[r * KW + v];
-      const float4 y = *reinterpret_cast<const float4*>(acc + (v * M + r) * kOutRow + e);
-      sum.x += f * y.x;
-      sum.y += f * y.y;
-      sum.z += f * y.z;
-      sum.w += f * y.w;
+  auto join = [&](int e0) {
+    for (int i = tid; i < rows * (kPart / 4); i += 64 * KW) {
+      const int r = i / (kPart / 4), e = i % (kPart / 4) * 4;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  #pragma unroll
+      for (int v = 0; v < KW; ++v) {
+        const float f = factor[r * KW + v];
+        const float4 y = *reinterpret_cast<const float4*>(acc + (v * M + r) * kOutRow + e);
+        sum.x += f * y.x;
+        sum.y += f * y.y;
+        sum.z += f * y.z;
+        sum.w += f * y.w;
+      }
+      if (e0 + e < a.D) {
+        const int64_t to = static_cast<int64_t>(place[r]) * a.D + e0 + e;
+        if (p.part)
+          *reinterpret_cast<float4*>(p.part + to) = sum;
+        else
+          *reinterpret_cast<uint2*>(a.out + to) = make_uint2(pack2<F16>(sum.x, sum.y), pack2<F16>(sum.z, sum.w));
+      }
     }
-    if (e < a.D) {
-      const int64_t to = static_cast<int64_t>(place[r]) * a.D + e;
-      if (p.part)
-        *reinterpret_cast<float4*>(p.part + to) = sum;
-      else
-        *reinterpret_cast<uint2*>(a.out + to) = make_uint2(pack2<F16>(sum.x, sum.y), pack2<F16>(sum.z, sum.w));
-    }
-  }
+  };
+  join(0);
+  if constexpr (kPart < W)
+    each_index<W / kPart - 1>([&](auto index) {
+      __syncthreads();
+      put(std::integral_constant<int, (index + 1) * kPart>{});
+      __syncthreads();
+      join((index + 1) * kPart);
+    });
 }
 
 // A launch's workgroups: rows of a tile, wavefronts, and the runs of the own keys.
@@ -670,28 +725,37 @@ constexpr int kHeld = 2 * 4 * kCUs;                // wavefronts that the GPU wo
 // Whether a launch's workgroups go by length: those of more than a round, and lengths that a wavefront has at hand.
 bool by_length(int B, double rounds) { return B > 1 && B <= 64 && rounds > 1; }
 
-// More than 16 rows.  A workgroup's start, its join and the partial sums of its rows, written and read
-// again, count as `start` keys.  One sequence's runs are of one length, and take rounds of workgroups.
-// Sequences differ in lengths that are not known here: the last workgroup to end then has at most a run
-// more than its share of all, and about a third of one where long runs go first.  (64 blocks of 16 over 16 to 4096
-// slots: 1 run 65 us, 2 runs 78; one of 32 over 65536: 12 runs 75, 16 61, 24 64; 13 of 21 over 5 to 1777: 46, 39, 42 in
-// 1, 2 and 3 runs.)
-Shape many_rows(int keys, int B, int64_t whole, int rows) {
-  constexpr int kKeys = 128;
-  const double start = 650. + 24. * rows;
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+
+// More than 16 rows: tiles of 32 or 64, by what a plan would take in us.  A round of workgroups takes `start` and `step` for
+// each of its steps of 128 slots; a batch's lengths may be all the same or, as likely again, anything up to the
+// bound.  Tiles of 64 make the codes half as often, but take longer to start and join, and leave fewer workgroups to
+// even out lengths with.  (One block of 32 with 4 heads a key head over 65568 slots: 57 us with 64, 67 with 32; 8 of
+// them over 8192: 55, 62; one of 64 with 8 heads over 32768: 56, 62; 64 of 16 over 16 to 4096: 76, 68; 13 of 21 with 5 over 5 to
+// 1777: 44, 40.)
+Shape many_rows(int keys, int B, int64_t whole, int rows, int64_t all_rows, bool prefix) {
+  constexpr double kTwo = 4., kRow = 2e-4;
   Shape best{32, 4, {}};
   double least = 1e300;
-  for (int s = 1; s <= 64; ++s) {
-    const int run = (keys + s * kKeys - 1) / (s * kKeys) * kKeys, count = (keys + run - 1) / run;
-    if (s > 1 && whole * count > kMostRuns) break;
-    const double rounds = static_cast<double>(whole * count) * 4 / kHeld;
-    const double cost = (count > 1 ? 128. : 0.) + (B == 1 ? std::ceil(rounds) * (run + start)
-                                                          : run * (by_length(B, rounds) ? 0.35 : 1.) + start * std::max(1., rounds));
-    if (cost < least) {
-      least = cost;
-      best.runs = {count, run};
+  for (int tile : {32, 64}) {
+    if (tile > 32 && rows <= 32) break;
+    const double step = tile > 32 ? 2.45 : 1.6, start = tile > 32 ? 11. : 6.;
+    const int64_t groups = whole * ceil_div(rows, tile);
+    for (int s : kSplits) {
+      const int run = (keys + s * 128 - 1) / (s * 128) * 128, count = (keys + run - 1) / run;
+      if (s > 1 && groups * count > kMostRuns) break;
+      const double steps = run / 128 * step, rounds = static_cast<double>(groups * count) * 4 / kHeld;
+      const double same = std::max(1., B > 1 && rounds > 2 ? rounds : std::ceil(rounds)) * (steps + start);
+      const double total = rounds * (steps / 2 + start), longest = steps + start;
+      const double other = by_length(B, rounds) || rounds <= 1 ? std::max(longest, total) : total + steps / 2;
+      const double cost = (B > 1 ? (same + 2 * other) / 3 : same) + (count > 1 || prefix ? kTwo + kRow * all_rows * count : 0.);
+      if (cost < least) {
+        least = cost;
+        best.rows = tile;
+        best.runs = {count, run};
+      }
+      if (run == 128) break;                       // no shorter ones
     }
-    if (run == kKeys) break;                       // no shorter ones
   }
   return best;
 }
@@ -710,7 +774,7 @@ Shape few_rows(int keys, int B, int64_t whole, int64_t rows, bool prefix) {
   double least = 1e300;
   for (int waves : {2, 4, 8}) {
     const int step = 32 * waves;
-    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+    for (int s : kSplits) {
       const int run = (keys + s * step - 1) / (s * step) * step, count = (keys + run - 1) / run;
       if (s > 1 && whole * count > kMostRuns) break;
       const double steps = run / step * kStep, rounds = static_cast<double>(whole * count) * waves / kHeld;
@@ -744,9 +808,9 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int prefix_len, int max_seq_len
   if (max_seq_len > 0 || prefix_len == 0) {
     const int rows = L * (H / Hkv), keys = std::max(max_seq_len, 1);
     const int64_t whole = static_cast<int64_t>(B) * Hkv;
-    c.p.tiles = rows > 16 ? ceil_div(rows, 32) : 1;
-    const Shape s = rows > 16 ? many_rows(keys, B, whole * c.p.tiles, std::min(rows, 32))
-                              : few_rows(keys, B, whole, static_cast<int64_t>(B) * L * H, prefix_len > 0);
+    const int64_t all_rows = static_cast<int64_t>(B) * L * H;
+    const Shape s = rows > 16 ? many_rows(keys, B, whole, rows, all_rows, prefix_len > 0) : few_rows(keys, B, whole, all_rows, prefix_len > 0);
+    c.p.tiles = ceil_div(rows, s.rows);
     c.rows = s.rows;
     c.waves = s.waves;
     c.p.run = s.runs.keys;
@@ -778,7 +842,9 @@ void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
     else
       hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 1>), grid, threads, 0, s, a, c.p);
   };
-  if (c.rows > 16)
+  if (c.rows > 32)
+    hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 4, 4, 1>), grid, threads, 0, s, a, c.p);
+  else if (c.rows > 16)
     hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 2, 4, 1>), grid, threads, 0, s, a, c.p);
   else if (c.waves == 8)
     few(std::integral_constant<int, 8>{});

@@ -107,6 +107,22 @@ def test_rows_of_every_tile(L, G, mask, dtype):
     c.check(*_run(c))
 
 
+@pytest.mark.parametrize("kw", [
+    # enough blocks to fill the GPU with tiles of 64 rows: one tile, inside it and full, two, with values of one and of two words
+    dict(B=64, L=40, H=8, D=24, mask="causal"),
+    dict(B=64, L=33, H=8, D=72, mask="hidden", dtype="f16"),
+    dict(B=64, L=64, H=8, D=8, mask="random", dtype="f16"),
+    dict(B=32, L=40, H=16, D=40, mask="mixed", prefix=33),
+    dict(B=32, L=33, H=16, D=104, mask="random"),
+], ids=str)
+def test_tiles_of_64_rows(kw):
+    kw = dict(kw)
+    B, L, H, D, prefix = (kw.pop(n, None) for n in ("B", "L", "H", "D", "prefix"))
+    lens = [(0, 1, L - 1, L, L + 1, 63, 64, 65, 128, 129, 256)[b % 11] for b in range(B)]
+    c = Case4(brisk, B, L, H, 8, D, prefix, lens, seed=B + L, **kw)
+    c.check(*_run(c))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("L", [2, 20])
 def test_queries_that_are_not_finite(L, dtype):
