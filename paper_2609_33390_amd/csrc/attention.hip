@@ -92,14 +92,14 @@ __global__ __launch_bounds__(64 * RW * KW, RW >= 2 ? 2 : 1) void attend_kernel(A
   const int half = lane >> 5, col = lane & 31;
   const int G = a.H / a.Hkv;
 
-  // ---- which rows and keys: the row tiles of a group follow each other on one XCD
+  // ---- which rows and keys
   int bid = blockIdx.x;
-  const int pre_grid = (p.pre_groups + 7) / 8 * 8 * p.pre_tiles;
+  const int pre_grid = tile_grid(p.pre_groups, p.pre_tiles);
   const bool own = bid >= pre_grid;
   if (own) bid -= pre_grid;
-  const int tiles = own ? p.own_tiles : p.pre_tiles;
-  const int group = bid / 8 / tiles * 8 + bid % 8, tile = bid / 8 % tiles;
-  if (group >= (own ? p.own_groups : p.pre_groups)) return;
+  const int groups = own ? p.own_groups : p.pre_groups;
+  const auto [group, tile] = group_tile(bid, groups, own ? p.own_tiles : p.pre_tiles);
+  if (group >= groups) return;
   int b = 0, hk, split, key0, key1, row0, rows;
   const int held = rw * NI * RPI + held_key<RB>(lane);  // the key of a tile whose place this lane works out
   int page = 0;                                  // page id of the held key, a tile ahead
@@ -556,7 +556,7 @@ CallPlan make_plan(int B, int L, int H, int Hkv, int D, int prefix_len, int max_
 
 template <bool F16, int ND>
 void launch_shape(int shape, const AttentionArgs& a, const AttnPlan& p, hipStream_t s) {
-  const dim3 grid((p.pre_groups + 7) / 8 * 8 * p.pre_tiles + (p.own_groups + 7) / 8 * 8 * p.own_tiles);
+  const dim3 grid(tile_grid(p.pre_groups, p.pre_tiles) + tile_grid(p.own_groups, p.own_tiles));
   switch (shape) {
     case 0: hipLaunchKernelGGL((attend_kernel<F16, ND, 1, 2, 1>), grid, dim3(128), 0, s, a, p); break;
     case 1: hipLaunchKernelGGL((attend_kernel<F16, ND, 2, 2, 1>), grid, dim3(256), 0, s, a, p); break;

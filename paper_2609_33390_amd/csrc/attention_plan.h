@@ -1,6 +1,7 @@
 // How the keys of an attention call are split over the GPU.
 #pragma once
 
+#include <hip/hip_runtime.h>
 #include <stdint.h>
 
 namespace brisk {
@@ -29,6 +30,17 @@ inline Runs runs_of(int keys, int64_t whole, int step, int slots) {
     }
   }
   return best;
+}
+
+// Workgroups of a launch, and which one has which row tile of which group (a workgroup without one gets a group past the
+// last): tiles of a group follow each other on one XCD (workgroups take turns on the 8 of them), whose cache then has
+// its keys; but fewer groups than XCDs spread over all.  (253 blocks of 16 with 16 heads of 64 over one key head, 269 slots of
+// prefix and up to 20 own ones in 4 bits: 123 us on one XCD, 58 so.)
+__host__ __device__ constexpr int tile_grid(int groups, int tiles) { return (groups < 8 ? groups : (groups + 7) / 8 * 8) * tiles; }
+struct GroupTile { int group, tile; };
+__host__ __device__ constexpr GroupTile group_tile(int bid, int groups, int tiles) {
+  if (groups < 8) return {bid % groups, bid / groups};
+  return {bid / 8 / tiles * 8 + bid % 8, bid / 8 % tiles};
 }
 
 }  // namespace brisk

@@ -166,15 +166,15 @@ __device__ __forceinline__ int sum_before(int v, int lane) {
   return sum - v;
 }
 
-// Which rows and slots a workgroup has: row tiles of a group follow each other on one XCD.
+// Which rows and slots a workgroup has.
 struct Place {
   int hk, b, split, tile;
 };
 __device__ __forceinline__ bool place_of(const Kv4AttentionArgs& a, const Kv4Plan& p, int lane, Place& w) {
-  const int bid = blockIdx.x, group = bid / 8 / p.tiles * 8 + bid % 8;
+  const auto [group, tile] = group_tile(blockIdx.x, p.groups, p.tiles);
   if (group >= p.groups) return false;
   // first runs of all sequences go first, then second ones, ...: later runs are fewer where lengths differ
-  w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, bid / 8 % p.tiles};
+  w = {group % a.Hkv, group / a.Hkv % a.B, group / a.Hkv / a.B, tile};
   if (p.by_length) {
     // Long runs first (single tokens of 64 caches of 500 to 8000 slots: 64 us in the order above, 53 so; blocks of 16 over
     // 16 to 4096: 76, 67; for more caches than that the search costs what the order gains): the whole ones,
@@ -831,7 +831,7 @@ size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
 
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
-  const dim3 grid((c.p.groups + 7) / 8 * 8 * c.p.tiles), threads(64 * c.waves);
+  const dim3 grid(tile_grid(c.p.groups, c.p.tiles)), threads(64 * c.waves);
   const int rows = a.L * (a.H / a.Hkv);
   auto few = [&](auto waves) {
     constexpr int KW = waves;
