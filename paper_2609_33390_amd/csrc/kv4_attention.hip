@@ -23,9 +23,9 @@
 // turns on a SIMD whatever its wavefronts are: a step's 290 vector ones (56 make the keys' codes,
 // 56 the values', 32 take steps and lowest values to the logits, 104 make the weights and their sums)
 // keep it for 1215 cycles, its 32 products for 512, and a step takes 1725.
-// (One block of 32 over 65536 slots: 59 us, 0.58 PFLOP/s.)  So more wavefronts a SIMD
-// (3 with the queries in LDS) or codes two steps ahead change nothing, 64 rows a
-// wavefront make half as many codes but leave half as many tiles to share a batch's ends.
+// So more wavefronts a SIMD (3 with the queries in LDS) or codes two steps ahead change nothing, and 64 rows a wavefront,
+// which make the codes once for twice as many, take 2.45 us a step where 32 take 1.6 (two wavefronts a SIMD).
+// (One block of 32 over 65536 slots: 55 us, 0.62 PFLOP/s.)
 // A wavefront's 800 instructions before and after its steps count as two or three of them.
 #include <algorithm>
 #include <cmath>
@@ -39,7 +39,6 @@ namespace brisk {
 
 namespace {
 
-constexpr int kCUs = 256;
 // As in the attention over 2-byte caches: the subtracted logit may be kLag behind the maximum (in base
 // 2).  Weights are further divided by 2^unit, the same for all rows of a wavefront, which the
 // sum of the probabilities shares: in f16 the largest step seen, so that f16's range is used from
