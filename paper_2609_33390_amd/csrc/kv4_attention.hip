@@ -766,9 +766,9 @@ Shape many_rows(int keys, int B, int64_t whole, int rows, int64_t all_rows, bool
 // and otherwise takes the wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52 us
 // with 8 (68 with 4 and 123 with 2, in one round; 56 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 51 with 4 (60
 // with 8, 67 with 2), 128 of 600 17 with 2 (20 with 4, 25 with 8), 16 of 6000 22 in 2 runs with 8 (28 whole), one of 1500
-// 10.8 whole with 8 (12.2 to 13.9 in runs).
+// 10.8 whole with 8 (12.2 to 13.9 in runs), 4 of 32768 27 in 8 runs with 8 (33 in 16, 41 in 4).
 Shape few_rows(int keys, int B, int64_t whole, int64_t rows, bool prefix) {
-  constexpr double kStart = 3., kStep = 1.1, kOne = 9., kTwo = 12.5, kRow = 2 * 512 / 5e6;
+  constexpr double kStart = 4.3, kStep = 1.1, kOne = 9., kTwo = 12.5, kRow = 2 * 512 / 5e6;
   Shape best{16, 8, {}};
   double least = 1e300;
   for (int waves : {2, 4, 8}) {
