@@ -320,7 +320,12 @@ int blocks_of(int T) { return (T + 2 * kKv4Block - 2) / kKv4Block; }
 
 }  // namespace
 
-bool kv4_launchable(int B, int Hkv, int T) { return static_cast<int64_t>(B) * Hkv * blocks_of(T) < (int64_t{1} << 25); }
+// (A step at a time: the three sizes together may pass 64 bits.)
+bool kv4_launchable(int B, int Hkv, int T) {
+  constexpr int64_t kMost = 1 << 25;
+  const int64_t heads = static_cast<int64_t>(B) * Hkv;
+  return heads < kMost && heads * blocks_of(T) < kMost;
+}
 
 template <class Args, class Fn>
 static void launch_blocks(const Args& a, Fn kernel, hipStream_t s) {
