@@ -60,9 +60,11 @@ __device__ __forceinline__ float poisoned(uint32_t pair, float acc) {
 // How a head is held.  The quotient t / s is taken as t (1 / s) with the reciprocal in two parts,
 // good to 2^-46: rounded to 32 bits that is a tie between two codes only where the quotient
 // is one, since t has 24 bits and s at most 11 (a quotient that is none is at least 2^-24 of
-// itself away from one, and 2^-35 of itself past the middle of its rounding).
+// itself away from one, and 2^-35 of itself past the middle of its rounding).  Past s = 2^103, which
+// bf16 has, the second part would be a subnormal number and short of bits: beyond 2^64 both t and s are taken 2^-64 times,
+// which changes neither t's rounding nor the quotient.
 struct Scheme {
-  float low, inv, inv_rest;
+  float low, unit, inv, inv_rest;                  // low: -z, times the unit
   uint32_t pair;
 };
 
@@ -77,8 +79,10 @@ __device__ __forceinline__ Scheme scheme_of(float lowest, float highest, float p
   const uint32_t low = bad ? (F16 ? 0x7E00u : 0x7FC0u) : f32_to_half<F16>(lowest);
   if (bad) step = 0;
   h.pair = step | low << 16;
-  const float s = half_to_f32<F16>(step);
-  h.low = lowest;
+  float s = half_to_f32<F16>(step);
+  h.unit = !F16 && s > 0x1p64f ? 0x1p-64f : 1.f;
+  s *= h.unit;
+  h.low = -lowest * h.unit;
   h.inv = step ? 1.f / s : 0.f;
   h.inv_rest = fmaf(-s, h.inv, step ? 1.f : 0.f) * h.inv;
   return h;
@@ -88,7 +92,7 @@ __device__ __forceinline__ Scheme scheme_of(float lowest, float highest, float p
 // a fifteenth of the range, so only a subnormal one, which f16 may have, can give more than 15.
 template <bool F16>
 __device__ __forceinline__ float code_of(float x, const Scheme& h) {
-  const float t = x - h.low, y = fmaf(t, h.inv, t * h.inv_rest);
+  const float t = F16 ? x + h.low : fmaf(x, h.unit, h.low), y = fmaf(t, h.inv, t * h.inv_rest);
   return __builtin_rintf(F16 ? fminf(y, 15.f) : y);
 }
 
