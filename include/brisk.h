@@ -721,7 +721,8 @@ int brisk_kv4_attention_workspace_size(int32_t B, int32_t L, int32_t n_heads, in
  * masks, empty rows, hidden slots and the roundings of the results are those of
  * brisk_block_attention (weights are rounded to the cache's type where they meet
  * the codes; a weight counts by how far a value lies from the middle of its head's
- * range).
+ * range; in f16 a weight times a value's step is off besides by at most 2^-36 of the
+ * row's largest weight times the largest step that it sees).
  *
  * Limits as there, with B * L * n_heads <= 2^22.  A logit is made of s times
  * products with codes and of z times the query's sum: (31 s + |z|) sum_d |q_d| must

@@ -40,10 +40,10 @@ namespace brisk {
 namespace {
 
 // As in the attention over 2-byte caches: the subtracted logit may be kLag behind the maximum (in base
-// 2).  Weights are further divided by 2^unit, the same for all rows of a wavefront, which the
-// sum of the probabilities shares: in f16 the largest step seen, so that f16's range is used from
-// the top (times 2^12, so at most 2^15); in bf16 only what keeps steps past 2^60 from
-// overflowing sums.
+// 2).  A row's weights are further divided by 2^unit, which the sum of the probabilities shares: in f16 the
+// largest step of the values that it sees, so that f16's range is used from the top (times 2^12, so at most 2^15,
+// and a weight times a step is off by at most 2^-36 of the largest step besides its rounding); in bf16 only what
+// keeps steps past 2^60 from overflowing sums.
 template <bool F16> constexpr float kLag = F16 ? 3.f : 8.f;
 template <bool F16> constexpr int kTop = F16 ? 12 : 0;
 template <bool F16> constexpr int kLeastUnit = F16 ? -24 : 0;
@@ -138,6 +138,14 @@ __device__ __forceinline__ uint32_t along_row(uint32_t v) {
 }
 template <int N> __device__ __forceinline__ float round_row(float v) { return __uint_as_float(along_row<0x120, N>(__float_as_uint(v))); }
 
+// v, and what is made of it made where it is used: four tiles' registers are not enough to hold it over the loop, and a
+// reload of what spilled waits for the codes on their way.
+template <bool SHORT>
+__device__ __forceinline__ int anew(int v) {
+  if constexpr (SHORT) asm volatile("" : "+v"(v));
+  return v;
+}
+
 // Over the lanes that share a row: the four quarters and, of a row on SP lanes of each, those.
 template <int SP>
 __device__ __forceinline__ float row_sum(float v) {
@@ -229,20 +237,24 @@ struct Rows {
   uint4 q[kHeld ? RT : 1][NF];                     // elements t W / 4 + ..., the second operand of K Q^T
   uint4* far;                                      // [RT][NF][64] in LDS
   float qz[RT];                                    // sum of q, as the logits are held
-  uint64_t word[RT];                               // what a row sees of the block (one tile reads it where it is used)
+  uint64_t word[LEAN ? 1 : RT];                    // what a row sees of the block
   floatx4 o[RT][NO];
   // m: the subtracted logit (unscaled); mc = c m - lift, lift = kTop - unit; l: this lane's part of the
   // sum of the weights; add: its part of what joins every element of the output
   float m[RT], mc[RT], l[RT], add[RT];
-  int unit;
-  float limit;                                     // of a value's size within that unit
+  float* units;                                    // [RT][kRows] in LDS: they are wanted where sizes or maxima grow
+  float limit;                                     // of a value's size within all rows' units (the same in all lanes)
   bool wide;                                       // a row's mc is past kFine (the same in all lanes)
   float c;                                         // f16 logits are held 2^-21 of what they are
   int key1, base, row0, rows;                      // end of the run, begin of the block, the wavefront's rows
   const uint64_t* mask;
   int slot0;                                       // first of a step's slots whose weights this lane takes
 
-  __device__ __forceinline__ uint64_t sees(int r, int x, int G) const { return mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G]; }
+  __device__ __forceinline__ uint64_t sees(int r, int x, int G) const {
+    if (!LEAN) return word[r];
+    if (!mask) return ~0ull;
+    return mask[(row0 + min(16 * r + anew<true>(x) % kRows, rows - 1)) / G];
+  }
 
   // The queries, which wait for nothing that the kernel reads first.
   __device__ __forceinline__ void load(const Kv4AttentionArgs& a, int hk, int first_row, int n_rows, int lane, int wave, uint4* lds) {
@@ -252,7 +264,7 @@ struct Rows {
     mask = a.mask;
     far = lds;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) word[r] = !LEAN && mask ? mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G] : ~0ull;
+    for (int r = 0; r < (LEAN ? 0 : RT); ++r) word[r] = mask ? mask[(row0 + min(16 * r + x % kRows, rows - 1)) / G] : ~0ull;
 #pragma unroll
     for (int r = 0; r < (kHeld ? RT : 1); ++r) {
       const int row = row0 + min(16 * (kHeld ? r : wave) + x % kRows, rows - 1), bi = row / G;
@@ -263,7 +275,7 @@ struct Rows {
   }
 
   // (the same in all wavefronts of a workgroup where queries are in LDS)
-  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane, int wave) {
+  __device__ __forceinline__ void begin(const Kv4AttentionArgs& a, int n, int end, int lane, int wave, float* unit_lds) {
     const int t = lane >> 4, skip = (lane & 15) / kRows * NZ;
     slot0 = 16 * (skip / 4) + 4 * t + skip % 4;
     key1 = end;
@@ -300,29 +312,67 @@ struct Rows {
       for (int d = 0; d < NO; ++d) o[r][d] = floatx4{};
     }
     wide = false;
-    set_unit(kLeastUnit<F16>);
+    units = unit_lds;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) unit_of(r, lane & 15) = kLeastUnit<F16>;
+    limit = __builtin_ldexpf(1.f, kLeastUnit<F16> + kRoom);
   }
 
-  __device__ __forceinline__ void set_unit(int to) {
-    unit = to;
-    limit = __builtin_ldexpf(1.f, F16 ? unit : unit + 60);
+  // Sizes up to 2^(unit + kRoom) fit a unit.
+  static constexpr int kRoom = F16 ? 0 : 60;
+  // (every lane of a row writes the row's, and reads what it wrote)
+  __device__ __forceinline__ float& unit_of(int r, int x) const {
+    return units[kRows * r + anew<LEAN>(x) % kRows];
+  }
+  // Of a value: its step, and in bf16 the middle of its range.
+  static __device__ __forceinline__ float size_of(float step, float middle) {
+    return F16 ? step : fmaxf(step, fabsf(middle) * 0.0625f);
   }
 
-  // Grows the unit to what values of the upper lanes' sizes need.
-  __device__ __forceinline__ void fit(float size, int lane) {
-    if (static_cast<uint32_t>(__ballot(size > limit) >> 32) == 0) return;
-    const float finite = lane & 32 && size < INFINITY ? size : 0.f;
-    const int grown = max(unit, __builtin_amdgcn_frexp_expf(wave_allmax(finite)) - (F16 ? 0 : 60));
-    const float f = __builtin_ldexpf(1.f, unit - grown);
+  // Which of this lane's slots a row of that word sees, of those from slot `at` of the step on (one of its fours).
+  __device__ __forceinline__ uint32_t seen_from(uint64_t row, int at, int j0) const {
+    return seen4(row, mask ? j0 + at - base : 0, key1 - j0 - at) & ((1 << min(NZ, 4)) - 1);
+  }
+
+  // Grows the rows' units to what the values that they see need, the upper lanes' `own` where all rows see all of them.
+  // Slots that a row does not see leave its unit as it is: they have no effect on it.
+  __device__ __forceinline__ void fit(float own, const float2* values, int j0, int lane, int G) {
+    const int x = lane & 15;
+    float size = lane & 32 && own < INFINITY ? own : 0.f, least = INFINITY;
+    const bool some = cut(j0);
+    if (!some) size = wave_allmax(size);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      l[r] *= f;
-      add[r] *= f;
+      if (some) {
+        const uint64_t row = sees(r, x, G);
+        size = 0.f;
 #pragma unroll
-      for (int d = 0; d < NO; ++d) o[r][d] *= f;
-      mc[r] = m[r] == -INFINITY ? 0.f : m[r] * c - static_cast<float>(kTop<F16> - grown);
+        for (int i = 0; i < NZ; i += 4) {
+          const int at = slot0 + i / 4 * 16;
+          const uint32_t seen = seen_from(row, at, j0);
+#pragma unroll
+          for (int u = 0; u < min(NZ, 4); ++u) {
+            const float2 y = values[at + u];
+            const float of = size_of(y.x, y.y);
+            if ((seen >> u) & 1 && of < INFINITY) size = fmaxf(size, of);
+          }
+        }
+        size = row_max<SP>(size);
+      }
+      const float unit = unit_of(r, x);
+      const float need = size > 0.f ? fmaxf(unit, static_cast<float>(__builtin_amdgcn_frexp_expf(size) - kRoom)) : unit;
+      if (need > unit) {
+        const float f = __builtin_amdgcn_exp2f(unit - need);
+        l[r] *= f;
+        add[r] *= f;
+#pragma unroll
+        for (int d = 0; d < NO; ++d) o[r][d] *= f;
+        unit_of(r, x) = need;
+        mc[r] = m[r] == -INFINITY ? 0.f : m[r] * c - (kTop<F16> - need);
+      }
+      least = fminf(least, need);
     }
-    set_unit(grown);
+    limit = __builtin_amdgcn_exp2f(-wave_allmax(-least) + kRoom);
   }
 
   // Whether some row does not see some of the slots j0 .. j0 + 31 (the same in all lanes).
@@ -362,11 +412,11 @@ struct Rows {
     if (cut(j0)) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        if (LEAN && mask) word[r] = sees(r, x, G);
+        const uint64_t row = sees(r, x, G);
 #pragma unroll
         for (int i = 0; i < NZ; i += 4) {
-          const int at = slot0 + i / 4 * 16, first = j0 + at;
-          const uint32_t seen = seen4(word[r], mask ? first - base : 0, key1 - first) & ((1 << min(NZ, 4)) - 1);
+          const int at = slot0 + i / 4 * 16;
+          const uint32_t seen = seen_from(row, at, j0);
 #pragma unroll
           for (int u = 0; u < min(NZ, 4); ++u) z[r][i + u] = (seen >> u) & 1 ? z[r][i + u] : -INFINITY;
           if (seen & odd >> at) add[r] = NAN;
@@ -399,7 +449,7 @@ struct Rows {
           for (int d = 0; d < NO; ++d) o[r][d] *= f;
         }
         m[r] = up;
-        mc[r] = up == -INFINITY ? 0.f : up * c - static_cast<float>(kTop<F16> - unit);
+        mc[r] = up == -INFINITY ? 0.f : up * c - (kTop<F16> - unit_of(r, x));
         far |= fabsf(mc[r]) > kFine;
       }
       wide = __any(far);
@@ -413,7 +463,7 @@ struct Rows {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const float from = m[r] == -INFINITY ? 0.f : m[r];
-        sub[r] = static_cast<float>(unit - kTop<F16>);
+        sub[r] = unit_of(r, x) - kTop<F16>;
 #pragma unroll
         for (int i = 0; i < NZ; ++i) z[r][i] -= from;
       }
@@ -533,7 +583,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   // Chunk `lane` of a block's keys or values: a wavefront reads them in one piece, and one tile's rows are the only
   // ones to read them (64 caches of 500 to 8000 keys: 58 us as ordinary loads, 53 so; 32 of 40 to 4000 with 32 heads: 56, 51).
   auto codes = [&](const uint8_t* blk) {
-    const auto* at = reinterpret_cast<const Codes*>(blk + lane * static_cast<uint32_t>(sizeof(Codes)));
+    const auto* at = reinterpret_cast<const Codes*>(blk + anew<(RT > 2)>(lane) * static_cast<uint32_t>(sizeof(Codes)));
     if constexpr (RT == 1) return __builtin_nontemporal_load(at);
     return *at;
   };
@@ -542,9 +592,6 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
     return *reinterpret_cast<const uint32_t*>((lane & 16 ? b1 : b0) + static_cast<uint32_t>(16 * W + (lane & 32 ? 64 : 0) + 4 * x));
   };
   float2* const my_marks = marks + 64 * wave;
-  // what joins a slot's lowest value, in steps: of a value the middle of its codes, of a key less what bf16 codes
-  // stand on
-  const float middle = lane & 32 ? 8.f : F16 ? 0.f : -16.f;
   const CodeBits<F16> bits;
 
   const int steps = key1 > my0 ? (key1 - my0 + kStep * KW - 1) / (kStep * KW) : 0;
@@ -558,21 +605,26 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
   v[0] = codes(b0 + 8 * W);
   v[1] = codes(b1 + 8 * W);
   __builtin_amdgcn_sched_barrier(0);
-  rs.begin(a, n, key1, lane, wave);
+  rs.begin(a, n, key1, lane, wave, stat + 2 * M * wave);   // (which the join takes when they are done with)
   for (int step0 = 0; step0 < steps; step0 += kLooked) {
     const int end = min(steps - step0, kLooked);
     for (int nth = 0; nth < end; ++nth) {
       const int step = step0 + nth, j0 = my0 + kStep * KW * step;
       // ---- steps and lowest values: one slot a lane, handed round through LDS
+      const int slot = anew<(RT > 2)>(lane);
       float st = kv4_step<F16>(mark), y = kv4_low<F16>(mark);
       uint32_t odd = 0;
       if (rs.cut(j0)) {
-        const bool past = j0 + (lane & 31) >= key1;                     // what lies past the run may be anything
+        const bool past = j0 + (slot & 31) >= key1;                     // what lies past the run may be anything
         const bool finite = fabsf(st) < INFINITY && fabsf(y) < INFINITY;
         odd = static_cast<uint32_t>(__ballot(!past && !finite) >> 32);
-        if (past || (lane & 32 && !finite)) st = y = 0.f;
+        if (past || (slot & 32 && !finite)) st = y = 0.f;
       }
-      my_marks[lane] = make_float2(st, fmaf(middle, st, y));
+      // what joins the lowest value, in steps: of a value the middle of its codes, of a key less what bf16 codes stand on
+      const float mid = fmaf(slot & 32 ? 8.f : F16 ? 0.f : -16.f, st, y);
+      my_marks[slot] = make_float2(st, mid);
+      const float size = R::size_of(st, mid);
+      const bool large = __ballot(size > rs.limit) >> 32;                // of the values, which upper lanes have
       asm volatile("" ::: "memory");             // LDS works in order for a wavefront; so must the compiler
       __builtin_amdgcn_wave_barrier();
       // ---- S^T = K Q^T over the codes
@@ -601,7 +653,7 @@ __global__ __launch_bounds__(64 * KW, RT == 1 && KW < 8 ? 3 : 2) void kv4_attend
           }
         }
       }
-      rs.fit(fmaxf(st, fabsf(y) * 0.0625f), lane);
+      if (large) rs.fit(size, my_marks + 32, j0, lane, G);
       // ---- the next step's keys
       b0 = block(nth + 1, step + 1, 0);
       b1 = block(nth + 1, step + 1, 1);
