@@ -136,6 +136,7 @@ struct Kv4AttentionArgs {
   int B, L, H, Hkv, D, max_seq_len;
   float scale;
 };
+bool kv4_attention_plan_info(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len, int* out);
 size_t kv4_attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len);
 // `pre` holds the same call as the attention over a 2-byte prefix sees it (no cache).  False, with nothing launched,
 // where the workspace is too small.

@@ -29,6 +29,7 @@
 // A wavefront's 800 instructions before and after its steps count as two or three of them.
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 #include <type_traits>
 
 #include "attention_plan.h"
@@ -880,18 +881,20 @@ size_t bytes_of(const CallPlan& c, int64_t rows, int D) {
   return (runs + 3) / 4 * 16 + runs * D * sizeof(float);
 }
 
+// Lanes of each quarter that share a row, of up to 16.
+int lanes_of(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 2 : 1; }
+
 template <bool F16, int W>
 void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
   const dim3 grid(tile_grid(c.p.groups, c.p.tiles)), threads(64 * c.waves);
   const int rows = a.L * (a.H / a.Hkv);
   auto few = [&](auto waves) {
     constexpr int KW = waves;
-    if (rows <= 4)
-      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 4>), grid, threads, 0, s, a, c.p);
-    else if (rows <= 8)
-      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 2>), grid, threads, 0, s, a, c.p);
-    else
-      hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 1>), grid, threads, 0, s, a, c.p);
+    switch (lanes_of(rows)) {
+      case 4: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 4>), grid, threads, 0, s, a, c.p); break;
+      case 2: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 2>), grid, threads, 0, s, a, c.p); break;
+      default: hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 1, KW, 1>), grid, threads, 0, s, a, c.p);
+    }
   };
   if (c.rows > 32)
     hipLaunchKernelGGL((kv4_attend_kernel<F16, W, 4, 4, 1>), grid, threads, 0, s, a, c.p);
@@ -910,6 +913,17 @@ void launch_own(const Kv4AttentionArgs& a, const CallPlan& c, hipStream_t s) {
 // Workspace: where rows have several runs, a log-sum-exp and D sums of each.
 size_t kv4_attention_workspace_bytes(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len) {
   return bytes_of(make_plan(B, L, H, Hkv, prefix_len, max_seq_len), static_cast<int64_t>(B) * L * H, D);
+}
+
+// What the own keys of a call run on: the kernel's width, rows of a tile, wavefronts and lanes a row, then its row tiles,
+// runs, slots of a run, and whether long runs go first.  False where there is no such launch.
+bool kv4_attention_plan_info(int B, int L, int H, int Hkv, int D, int prefix_len, int max_seq_len, int* out) {
+  const CallPlan c = make_plan(B, L, H, Hkv, prefix_len, max_seq_len);
+  if (!c.p.groups) return false;
+  const int info[] = {kv4_width(D), c.rows, c.waves, c.rows > 16 ? 1 : lanes_of(L * (H / Hkv)), c.p.tiles,
+                      c.p.splits - c.p.own_first, c.p.run, c.p.by_length};
+  std::copy(std::begin(info), std::end(info), out);
+  return true;
 }
 
 bool launch_kv4_attention(const Kv4AttentionArgs& a, const AttentionArgs& pre, bool f16, void* ws, size_t ws_bytes, hipStream_t s) {
