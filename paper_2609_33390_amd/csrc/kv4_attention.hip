@@ -18,14 +18,12 @@
 // of a wavefront, the next ones' on the way; the wavefronts of a workgroup take
 // steps in turn and join through LDS.
 //
-// What bounds it.  Single tokens of a batch: the read of the cache (64 caches of 500 to 8000
-// slots of 8 heads, 296 MB in 52 us, 5.7 TB/s).  32 rows: vector and matrix instructions, which take
-// turns on a SIMD whatever its wavefronts are: a step's 290 vector ones (56 make the keys' codes,
-// 56 the values', 32 take steps and lowest values to the logits, 104 make the weights and their sums)
-// keep it for 1215 cycles, its 32 products for 512, and a step takes 1725.
-// So more wavefronts a SIMD (3 with the queries in LDS) or codes two steps ahead change nothing, and 64 rows a wavefront,
-// which make the codes once for twice as many, take 2.45 us a step where 32 take 1.6 (two wavefronts a SIMD).
-// (One block of 32 over 65536 slots: 55 us, 0.62 PFLOP/s.)
+// What bounds it.  Single tokens of a batch: the read of the cache (64 caches of 500 to 8000 slots of 8 heads, 296 MB in
+// 51 us, 5.8 TB/s).  32 rows: vector instructions, 290 a step (56 make the keys' codes, 56 the values', 32 take steps and lowest
+// values to the logits, 104 make the weights and their sums) beside its 32 products.  Of the cycles in which a CU has
+// wavefronts its SIMDs spend 67% on them and 24% on products, a third of those beside vector instructions; 17% on neither (64
+// blocks of 16 over 16 to 4096 slots: 62 us, 0.55 PFLOP/s).  64 rows a wavefront make the codes once for twice as many: 63% and
+// 30% (one block of 32 over 65568 slots: 50 us, 0.69 PFLOP/s; with the join 55, with tiles of 32 rows 60).
 // A wavefront's 800 instructions before and after its steps count as two or three of them.
 #include <algorithm>
 #include <cmath>
@@ -510,7 +508,7 @@ struct Rows {
 
   // Brings what joins every element into the sums, which are then of values about the middle of their heads' ranges.
   // Sums of codes on 64 or 128 grow with the length, sums about the middle with its root, and so do their roundings
-  // (131072 slots a run: f16 outputs off by 6.5e-4 without this, by 3.1e-4 with it once in 31 steps).
+  // (131072 slots a run: f16 outputs off by 6.5e-4 without this, by 3.1e-4 to 3.5e-4 with it once in 31 steps).
   __device__ __forceinline__ void center() {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -780,11 +778,12 @@ bool by_length(int B, double rounds) { return B > 1 && B <= 64 && rounds > 1; }
 constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
 // More than 16 rows: tiles of 32 or 64, by what a plan would take in us.  A round of workgroups takes `start` and `step` for
-// each of its steps of 128 slots; a batch's lengths may be all the same or, as likely again, anything up to the
-// bound.  Tiles of 64 make the codes half as often, but take longer to start and join, and leave fewer workgroups to
-// even out lengths with.  (One block of 32 with 4 heads a key head over 65568 slots: 57 us with 64, 67 with 32; 8 of
-// them over 8192: 55, 62; one of 64 with 8 heads over 32768: 56, 62; 64 of 16 over 16 to 4096: 76, 68; 13 of 21 with 5 over 5 to
-// 1777: 44, 40.)
+// each of its steps of 128 slots; a batch's lengths may be all the same or anything up to the bound, and the second
+// counts twice: a plan for it loses less where they are the same than the other way round.  Tiles of 64 make the codes half as
+// often, but take longer to start and join, and leave fewer workgroups to even out lengths with.  In us with 64 and with 32 rows:
+// one block of 32 with 4 heads a key head over 65568 slots 55 and 60; one of 64 with 8 heads over 32768 91 and 107; 8 of 32 over
+// 8192 53 and 63, over 32 to 8192 52 and 43; 64 of 16 over 4096 98 and 114, over 16 to 4096 74 and 63; 13 of 21 with 5 over 5 to
+// 1777 44 and 38.  (A bound far past the lengths is planned for as if they reached it.)
 Shape many_rows(int keys, int B, int64_t whole, int rows, int64_t all_rows, bool prefix) {
   constexpr double kTwo = 4., kRow = 2e-4;
   Shape best{32, 4, {}};
@@ -814,12 +813,14 @@ Shape many_rows(int keys, int B, int64_t whole, int rows, int64_t all_rows, bool
 
 // Up to 16 rows: 2, 4 or 8 wavefronts a workgroup, by what a plan would take in us.  A round of wavefronts takes
 // kStart and kStep for each of its steps; lengths may be all the same or anything up to the bound, and the
-// plan is for the mean of both.  Runs cost a second launch, the scratch (together at least kTwo a call, where one
-// launch takes kOne) and the partial sums.  So a batch is split when it does not fill the GPU,
-// and otherwise takes the wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52 us
-// with 8 (68 with 4 and 123 with 2, in one round; 56 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 51 with 4 (60
-// with 8, 67 with 2), 128 of 600 17 with 2 (20 with 4, 25 with 8), 16 of 6000 22 in 2 runs with 8 (28 whole), one of 1500
-// 10.8 whole with 8 (12.2 to 13.9 in runs), 4 of 32768 27 in 8 runs with 8 (33 in 16, 41 in 4).
+// plan is for the mean of both: weighed as for more rows, 8 caches of 16384 slots would be split in 8 (32 us; 28 in 4; of 100 to
+// 16384 slots 25 and 23).  Runs cost a second launch, the scratch (together at least kTwo a call,
+// where one launch takes kOne) and the partial sums.  So a batch is split when it does not fill the GPU, and otherwise takes the
+// wavefronts that make two rounds, the long caches first: 64 caches of 500 to 8000 slots 52 us with 8 (64 with 4 and 112 with 2,
+// in one round; 55 with 4 and 2 runs), 32 of 40 to 4000 with 32 heads 48 with 4 (58 with 8, 65 with 2), 128 of 600 17 with 2 (20
+// with 4, 25 with 8), 16 of 6000 22 in 2 runs with 8 (28 whole), one of 1500 9.9 whole with 8 (12.6 in runs), 4 of 32768 27 in 8
+// runs with 8 (32 in 16, 40 in 4).  At the edge of two plans the mean is for the one and loses by the other: 128 caches of
+// 4000 slots take 84 with 2 (93 with 8, 97 with 4), but of 16 to 4000 65 (59, 58).
 Shape few_rows(int keys, int B, int64_t whole, int64_t rows, bool prefix) {
   constexpr double kStart = 4.3, kStep = 1.1, kOne = 9., kTwo = 12.5, kRow = 2 * 512 / 5e6;
   Shape best{16, 8, {}};

@@ -9,9 +9,9 @@
 // a decoding step and a prompt give alike, share no bytes across wavefronts.
 //
 // Both passes are bound by memory.  Writing 8 x 4096 tokens of 8 heads of 128 (134 MB in, 36 MB out) takes
-// 19 us (the last-level cache helps: more than a copy's rate); reading 16 x 8190 slots back (97 MB in, 537 MB out)
-// takes 92 us on one cache over and over, 6.9 TB/s, and 107 on several in turn.  64 single tokens take 5 us to
-// write and 4.8 to read, of which the launch is 3.
+// 20 us (the last-level cache helps: more than a copy's rate); reading 16 x 8190 slots back (97 MB in, 537 MB out)
+// takes 90 us on one cache over and over, 7.0 TB/s, and 103 on several in turn.  64 single tokens take 5.1 us to
+// write and 4.7 to read, of which the launch is 3.
 #include "kernels.h"
 #include "kv4_common.h"
 
