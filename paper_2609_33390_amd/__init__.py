@@ -1096,7 +1096,8 @@ class KVCache4:
     ``pages`` is [n_pages, n_kv_heads, kv4_page_bytes(page_size, d_head)] uint8,
     contiguous in its last dimension (pages and heads may lie further apart);
     ``dtype`` (bfloat16 or float16) is that of the keys and values written and
-    read and of the queries.  ``block_table`` [B, max_pages] int32 lists each
+    read and of the queries.  A slot of a head takes 72 bytes up to 64 elements and
+    136 beyond, so heads of 16 and 8 take more than in 2 bytes.  ``block_table`` [B, max_pages] int32 lists each
     sequence's pages and ``seq_len`` [B] int32 the slots it holds, the block in
     flight included.  The tensors stay the caller's, as with :class:`KVCache`:
     lengths and pages may be written between calls, which tensors they are is
