@@ -361,7 +361,7 @@ struct Rows {
       const float unit = unit_of(r, x);
       const float need = size > 0.f ? fmaxf(unit, static_cast<float>(__builtin_amdgcn_frexp_expf(size) - kRoom)) : unit;
       if (need > unit) {
-        const float f = __builtin_amdgcn_exp2f(unit - need);
+        const float f = __builtin_ldexpf(1.f, static_cast<int>(unit - need));
         l[r] *= f;
         add[r] *= f;
 #pragma unroll
@@ -371,7 +371,7 @@ struct Rows {
       }
       least = fminf(least, need);
     }
-    limit = __builtin_amdgcn_exp2f(-wave_allmax(-least) + kRoom);
+    limit = __builtin_ldexpf(1.f, static_cast<int>(-wave_allmax(-least)) + kRoom);
   }
 
   // Whether some row does not see some of the slots j0 .. j0 + 31 (the same in all lanes).
