@@ -31,7 +31,7 @@
  *     takes no strides.
  *   - Rows of a block are numbered r = b * L + (i - 1) for sequence b and
  *     in-block position i = 1..L.
- *   - `stream` is a hipStream_t (NULL = the default stream).  Work is queued
+ *   - `stream` is a hipStream_t (NULL = the current device's default stream).  Work is queued
  *     on it asynchronously; nothing synchronises.
  *   - Every call returns a brisk_status.  Arguments are validated on the host
  *     before any HIP call: on an error return nothing has been launched and no

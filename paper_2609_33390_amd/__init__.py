@@ -279,14 +279,22 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 # The current stream's handle without a Stream object around it, where torch offers that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# The current device's number, the same way.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_ptr(device: torch.device, stream) -> Optional[int]:
-    if stream is None:
-        if _raw_stream is not None and device.index is not None:
-            return _raw_stream(device.index)
-        stream = torch.cuda.current_stream(device)
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    """The handle of the stream that a call queues on.  Every device's default stream has the handle 0, which
+    means the current device's: with tensors of another device that is refused."""
+    if stream is None and _raw_stream is not None and device.index is not None:
+        handle = _raw_stream(device.index)
+    else:
+        stream = torch.cuda.current_stream(device) if stream is None else stream
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if not handle and device.type == "cuda" and device.index not in (None, _current_device()):
+        raise ValueError(f"the tensors are on {device}, the default stream is that of cuda:{_current_device()}: call "
+                         f"under torch.cuda.device({device.index}), or on another stream of {device}")
+    return handle
 
 
 _ws: Dict[Tuple[Optional[int], str, Optional[int]], torch.Tensor] = {}
