@@ -422,7 +422,8 @@ struct Rows {
         }
       }
     }
-    // The subtracted logit follows the maximum only once that is kLag ahead.
+    // The subtracted logit follows a row's maximum only once that is kLag ahead, and no other row's: what that row sees
+    // and this one does not has no effect on it.
     float top[RT];
     bool behind = false;
 #pragma unroll
@@ -433,22 +434,24 @@ struct Rows {
       behind |= (top[r] - m[r]) * c > kLag<F16>;
     }
     if (__any(behind)) {
-      bool far = false, held = false;              // whether a row holds anything yet
-#pragma unroll
-      for (int r = 0; r < RT; ++r) held |= m[r] != -INFINITY;
-      held = __any(held);
+      bool far = false;
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float up = fmaxf(m[r], row_max<SP>(top[r]));
-        const float f = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - up) * c);
-        if (held) {
-          l[r] *= f;
-          add[r] *= f;
+        const float best = row_max<SP>(top[r]);
+        const bool moves = (best - m[r]) * c > kLag<F16>;
+        if (__any(moves)) {                        // most often a tile of few, or of none
+          if (__any(moves && m[r] != -INFINITY)) { // (nothing to scale in a row's first step)
+            const float f = !moves ? 1.f : m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[r] - best) * c);
+            l[r] *= f;
+            add[r] *= f;
 #pragma unroll
-          for (int d = 0; d < NO; ++d) o[r][d] *= f;
+            for (int d = 0; d < NO; ++d) o[r][d] *= f;
+          }
+          if (moves) {
+            m[r] = best;
+            mc[r] = best * c - (kTop<F16> - unit_of(r, x));
+          }
         }
-        m[r] = up;
-        mc[r] = up == -INFINITY ? 0.f : up * c - (kTop<F16> - unit_of(r, x));
         far |= fabsf(mc[r]) > kFine;
       }
       wide = __any(far);
@@ -461,8 +464,9 @@ struct Rows {
     if (wide) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float from = m[r] == -INFINITY ? 0.f : m[r];
-        sub[r] = unit_of(r, x) - kTop<F16>;
+        const bool far = fabsf(mc[r]) > kFine;
+        const float from = far ? m[r] : 0.f;
+        sub[r] = far ? unit_of(r, x) - kTop<F16> : mc[r];
 #pragma unroll
         for (int i = 0; i < NZ; ++i) z[r][i] -= from;
       }

@@ -1,5 +1,5 @@
-"""GPU checks that values which a row does not see have no effect on it, whatever their size: not on
-the scale that its weights are held at either."""
+"""GPU checks that keys and values which a row does not see have no effect on it, whatever their size: not on
+the logit that it subtracts or the scale that its weights are held at either."""
 import numpy as np
 import pytest
 import torch
@@ -96,3 +96,26 @@ def test_f16_weights_beside_a_seen_value_of_a_large_step():
     o, z, tol, ltol = c.expect()
     step = 2 * torch.finfo(torch.float16).max / 15
     c.check(*_run(c), want=(o, z, tol + 8 * 2.0 ** -36 * step, ltol))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [20.0, 1e4])
+@pytest.mark.parametrize("L,G,n", [(2, 1, 40), (2, 4, 700), (5, 2, 3000), (16, 1, 500), (20, 1, 300), (32, 4, 9000), (40, 2, 5000)])
+def test_rows_are_the_same_bits_beside_any_hidden_key(L, G, n, size, D, dtype):
+    """The block's last slot, which only its last position sees, has a key whose logits are far above all others (or so
+    large that differences of them are taken before they are scaled): no other row's maximum moves with that one's."""
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(1, n, 2, D, generator=g).to(TYPES[dtype]) for _ in range(2))
+    q = torch.randn(1, L, 2 * G, D, generator=g).to(TYPES[dtype])
+    q[:, L - 1] = q[:, L - 1, :1]
+    far = k.clone()
+    far[0, n - 1] = (size * q[0, L - 1, 0].float()).to(TYPES[dtype])
+    outs = []
+    for x in (k, far):
+        c = Case4(brisk, 1, L, 2 * G, 2, D, None, [n], mask="causal", dtype=dtype, seed=n + L, k=x, v=v)
+        c.q = q                                    # logits so alike that the subtracted one may lag behind the largest
+        out, lse = _run(c)
+        outs.append((out[:, :L - 1], lse[:, :L - 1], lse[:, L - 1]))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert torch.isfinite(outs[1][2]).all() and (outs[1][2] > outs[0][2] + 100).all()
