@@ -116,7 +116,7 @@ _lib_lock = threading.Lock()
 
 def lib() -> ctypes.CDLL:
     """The loaded library; raises if it has not been built."""
-    global _lib
+    global _lib, _several_devices
     if _lib is not None:
         return _lib
     with _lib_lock:
@@ -213,6 +213,7 @@ def lib() -> ctypes.CDLL:
             L.brisk_kv4_attention_workspace_size.argtypes = [_i32] * 7 + [_szp]
             L.brisk_kv4_attention.restype = ctypes.c_int
             L.brisk_kv4_attention.argtypes = [_cache4] + L.brisk_block_attention.argtypes[1:]
+            _several_devices = torch.cuda.device_count() > 1
             _lib = L
         return _lib
 
@@ -279,8 +280,9 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 # The current stream's handle without a Stream object around it, where torch offers that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-# The current device's number, the same way.
+# The current device's number, the same way, and whether there is another one (known once the library is loaded).
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_several_devices = False
 
 
 def _stream_ptr(device: torch.device, stream) -> Optional[int]:
@@ -291,7 +293,7 @@ def _stream_ptr(device: torch.device, stream) -> Optional[int]:
     else:
         stream = torch.cuda.current_stream(device) if stream is None else stream
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if not handle and device.type == "cuda" and device.index not in (None, _current_device()):
+    if _several_devices and not handle and device.type == "cuda" and device.index not in (None, _current_device()):
         raise ValueError(f"the tensors are on {device}, the default stream is that of cuda:{_current_device()}: call "
                          f"under torch.cuda.device({device.index}), or on another stream of {device}")
     return handle

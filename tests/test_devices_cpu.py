@@ -12,8 +12,9 @@ class Stream:
 
 @pytest.fixture
 def current(monkeypatch):
-    """The current device, and each device's current stream."""
+    """Two devices: which is current, and each one's current stream."""
     now = {"device": 0, "streams": {0: 0, 1: 0}}
+    monkeypatch.setattr(brisk, "_several_devices", True)
     monkeypatch.setattr(brisk, "_current_device", lambda: now["device"])
     monkeypatch.setattr(brisk, "_raw_stream", lambda index: now["streams"][index])
     return now
