@@ -21,7 +21,7 @@
 // What bounds it.  Single tokens of a batch: the read of the cache (64 caches of 500 to 8000 slots of 8 heads, 296 MB in
 // 51 us, 5.8 TB/s).  32 rows: vector instructions, 290 a step (56 make the keys' codes, 56 the values', 32 take steps and lowest
 // values to the logits, 104 make the weights and their sums) beside its 32 products.  Of the cycles in which a CU has
-// wavefronts its SIMDs spend 67% on them and 24% on products, a third of those beside vector instructions; 17% on neither (64
+// wavefronts its SIMDs spend 68% on them and 25% on products, a third of those beside vector instructions; 17% on neither (64
 // blocks of 16 over 16 to 4096 slots: 62 us, 0.55 PFLOP/s).  64 rows a wavefront make the codes once for twice as many: 63% and
 // 30% (one block of 32 over 65568 slots: 50 us, 0.69 PFLOP/s; with the join 55, with tiles of 32 rows 60).
 // A wavefront's 800 instructions before and after its steps count as two or three of them.
